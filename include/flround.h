@@ -59,7 +59,8 @@ typedef enum {
   FL_ERR_HIP = -5,     /* a HIP runtime call or a kernel launch failed          */
   FL_ERR_NOMEM = -6,   /* host or device allocation failed                      */
   FL_ERR_SCRATCH = -7  /* fl_round_noalloc: the layout's per-segment workspace
-                          exceeds the library's static scratch                 */
+                          exceeds the library's static scratch; fl_head_*,
+                          fl_top_logits: the workspace given is too small      */
 } fl_status;
 
 #define FL_MAX_PEERS 64  /* upper bound on R */
@@ -73,7 +74,8 @@ const char* fl_status_string(int status);
  * minor k needs a library of minor >= k.  Minor 1: the FL+HSDP entry
  * points; 2: the outer step; 3: fl_lr_cosine and fl_round_cfg.step_lr;
  * 4: fl_round_cfg.max_grad_norm and the clipping entry points;
- * 5: fl_round_cfg.grad_scratch. */
+ * 5: fl_round_cfg.grad_scratch; 8: the output head (fl_head_*,
+ * fl_top_logits). */
 int fl_version(void);
 
 /* ------------------------------------------------------------------------
@@ -430,6 +432,113 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
                   uint16_t* wire, const uint16_t* const* replicas, const float* bcast_master,
                   float* master, float* m, float* v, uint16_t* working, float* seg_sumsq,
                   void* stream);
+
+/* ------------------------------------------------------------------------
+ * The output head: where a local step's gradients begin, and what federation
+ * groups exchange when they share predictions in place of parameters.
+ *
+ * With T tokens, V words of the vocabulary and D elements of the hidden state,
+ *     z[t][v] = sum_d hidden[t][d] * weight[v][d]
+ * is never stored.  bf16 inputs, products summed in fp32; these functions use
+ * the matrix cores, so their sums run in an order of their own (fixed for given
+ * sizes: the same call gives the same bits) and the conventions on arithmetic
+ * at the top of this file do not apply to them.
+ *
+ * Conventions that differ from those at the top: there is no layout handle; the
+ * device is the current one.  weight and workspace need 16-byte alignment
+ * (workspace: any; it is rounded up), the others that of their elements.  hidden
+ * and weight may have longer rows than they use (the strides, in elements; 0:
+ * rows follow each other).  Weight rows of a width or stride that is not a
+ * multiple of 8 are copied to the workspace by every call.
+ *
+ * workspace: device memory, fl_head_workspace_bytes(shape, k, grad) bytes
+ *   (k = 0 for fl_head_loss and its gradient; grad nonzero for the gradients;
+ *   0 is returned for an invalid shape), owned by the caller, for one call at a
+ *   time; nothing is kept in it between calls.  Less: FL_ERR_SCRATCH.  No call
+ *   allocates or synchronises, and all may be captured into a HIP graph.
+ *
+ * fl_head_loss -- cross entropy over the vocabulary:
+ *     lse[t] = log sum_v exp(z[t][v]);  target[t] = z[t][labels[t]]
+ *     loss[t] = lse[t] - target[t]
+ *   labels: device, T int64.  A token with a negative label takes no part: its
+ *   three results are 0 and its hidden state is not looked at.  A label >= V
+ *   gives NaN.  lse and target are what the gradient needs.
+ *
+ * fl_head_loss_grad -- gradient of sum_t dloss[t] * loss[t]:
+ *     G[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - (v == labels[t]))
+ *     dhidden = G weight;  dweight = G^T hidden
+ *   dloss: device, T floats (1 / tokens that take part, for a mean).  dhidden:
+ *   T x D bf16, 0 for a token that takes no part; dweight: V x D bf16, the
+ *   peer gradient that fl_local_step takes for the head's segment.  Both are
+ *   written, not added to.  G is made again for a piece of the vocabulary at a
+ *   time and rounded to bf16 relative to the largest |dloss|, which leaves a
+ *   relative error of up to 2^-8 per term beside that of rounding the results.
+ *   The workspace holds one piece of G (256 MiB, or 8192 words).
+ *
+ * fl_head_distill -- distillation from a teacher's top logits:
+ *     logp[t][j] = teacher[t][j] / tau - A[t], A[t] = teacher_lse[t], or, where
+ *       teacher_lse is NULL, log sum_j exp(teacher[t][j] / tau)
+ *     lse[t] = log sum_v exp(z[t][v] / tau);  target[t][j] = z[t][ids[t][j]]
+ *     loss[t] = tau^2 sum_j p[t][j] (logp[t][j] - target[t][j] / tau + lse[t])
+ *   with p = exp(logp): the divergence of the student from the teacher, over the
+ *   listed words.  ids: device, T x k int32; an entry < 0 is absent, whatever
+ *   its teacher logit; one >= V gives NaN; a repeated one counts each time.  A
+ *   teacher logit of -inf has probability 0.  A token with no entry that is
+ *   present and above -inf takes no part.  teacher: T x k floats; teacher_lse:
+ *   T floats at the same tau (fl_top_logits gives it) or NULL.  1 <= k <=
+ *   FL_MAX_TARGETS; tau finite, > 0.
+ *
+ * fl_head_distill_grad -- its gradient, as fl_head_loss_grad with
+ *     G[t][v] = dloss[t] tau (exp(z[t][v] / tau - lse[t]) sum_j p[t][j]
+ *                             - sum over j with ids[t][j] == v of p[t][j])
+ *   (teacher and teacher_lse are constants).
+ *
+ * fl_top_logits -- the k largest of each row of logits, largest first, ties to
+ *   the lowest id, and lse[row] = log sum_v exp(logits[row][v] / tau) (lse may
+ *   be NULL).  logits: rows x vocab of dtype FL_BF16 or FL_F32, `stride`
+ *   elements between rows (0: vocab).  NaN counts as larger than any number,
+ *   -0 as 0.  values: rows x k floats; ids: rows x k int32.  1 <= k <=
+ *   min(vocab, FL_MAX_TARGETS).  workspace: fl_top_workspace_bytes, NULL where
+ *   that is 0.
+ *
+ * Limits (FL_ERR_INVALID beyond): tokens and rows <= 2^20, vocab <= 2^24
+ * (fl_top_logits 2^20), width <= 2^16, strides of hidden and weight <= 2^22,
+ * ceil(tokens / 128) * ceil(vocab / 128) <= 2^22.
+ * ---------------------------------------------------------------------- */
+#define FL_MAX_TARGETS 128
+
+enum { FL_BF16 = 0, FL_F32 = 1 };
+
+typedef struct {
+  int64_t tokens;        /* T >= 0                                        */
+  int64_t vocab;         /* V >= 1                                        */
+  int64_t width;         /* D >= 1                                        */
+  int64_t hidden_stride; /* elements between rows of hidden, or 0: width  */
+  int64_t weight_stride; /* elements between rows of weight, or 0: width  */
+} fl_head_shape;
+
+size_t fl_head_workspace_bytes(const fl_head_shape* shape, int k, int grad);
+int fl_head_loss(const fl_head_shape* shape, const uint16_t* hidden, const uint16_t* weight,
+                 const int64_t* labels, float* loss, float* lse, float* target, void* workspace,
+                 size_t workspace_bytes, void* stream);
+int fl_head_loss_grad(const fl_head_shape* shape, const uint16_t* hidden, const uint16_t* weight,
+                      const int64_t* labels, const float* lse, const float* target,
+                      const float* dloss, uint16_t* dhidden, uint16_t* dweight, void* workspace,
+                      size_t workspace_bytes, void* stream);
+int fl_head_distill(const fl_head_shape* shape, const uint16_t* hidden, const uint16_t* weight,
+                    int k, const int32_t* ids, const float* teacher, const float* teacher_lse,
+                    float tau, float* loss, float* lse, float* target, void* workspace,
+                    size_t workspace_bytes, void* stream);
+int fl_head_distill_grad(const fl_head_shape* shape, const uint16_t* hidden,
+                         const uint16_t* weight, int k, const int32_t* ids, const float* teacher,
+                         const float* teacher_lse, float tau, const float* lse,
+                         const float* target, const float* dloss, uint16_t* dhidden,
+                         uint16_t* dweight, void* workspace, size_t workspace_bytes,
+                         void* stream);
+size_t fl_top_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int k);
+int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const void* logits, int k,
+                  float tau, float* values, int32_t* ids, float* lse, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Launch-shape control, for tuning sweeps and for tests that check that

@@ -16,7 +16,10 @@ ROOT = os.path.dirname(HERE)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 LIB = os.path.join(HERE, "libflround.so")
 SOURCES = [os.path.join(HERE, "csrc", "flround_api.cpp"),
-           os.path.join(HERE, "csrc", "flround_kernels.hip")]
+           os.path.join(HERE, "csrc", "flround_kernels.hip"),
+           os.path.join(HERE, "csrc", "flround_head_api.cpp"),
+           os.path.join(HERE, "csrc", "flround_head.hip"),
+           os.path.join(HERE, "csrc", "flround_top.hip")]
 
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,699 @@
+// flround_head.hip -- gfx950 kernels of the output head: the cross entropy over
+// the vocabulary, the distillation from a teacher's top logits, and their
+// gradients.
+//
+// With z = h W^T (T tokens, V words, D wide), lse_t = log sum_v exp(z_tv / tau)
+// and a target distribution p of mass M listed by a few words per token:
+//     forward:   lse, and z at the listed words
+//     gradient:  G_tv = dloss_t tau (M_t exp(z_tv / tau - lse_t) - p_tv),
+//                dh = G W,  dW = G^T h
+// z is never stored: the forward pass keeps a running maximum and sum per row,
+// the gradient makes z again for a piece of the vocabulary and stores G of that
+// piece in bf16.  Everything large is a matrix product on the matrix cores, so
+// the file is one tiled product with four epilogues and the small kernels
+// around it.
+//
+// Tokens that take no part are dropped first: the rest are copied to
+// consecutive rows, so that no product spends time on them, and nothing that
+// stands in their rows (infinities, NaN) reaches a sum.
+#include "flr_head.h"
+
+namespace flr {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+#define LDS_SPACE __attribute__((address_space(3)))
+#define GLOBAL_SPACE __attribute__((address_space(1)))
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float bf16_f(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+__device__ __forceinline__ uint16_t to_bf16(float x) { return (uint16_t)pack2(x, 0.f); }
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
+
+// ---- the tiled product ------------------------------------------------------
+//
+// A workgroup makes BP x BQ outputs, kStep of the summed axis at a time, from
+// two stages of LDS: while the waves multiply one, the other is filled by loads
+// that go from memory to LDS directly.  An operand comes in either order:
+//
+//   rows along the summed axis (TR = false): the stage holds B rows of 64
+//   elements (128 B).  A fragment is one 16-byte read per lane (row l % 16,
+//   elements 8 (l / 16) .. + 7).  The 16-byte chunk c of row r lies at place
+//   c ^ (r & 7), so that the rows' equal chunks fall on different banks.
+//
+//   rows across it (TR = true): the stage holds 64 rows of B elements.  A
+//   fragment is two transposing reads of 8 bytes: 16 lanes read 4 rows of 16
+//   elements, and lane i gets column i.  The 32-byte pair of chunks c of row k
+//   lies at place c ^ ((k & 3) | (k >> 3 & 3) << 2): the 16 rows that a wave
+//   reads at a time fall on different banks.
+//
+// The loads write LDS in lane order, so the places are permuted by permuting
+// which global chunk a lane asks for.
+
+template <int B, int NT, bool TR>
+struct Operand {
+  static constexpr int kLoads = (B * 8 + NT - 1) / NT;   // 16-byte loads per thread and step
+  static constexpr int kChunks = TR ? B / 8 : 8;   // 16-byte chunks per LDS row
+  static constexpr int kPairs = B / 16;
+  static_assert(B * 8 % NT == 0 || B * 8 < NT, "whole loads, or the first waves' alone");
+
+  const char* base;       // of the tile
+  uint32_t at[kLoads];    // byte offset of each load
+  int64_t step;           // bytes per step
+
+  __device__ __forceinline__ static int row(int tid, int c) { return (tid + c * NT) / kChunks; }
+  __device__ __forceinline__ static int chunk(int tid, int c) {
+    const int place = (tid + c * NT) % kChunks, r = row(tid, c);
+    if (!TR) return place ^ (r & 7);
+    const int x = ((r & 3) | ((r >> 3) & 3) << 2) & (kPairs - 1);
+    return place ^ (x << 1);
+  }
+
+  // src: row 0 of the tile (TR = false: row b0, column 0; TR = true: row 0,
+  // column b0); n: rows (TR = false) or columns (TR = true) from there on.
+  // Those beyond n are replaced by ones that exist, their products are not
+  // used.
+  __device__ __forceinline__ void init(const uint16_t* src, int64_t ld, int64_t n, int tid) {
+    base = reinterpret_cast<const char*>(src);
+    step = TR ? (int64_t)kStep * ld * 2 : (int64_t)kStep * 2;
+#pragma unroll
+    for (int c = 0; c < kLoads; ++c) {
+      const int r = row(tid, c), ch = chunk(tid, c);
+      if (TR)
+        at[c] = (uint32_t)((r * ld + (ch * 8 < n ? ch * 8 : 0)) * 2);
+      else
+        at[c] = (uint32_t)(((r < n ? r : (int)n - 1) * ld + ch * 8) * 2);
+    }
+  }
+
+  __device__ __forceinline__ void load(uint16_t* lds, int64_t s, int wave) const {
+    const char* b = base + s * step;
+#pragma unroll
+    for (int c = 0; c < kLoads; ++c)
+      if (c * NT + wave * 64 < B * 8)
+        __builtin_amdgcn_global_load_lds((const GLOBAL_SPACE void*)(b + at[c]),
+                                         (LDS_SPACE void*)(lds + (c * NT + wave * 64) * 8), 16, 0, 0);
+  }
+
+  // The last step when the summed axis ends inside it: `left` elements of it
+  // remain (in whole chunks where TR = false), the others are zero.
+  __device__ __forceinline__ void load_tail(uint16_t* lds, int64_t s, int wave, int tid, int left,
+                                            const uint16_t* zero) const {
+    const char* b = base + s * step;
+#pragma unroll
+    for (int c = 0; c < kLoads; ++c) {
+      if (c * NT + wave * 64 >= B * 8) continue;
+      const bool in = TR ? row(tid, c) < left : chunk(tid, c) * 8 < left;
+      const char* p = in ? b + at[c] : reinterpret_cast<const char*>(zero);
+      __builtin_amdgcn_global_load_lds((const GLOBAL_SPACE void*)p,
+                                       (LDS_SPACE void*)(lds + (c * NT + wave * 64) * 8), 16, 0, 0);
+    }
+  }
+
+  // Fragment at rows (columns) b0 + 16 i of the tile, half ks of the step.
+  __device__ __forceinline__ static bf16x8 frag(const uint16_t* lds, int b0, int i, int ks, int l) {
+    if (!TR) {
+      const int ch = (ks * 4 + (l >> 4)) ^ (l & 7);
+      return *reinterpret_cast<const bf16x8*>(lds + (b0 + i * 16 + (l & 15)) * kStep + ch * 8);
+    }
+    const int x = (((l & 15) >> 2) | (l >> 4) << 2) & (kPairs - 1);
+    const int k = ks * 32 + 8 * (l >> 4) + ((l & 15) >> 2);
+    const uint16_t* p = lds + k * B + ((b0 / 16 + i) ^ x) * 16 + (l & 3) * 4;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_SPACE s16x4*)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_SPACE s16x4*)(p + 4 * B));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+enum Epilogue { kStats, kGrad, kSlab, kOut };
+
+// Tiles are dealt so that the 32 workgroups which an XCD runs at a time share
+// rows: workgroups go to the XCDs in turn, each XCD takes a contiguous range of
+// an order that runs over q within bands of kBand p tiles.
+constexpr int kBand = 4;
+constexpr int kXcds = 8;
+
+template <int WP, int WQ, int FP, int FQ, bool PTR, bool QTR, int EPI>
+__global__ __launch_bounds__(WP* WQ * 64) void k_tile(const TileArgs a) {
+  constexpr int NT = WP * WQ * 64, BP = WP * FP * 16, BQ = WQ * FQ * 16;
+  using OpP = Operand<BP, NT, PTR>;
+  using OpQ = Operand<BQ, NT, QTR>;
+  __shared__ __attribute__((aligned(1024))) uint16_t sm[2][(BP + BQ) * kStep];
+
+  const int tid = threadIdx.x, l = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wp = w % WP, wq = w / WP;
+  const int n_live = a.hdr->n_live;
+  const int64_t nq = a.live_q ? n_live : a.nq;
+  const int64_t nk = a.live_k ? n_live : a.nk;
+  const int tiles_p = (int)((a.np + BP - 1) / BP), tiles_q = (int)((nq + BQ - 1) / BQ);
+  const int tiles = tiles_p * tiles_q;
+  const int splits = EPI == kSlab ? a.splits : 1;
+  if ((int64_t)blockIdx.x >= (int64_t)tiles * splits) return;
+  const int split = EPI == kSlab ? (int)(blockIdx.x / tiles) : 0;
+  int tp, tq;
+  {
+    int id = (int)(blockIdx.x - split * tiles);
+    const int x = id % kXcds, per = tiles / kXcds, rem = tiles % kXcds;
+    id = x * per + (x < rem ? x : rem) + id / kXcds;
+    const int band = id / (kBand * tiles_q), in = id % (kBand * tiles_q);
+    const int width = tiles_p - band * kBand < kBand ? tiles_p - band * kBand : kBand;
+    tp = band * kBand + in % width;
+    tq = in / width;
+  }
+  const int64_t p0 = (int64_t)tp * BP, q0 = (int64_t)tq * BQ;
+  // the steps of this split
+  const int64_t steps_all = (nk + kStep - 1) / kStep;
+  const int64_t s0 = steps_all * split / splits, s1 = steps_all * (split + 1) / splits;
+  // an operand's rows of zeros make the last step whole, except the weight's
+  const int left = (int)(nk - (steps_all - 1) * kStep);
+  const bool ragged = EPI != kOut && left < kStep;
+
+  OpP op;
+  OpQ oq;
+  op.init(PTR ? a.P + p0 : a.P + p0 * a.ldp, a.ldp, a.np - p0, tid);
+  // the rows of q are padded to whole tiles
+  oq.init(QTR ? a.Q + q0 : a.Q + q0 * a.ldq, a.ldq, BQ, tid);
+  auto load = [&](int st, int64_t s) {
+    if (ragged && s == steps_all - 1)
+      op.load_tail(sm[st], s, w, tid, left, a.zero);
+    else
+      op.load(sm[st], s, w);
+    oq.load(sm[st] + BP * kStep, s, w);
+  };
+
+  f32x4 acc[FP][FQ];
+#pragma unroll
+  for (int i = 0; i < FP; ++i)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  if (s0 < s1) {
+    load(0, s0);
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (int64_t s = s0; s < s1; ++s) {
+    const int st = (int)((s - s0) & 1);
+    if (s + 1 < s1) load(st ^ 1, s + 1);
+    const uint16_t* lp = sm[st];
+    const uint16_t* lq = sm[st] + BP * kStep;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8 fp[FP], fq[FQ];
+#pragma unroll
+      for (int i = 0; i < FP; ++i) fp[i] = OpP::frag(lp, wp * FP * 16, i, ks, l);
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) fq[j] = OpQ::frag(lq, wq * FQ * 16, j, ks, l);
+#pragma unroll
+      for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+    }
+    __syncthreads();
+  }
+
+  // lane l holds, of the 16 x 16 outputs (i, j), q = l % 16 and
+  // p = 4 (l / 16) .. + 3
+  const int64_t pw = p0 + wp * FP * 16 + (l >> 4) * 4;
+  const int64_t qw = q0 + wq * FQ * 16 + (l & 15);
+
+  if constexpr (EPI == kStats) {
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = pw + i * 16 + e < a.np ? acc[i][j][e] * a.s2 : -INFINITY;
+          acc[i][j][e] = y;
+          m = fmaxf(m, y);
+        }
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      // a row of which nothing is there, or only -inf, sums to 0
+      const float ref = m == -INFINITY ? 0.f : m;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += exp2_(acc[i][j][e] - ref);
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (l < 16) a.parts[(int64_t)(tp * WP + wp) * a.parts_ld + qw + j * 16] = make_float2(m, sum);
+    }
+  } else if constexpr (EPI == kGrad) {
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int64_t q = qw + j * 16;
+      const bool live = q < n_live;
+      const float lse2 = live ? a.row_lse2[q] : 0.f, coef = live ? a.row_coef[q] : 0.f;
+      uint16_t* g = a.G + q * a.ldg;
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+        const int64_t p = pw + i * 16;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = live && p + e < a.np ? coef * exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -lse2)) : 0.f;
+        if (p < a.ldg) *reinterpret_cast<u32x2*>(g + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+      }
+    }
+  } else if constexpr (EPI == kSlab) {
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int64_t q = qw + j * 16;
+      if (q >= nq) continue;
+      float* o = a.slab + split * a.slab_stride + q * a.ld_slab;
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+        const int64_t p = pw + i * 16;
+        if (p < a.ld_slab) {
+          f32x4* d = reinterpret_cast<f32x4*>(o + p);
+          *d = a.add ? *d + acc[i][j] : acc[i][j];
+        }
+      }
+    }
+  } else {
+    const float f = a.hdr->scale * a.out_scale;
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int64_t q = qw + j * 16;
+      if (q >= nq) continue;
+      uint16_t* o = a.out + q * a.ld_out;
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+        const int64_t p = pw + i * 16;
+        const f32x4 v = acc[i][j] * f;
+        if (a.vec_out) {
+          if (p < a.np) *reinterpret_cast<u32x2*>(o + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (p + e < a.np) o[p + e] = to_bf16(v[e]);
+        }
+      }
+    }
+  }
+}
+
+template <bool PTR, bool QTR, int EPI>
+hipError_t launch_tile(const TileArgs& a, int64_t nq, int shape, hipStream_t st) {
+  const int64_t tp = (a.np + tile_p(shape) - 1) / tile_p(shape);
+  const int64_t tq = (nq + tile_q(shape) - 1) / tile_q(shape);
+  const int64_t grid = tp * tq * (EPI == kSlab ? a.splits : 1);
+  if (grid <= 0) return hipSuccess;
+  if (grid > (int64_t)1 << 22) return hipErrorInvalidValue;   // x 512 threads: within 2^32
+  const dim3 g((unsigned)grid);
+  switch (shape) {
+    case kTile256: k_tile<2, 4, 8, 4, PTR, QTR, EPI><<<g, 512, 0, st>>>(a); break;
+    case kTile128: k_tile<2, 2, 4, 4, PTR, QTR, EPI><<<g, 256, 0, st>>>(a); break;
+    case kTile64:
+      if constexpr (EPI != kOut) k_tile<4, 1, 2, 4, PTR, QTR, EPI><<<g, 256, 0, st>>>(a);
+      else return hipErrorInvalidValue;
+      break;
+    default:
+      if constexpr (EPI == kStats) k_tile<4, 1, 2, 1, PTR, QTR, EPI><<<g, 256, 0, st>>>(a);
+      else return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+// ---- small kernels ------------------------------------------------------------
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+
+// The teacher's log probabilities of the listed words, one wave per token.  An
+// entry with a negative id, or of a teacher logit of -inf, has probability 0; a
+// token without any other takes no part.
+__global__ __launch_bounds__(256) void k_teacher(const HeadArgs a) {
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int l = threadIdx.x & 63;
+  if (t >= a.T) return;
+  float x[2];
+  bool bad = false;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int k = l + 64 * h;
+    x[h] = -INFINITY;
+    if (k < a.K) {
+      const int32_t id = a.ids[t * a.K + k];
+      if (id >= 0) x[h] = a.teacher[t * a.K + k] / a.tau;
+      bad |= id >= a.V;
+    }
+  }
+  bad = __any(bad);
+  float ref;
+  if (a.teacher_lse) {
+    ref = a.teacher_lse[t];
+  } else {
+    const float m = wave_max(fmaxf(x[0], x[1]));
+    const float s = wave_sum(m == -INFINITY ? 0.f : expf(x[0] - m) + expf(x[1] - m));
+    ref = m + logf(s);   // NaN where an entry is NaN; -inf where nothing is listed
+  }
+  const bool any = __any(!(x[0] == -INFINITY) || !(x[1] == -INFINITY)) && ref != -INFINITY;
+  float mass = 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float lp = x[h] == -INFINITY ? -INFINITY : x[h] - ref;
+    mass += expf(lp);
+    const int k = l + 64 * h;
+    if (k < a.K) a.logp[t * a.K + k] = lp;
+  }
+  mass = wave_sum(mass);
+  if (l == 0) {
+    a.mass[t] = bad ? NAN : mass;
+    a.flag[t] = any || bad;
+  }
+}
+
+// Which tokens take part, in order, and (gradient) the largest finite |dloss|
+// among them.  One workgroup.
+__global__ __launch_bounds__(1024) void k_live(const HeadArgs a) {
+  __shared__ int counts[2][16];
+  __shared__ float tops[16];
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
+  int base = 0, par = 0;
+  float top = 0.f;
+  for (int64_t t0 = 0; t0 < a.T; t0 += 1024, par ^= 1) {
+    const int64_t t = t0 + tid;
+    bool on = false;
+    if (t < a.T) on = a.labels ? a.labels[t] >= 0 : a.flag[t] != 0;
+    const uint64_t mask = __ballot(on);
+    if (l == 0) counts[par][w] = __popcll(mask);
+    __syncthreads();
+    int before = base, all = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int c = counts[par][i];
+      before += i < w ? c : 0;
+      all += c;
+    }
+    base += all;
+    const int q = before + __popcll(mask & (((uint64_t)1 << l) - 1));
+    if (t < a.T) a.pos[t] = on ? q : -1;
+    if (on) {
+      a.rows[q] = (int32_t)t;
+      if (a.dloss) {
+        const float d = fabsf(a.dloss[t]);
+        if (d < INFINITY) top = fmaxf(top, d);
+      }
+    }
+  }
+  top = wave_max(top);
+  if (l == 0) tops[w] = top;
+  __syncthreads();
+  if (tid == 0) {
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i]);
+    a.hdr->n_live = base;
+    a.hdr->scale = top > 0.f ? top : 1.f;
+    for (int i = 0; i < 4; ++i) a.hdr->zero[i] = 0;
+  }
+}
+
+__device__ __forceinline__ bool aligned_rows(const uint16_t* p, int64_t ld, int64_t D) {
+  return ((reinterpret_cast<uintptr_t>(p) & 15) | (ld & 7) | (D & 7)) == 0;
+}
+
+// Copies the live tokens' rows to consecutive ones, padded with zeros to Dp
+// and, past the last, to whole tiles of rows.  Forward: also the products with
+// the listed words' rows of the weight (a wave per listed word), and zeros as
+// the results of the other tokens.  Gradient: also the coefficients of the
+// rows, and zeros as the other tokens' gradient.
+template <bool GRAD>
+__global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
+  int64_t t = blockIdx.x;
+  const u32x4 zero = {0, 0, 0, 0};
+  if (t >= a.T) {
+    const int n = a.hdr->n_live;
+    const int64_t q = n + (t - a.T);
+    if (q >= (n + kRowPad - 1) / kRowPad * kRowPad) return;
+    for (int64_t d = tid * 8; d < a.Dp; d += 2048) *reinterpret_cast<u32x4*>(a.hc + q * a.Dp + d) = zero;
+    return;
+  }
+  const int64_t q = a.pos[t];
+  if (q < 0) {
+    if (GRAD) {
+      for (int64_t d = tid; d < a.D; d += 256) a.dhidden[t * a.D + d] = 0;
+    } else {
+      if (tid == 0) a.loss[t] = a.lse[t] = 0.f;
+      if (tid < a.K) a.target[t * a.K + tid] = 0.f;
+    }
+    return;
+  }
+  const uint16_t* h = a.hidden + t * a.ldh;
+  uint16_t* hc = a.hc + q * a.Dp;
+  const bool vec = aligned_rows(a.hidden, a.ldh, a.D);
+  if (vec) {
+    for (int64_t d = tid * 8; d < a.Dp; d += 2048)
+      *reinterpret_cast<u32x4*>(hc + d) = d < a.D ? *reinterpret_cast<const u32x4*>(h + d) : zero;
+  } else {
+    for (int64_t d = tid; d < a.Dp; d += 256) hc[d] = d < a.D ? h[d] : 0;
+  }
+  if (GRAD) {
+    if (tid == 0) {
+      const float mass = a.labels ? (a.labels[t] < a.V ? 1.f : NAN) : a.mass[t];
+      a.row_lse2[q] = a.lse_in[t] * kLog2e;
+      a.row_coef[q] = a.dloss[t] / a.hdr->scale * mass;
+    }
+    return;
+  }
+  const bool wvec = vec && aligned_rows(a.weight, a.ldw, a.D);
+  for (int k = w; k < a.K; k += 4) {
+    const int64_t id = a.labels ? a.labels[t] : a.ids[t * a.K + k];
+    float s = 0.f;
+    if (id >= a.V) {
+      s = NAN;
+    } else if (id >= 0) {
+      const uint16_t* r = a.weight + id * a.ldw;
+      if (wvec) {
+        for (int64_t d = l * 8; d < a.D; d += 512) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(h + d);
+          const u32x4 y = *reinterpret_cast<const u32x4*>(r + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s = __builtin_fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
+            s = __builtin_fmaf(__uint_as_float(x[e] & 0xFFFF0000u),
+                               __uint_as_float(y[e] & 0xFFFF0000u), s);
+          }
+        }
+      } else {
+        for (int64_t d = l; d < a.D; d += 64) s = __builtin_fmaf(bf16_f(h[d]), bf16_f(r[d]), s);
+      }
+      s = wave_sum(s);
+    }
+    if (l == 0) a.target[t * a.K + k] = s;
+  }
+}
+
+// Weight rows whose length or place the 16-byte loads cannot take, copied to
+// rows of Dp.
+__global__ __launch_bounds__(256) void k_pack_weight(const HeadArgs a) {
+  const int64_t n = a.V * a.Dp;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n;
+       i += (int64_t)gridDim.x * 2048) {
+    const int64_t v = i / a.Dp, d = i % a.Dp;
+    const uint16_t* r = a.weight + v * a.ldw;
+    u32x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t lo = d + 2 * e < a.D ? r[d + 2 * e] : 0;
+      const uint32_t hi = d + 2 * e + 1 < a.D ? r[d + 2 * e + 1] : 0;
+      o[e] = lo | hi << 16;
+    }
+    *reinterpret_cast<u32x4*>(a.wc + i) = o;
+  }
+}
+
+// lse and loss of 16 live rows: 64 threads fold a row's parts, then a wave
+// sums over its listed words.
+__global__ __launch_bounds__(1024) void k_finish(const HeadArgs a) {
+  __shared__ float ms[16][17], ss[16][17];
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
+  const int n = a.hdr->n_live;
+  const int64_t q0 = (int64_t)blockIdx.x * 16;
+  if (q0 >= n) return;
+  const int c = tid & 15;
+  float m = -INFINITY, s = 0.f;
+  // (m, s) stands for s 2^m; a part of nothing is (-inf, 0)
+  auto join = [](float& m, float& s, float pm, float ps) {
+    const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
+    s = s * exp2_(m - ref) + ps * exp2_(pm - ref);
+    m = top;
+  };
+  if (q0 + c < n)
+    for (int i = tid >> 4; i < a.n_parts; i += 64) {
+      const float2 p = a.parts[(int64_t)i * a.rows_pad + q0 + c];
+      join(m, s, p.x, p.y);
+    }
+  join(m, s, __shfl_xor(m, 16), __shfl_xor(s, 16));
+  join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32));
+  if (l < 16) ms[w][l] = m, ss[w][l] = s;
+  __syncthreads();
+  if (q0 + w >= n) return;
+  m = l < 16 ? ms[l][w] : -INFINITY;
+  s = l < 16 ? ss[l][w] : 0.f;
+#pragma unroll
+  for (int d = 8; d; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  m = __shfl(m, 0);
+  s = __shfl(s, 0);
+  const float lse = (m + log2_(s)) * kLn2;
+  const int64_t t = a.rows[q0 + w];
+  if (a.labels) {
+    if (l == 0) {
+      a.lse[t] = lse;
+      a.loss[t] = lse - a.target[t];
+    }
+    return;
+  }
+  float sum = 0.f;
+  for (int k = l; k < a.K; k += 64) {
+    const float lp = a.logp[t * a.K + k];
+    if (lp != -INFINITY) sum += expf(lp) * (lp - a.target[t * a.K + k] / a.tau + lse);
+  }
+  sum = wave_sum(sum);
+  if (l == 0) {
+    a.lse[t] = lse;
+    a.loss[t] = a.tau * a.tau * sum;
+  }
+}
+
+// G at the listed words [v0, v1), a wave per live row: the tile's epilogue left
+// the softmax's share there in bf16; this replaces it by the whole difference,
+// rounded once.  A word that a token lists more than once gets the sum of its
+// probabilities.
+__global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int64_t ldg, int64_t v0,
+                                             int64_t v1) {
+  const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int l = threadIdx.x & 63;
+  if (q >= a.hdr->n_live) return;
+  const int64_t t = a.rows[q];
+  const float ratio = a.dloss[t] / a.hdr->scale;
+  if (a.labels) {
+    const int64_t y = a.labels[t];
+    if (l == 0 && y >= v0 && y < v1)
+      G[q * ldg + (y - v0)] = to_bf16(ratio * (exp2_((a.target_in[t] - a.lse_in[t]) * kLog2e) - 1.f));
+    return;
+  }
+  const float mass = a.mass[t], lse = a.lse_in[t];
+  for (int k0 = 0; k0 < a.K; k0 += 64) {
+    const int k = k0 + l;
+    const int32_t id = k < a.K ? a.ids[t * a.K + k] : -1;
+    float p = 0.f;
+    for (int j0 = 0; j0 < a.K; j0 += 64) {
+      const int j = j0 + l;
+      const int32_t jd = j < a.K ? a.ids[t * a.K + j] : -1;
+      const float jp = j < a.K ? expf(a.logp[t * a.K + j]) : 0.f;
+      const int n = a.K - j0 < 64 ? a.K - j0 : 64;
+      for (int i = 0; i < n; ++i) {
+        const int32_t other = __shfl(jd, i);
+        const float op = __shfl(jp, i);
+        if (other == id) p += op;
+      }
+    }
+    if (id >= v0 && id < v1) {
+      const float z = a.target_in[t * a.K + k];
+      G[q * ldg + (id - v0)] = to_bf16(ratio * (mass * exp2_((z / a.tau - lse) * kLog2e) - p));
+    }
+  }
+}
+
+// The gradient of the hidden state from the splits' fp32 sums, added in order.
+__global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab, int64_t ld_slab,
+                                            int64_t slab_stride, int splits, float out_scale) {
+  const unsigned blocks = (unsigned)((a.D + 1023) / 1024);
+  const int64_t q = blockIdx.x / blocks;
+  if (q >= a.hdr->n_live) return;
+  const int64_t d = ((int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x) * 4;
+  if (d >= a.D) return;
+  const float f = a.hdr->scale * out_scale;
+  const float* p = slab + q * ld_slab + d;
+  f32x4 s = *reinterpret_cast<const f32x4*>(p);
+  for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4*>(p + i * slab_stride);
+  s *= f;
+  uint16_t* o = a.dhidden + (int64_t)a.rows[q] * a.D + d;
+  if (((a.D & 3) | (reinterpret_cast<uintptr_t>(a.dhidden) & 7)) == 0) {
+    *reinterpret_cast<u32x2*>(o) = u32x2{pack2(s[0], s[1]), pack2(s[2], s[3])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d + e < a.D) o[e] = to_bf16(s[e]);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st) {
+  k_teacher<<<(unsigned)((a.T + 3) / 4), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_head_live(const HeadArgs& a, hipStream_t st) {
+  k_live<<<1, 1024, 0, st>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_head_pack(const HeadArgs& a, bool grad, hipStream_t st) {
+  const unsigned grid = (unsigned)(a.T + kRowPad);
+  if (grad) k_pack<true><<<grid, 256, 0, st>>>(a);
+  else k_pack<false><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_head_pack_weight(const HeadArgs& a, hipStream_t st) {
+  const int64_t blocks = (a.V * a.Dp / 8 + 255) / 256;
+  k_pack_weight<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_head_finish(const HeadArgs& a, hipStream_t st) {
+  k_finish<<<(unsigned)((a.T + 15) / 16), 1024, 0, st>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_head_fix(const HeadArgs& a, uint16_t* G, int64_t ldg, int64_t v0, int64_t v1,
+                           hipStream_t st) {
+  k_fix<<<(unsigned)((a.T + 3) / 4), 256, 0, st>>>(a, G, ldg, v0, v1);
+  return hipGetLastError();
+}
+hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab,
+                          int64_t slab_stride, int splits, float out_scale, hipStream_t st) {
+  const unsigned blocks = (unsigned)((a.D + 1023) / 1024);
+  k_dh<<<blocks * (unsigned)a.T, 256, 0, st>>>(a, slab, ld_slab, slab_stride, splits, out_scale);
+  return hipGetLastError();
+}
+hipError_t launch_logits_stats(const TileArgs& a, int shape, hipStream_t st) {
+  return launch_tile<false, false, kStats>(a, a.nq, shape, st);
+}
+hipError_t launch_logits_grad(const TileArgs& a, int shape, hipStream_t st) {
+  return launch_tile<false, false, kGrad>(a, a.nq, shape, st);
+}
+hipError_t launch_dhidden(const TileArgs& a, int shape, hipStream_t st) {
+  return launch_tile<true, false, kSlab>(a, a.nq, shape, st);
+}
+hipError_t launch_dweight(const TileArgs& a, int shape, hipStream_t st) {
+  return launch_tile<true, true, kOut>(a, a.nq, shape, st);
+}
+
+}  // namespace flr

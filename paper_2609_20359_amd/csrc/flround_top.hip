@@ -1,0 +1,296 @@
+// flround_top.hip -- gfx950 kernels of the top logits: the k largest of each
+// row with their ids, and the logarithm of the sum of exp(x / tau).
+//
+// One pass over the logits, bound by HBM.  A workgroup of 512 threads takes a
+// segment of a row into registers, so that nothing is read twice:
+//   * the maxima of its 512 threads give a lower bound on the k-th largest (k
+//     threads' maxima are at least their k-th largest), found by bisecting the
+//     leading 16 bits;
+//   * what is not below the bound, a few more than k as a rule, goes to a list
+//     in LDS; where it would not fit (a row of equal values), the exact k-th
+//     largest is found by bisecting (value, id) over the registers;
+//   * a list entry's place is the number of entries above it.
+// Rows longer than a segment are joined by a second kernel, in which an entry's
+// place is the sum of its places in the segments' sorted lists.
+//
+// The order is that of one 64-bit number: the value, then the lower id; so ties
+// go to the lowest id and no result depends on the order of the list.
+#include "flr_head.h"
+
+namespace flr {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kThreads = kTopThreads;
+constexpr int kWaves = kThreads / 64;
+constexpr int kList = 2048;   // entries of the list in LDS
+
+// Larger floats have larger keys, NaN the largest, and -0 that of +0.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const int32_t b = (int32_t)__float_as_uint(x + 0.f);
+  return x != x ? 0xFFFFFFFFu : (uint32_t)(b ^ ((b >> 31) & 0x7FFFFFFF)) ^ 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+  const int32_t b = (int32_t)(k ^ 0x80000000u);
+  return k == 0xFFFFFFFFu ? NAN : __uint_as_float((uint32_t)(b ^ ((b >> 31) & 0x7FFFFFFF)));
+}
+__device__ __forceinline__ uint64_t entry(float x, int64_t id) {
+  return (uint64_t)key_of(x) << 32 | (0xFFFFFFFFu - (uint32_t)id);
+}
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
+
+// (m, s) stands for s exp(m / tau); nothing is (-inf, 0).  Differences are taken
+// before they are scaled: a row masked by the type's lowest value would
+// overflow the other way round.
+__device__ __forceinline__ void join(float& m, float& s, float pm, float ps, float s2) {
+  const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
+  s = s * exp2_((m - ref) * s2) + ps * exp2_((pm - ref) * s2);
+  m = top;
+}
+__device__ __forceinline__ float lse_of(float m, float s, const TopArgs& a) {
+  return m / a.tau + log2_(s) * kLn2;
+}
+
+__device__ __forceinline__ void emit(const TopArgs& a, int64_t row, int place, uint64_t e) {
+  a.values[row * a.k + place] = value_of((uint32_t)(e >> 32));
+  a.ids[row * a.k + place] = (int32_t)(0xFFFFFFFFu - (uint32_t)e);
+}
+
+// NC: 16-byte chunks per thread.
+template <bool BF16, int NC>
+__global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
+  constexpr int E = BF16 ? 8 : 4;        // elements of a chunk
+  constexpr int ES = BF16 ? 2 : 4;
+  __shared__ uint64_t list[kList];
+  __shared__ uint32_t maxima[kThreads];
+  __shared__ float wave_m[kWaves], wave_s[kWaves];
+  __shared__ int counts[2][kWaves];
+  __shared__ int n_list;
+  __shared__ float bound;
+
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
+  const int64_t row = blockIdx.x / a.segs;
+  const int seg = (int)(blockIdx.x % a.segs);
+  // chunks are counted from the 16-byte boundary at or before the row
+  const char* src = static_cast<const char*>(a.logits) + row * a.stride * ES;
+  const int head = (int)(reinterpret_cast<uintptr_t>(src) & 15) / ES;
+  const int64_t first = ((int64_t)seg * kThreads * NC + tid) * E - head;   // id of chunk 0's first
+
+  u32x4 d[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int64_t id = first + (int64_t)c * kThreads * E;
+    // what is not there reads as -inf and is told apart by its id
+    if (id >= 0 && id + E <= a.vocab) {
+      d[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + id * ES));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (BF16) {
+          uint32_t x[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int64_t j = id + 2 * i + h;
+            x[h] = j >= 0 && j < a.vocab ? *reinterpret_cast<const uint16_t*>(src + j * 2) : 0xFF80u;
+          }
+          d[c][i] = x[0] | x[1] << 16;
+        } else {
+          const int64_t j = id + i;
+          d[c][i] = j >= 0 && j < a.vocab ? *reinterpret_cast<const uint32_t*>(src + j * 4) : 0xFF800000u;
+        }
+      }
+    }
+  }
+  auto value = [&](int c, int e) -> float {
+    if (!BF16) return __uint_as_float(d[c][e]);
+    const uint32_t u = d[c][e >> 1];
+    return __uint_as_float(e & 1 ? u & 0xFFFF0000u : u << 16);
+  };
+
+  float top = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int e = 0; e < E; ++e) top = fmaxf(top, value(c, e));
+  maxima[tid] = key_of(top) >> 16;
+  if (tid == 0) n_list = 0;
+  float m = top;
+#pragma unroll
+  for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+  if (l == 0) wave_m[w] = m;
+  __syncthreads();
+
+  // wave 0: the bound; all waves: the sum
+  if (w == 0) {
+    uint32_t v[kWaves], t = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) v[i] = maxima[i * 64 + l];
+    for (int bit = 15; bit >= 0; --bit) {
+      const uint32_t x = t | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) n += __popcll(__ballot(v[i] >= x));
+      if (n >= a.k) t = x;
+    }
+    // the least value whose key starts with these bits; as a float it may be a
+    // NaN's pattern below -inf, where nothing is below the bound
+    const float b = value_of(t << 16);
+    if (l == 0) bound = t <= 0x007Fu ? -INFINITY : b;
+  }
+  m = wave_m[0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i) m = fmaxf(m, wave_m[i]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += exp2_((value(c, e) - ref) * a.s2);
+#pragma unroll
+  for (int x = 32; x; x >>= 1) s += __shfl_xor(s, x);
+  if (l == 0) wave_s[w] = s;
+  __syncthreads();
+
+  // how many are not below the bound
+  const float b = bound;
+  const bool whole = first >= 0 && first + (int64_t)(NC - 1) * kThreads * E + E <= a.vocab;
+  auto there = [&](int c, int e) {
+    const int64_t id = first + (int64_t)c * kThreads * E + e;
+    return id >= 0 && id < a.vocab;
+  };
+  int n = 0;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int e = 0; e < E; ++e) n += !(value(c, e) < b);
+  if (!whole && n) {
+    n = 0;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < E; ++e) n += !(value(c, e) < b) && there(c, e);
+  }
+  auto total = [&](int mine, int par) {
+#pragma unroll
+    for (int x = 32; x; x >>= 1) mine += __shfl_xor(mine, x);
+    if (l == 0) counts[par][w] = mine;
+    __syncthreads();
+    int t = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) t += counts[par][i];
+    return t;
+  };
+  int all = total(n, 0);
+  uint64_t least = 0;
+  if (all > kList) {
+    // the k-th largest entry itself: the largest x that k entries reach
+    for (int bit = 63; bit >= 0; --bit) {
+      const uint64_t x = least | (uint64_t)1 << bit;
+      int r = 0;
+      if (n) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            r += there(c, e) && entry(value(c, e), first + (int64_t)c * kThreads * E + e) >= x;
+      }
+      if (total(r, (bit & 1)) >= a.k) least = x;
+    }
+    // counts[] is not read again before the next barrier
+    all = a.k;
+  }
+  if (n) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (!(value(c, e) < b) && there(c, e)) {
+          const uint64_t x = entry(value(c, e), first + (int64_t)c * kThreads * E + e);
+          if (x >= least) list[atomicAdd(&n_list, 1)] = x;
+        }
+  }
+  __syncthreads();
+  const bool last = a.segs == 1;
+  uint64_t* out = last ? nullptr : a.lists + (row * a.segs + seg) * a.k;
+  for (int i = tid; i < all; i += kThreads) {
+    const uint64_t x = list[i];
+    int place = 0;
+    for (int j = 0; j < all; ++j) place += list[j] > x;
+    if (place < a.k) {
+      if (last) emit(a, row, place, x);
+      else out[place] = x;
+    }
+  }
+  if (!last)
+    for (int i = all + tid; i < a.k; i += kThreads) out[i] = 0;   // fewer than k in the segment
+  if (tid == 0) {
+    s = 0.f;
+    for (int i = 0; i < kWaves; ++i) s += wave_s[i];
+    if (!last) a.parts[row * a.segs + seg] = make_float2(m, s);
+    else if (a.lse) a.lse[row] = lse_of(m, s, a);
+  }
+}
+
+// Joins a row's segments.
+__global__ __launch_bounds__(256) void k_top_join(const TopArgs a) {
+  extern __shared__ uint64_t lists[];
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const int n = a.segs * a.k;
+  for (int i = tid; i < n; i += 256) lists[i] = a.lists[row * n + i];
+  __syncthreads();
+  for (int i = tid; i < n; i += 256) {
+    const uint64_t x = lists[i];
+    if (x == 0) continue;
+    const int own = i / a.k;
+    int place = i - own * a.k;
+    for (int g = 0; g < a.segs && place < a.k; ++g) {
+      if (g == own) continue;
+      const uint64_t* p = lists + g * a.k;
+      int lo = 0, hi = a.k;   // how many of p are above x
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (p[mid] > x) lo = mid + 1;
+        else hi = mid;
+      }
+      place += lo;
+    }
+    if (place < a.k) emit(a, row, place, x);
+  }
+  if (a.lse && tid < 64) {
+    float m = -INFINITY, s = 0.f;
+    for (int g = tid; g < a.segs; g += 64) {
+      const float2 p = a.parts[row * a.segs + g];
+      join(m, s, p.x, p.y, a.s2);
+    }
+#pragma unroll
+    for (int x = 32; x; x >>= 1) join(m, s, __shfl_xor(m, x), __shfl_xor(s, x), a.s2);
+    if (tid == 0) a.lse[row] = lse_of(m, s, a);
+  }
+}
+
+template <bool BF16>
+void launch_segment(const TopArgs& a, unsigned grid, hipStream_t st) {
+  switch (a.chunks) {
+    case 1: k_top_segment<BF16, 1><<<grid, kThreads, 0, st>>>(a); break;
+    case 2: k_top_segment<BF16, 2><<<grid, kThreads, 0, st>>>(a); break;
+    case 4: k_top_segment<BF16, 4><<<grid, kThreads, 0, st>>>(a); break;
+    default: k_top_segment<BF16, 8><<<grid, kThreads, 0, st>>>(a); break;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_top(const TopArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)(a.rows * a.segs);
+  if (a.bf16) launch_segment<true>(a, grid, st);
+  else launch_segment<false>(a, grid, st);
+  if (const hipError_t e = hipGetLastError()) return e;
+  if (a.segs > 1) k_top_join<<<(unsigned)a.rows, 256, (size_t)a.segs * a.k * 8, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace flr

@@ -27,6 +27,8 @@ FL_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 FL_MAX_PEERS = 64
 FL_MAX_GROUPS = 64
+FL_MAX_TARGETS = 128
+FL_BF16, FL_F32 = 0, 1
 
 # Every symbol include/flround.h declares.
 EXPORTS = ("fl_status_string", "fl_version", "fl_layout_create", "fl_layout_destroy",
@@ -35,7 +37,9 @@ EXPORTS = ("fl_status_string", "fl_version", "fl_layout_create", "fl_layout_dest
            "fl_fedavg", "fl_round", "fl_set_blocks_per_cu", "fl_shard_reduce_wire",
            "fl_broadcast_recv", "fl_round_hsdp", "fl_fedopt", "fl_round_outer",
            "fl_lr_cosine", "fl_grad_sumsq", "fl_local_step_clipped", "fl_round_noalloc",
-           "fl_noalloc_workspace_bytes")
+           "fl_noalloc_workspace_bytes", "fl_head_workspace_bytes", "fl_head_loss",
+           "fl_head_loss_grad", "fl_head_distill", "fl_head_distill_grad",
+           "fl_top_workspace_bytes", "fl_top_logits")
 
 _P = ctypes.c_void_p
 
@@ -76,6 +80,11 @@ def outer_hparams(oh):
 class HsdpCfg(ctypes.Structure):
     _fields_ = [("H", ctypes.c_int), ("replica", ctypes.c_int), ("hsdp_scale", ctypes.c_float),
                 ("fedavg_member", ctypes.c_int)]
+
+
+class HeadShape(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("vocab", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -129,6 +138,21 @@ def lib():
         L.fl_lr_cosine.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_float,
                                    ctypes.c_float]
         L.fl_lr_cosine.restype = ctypes.c_float
+        shape = ctypes.POINTER(HeadShape)
+        L.fl_head_workspace_bytes.argtypes = [shape, ctypes.c_int, ctypes.c_int]
+        L.fl_head_workspace_bytes.restype = ctypes.c_size_t
+        L.fl_head_loss.argtypes = [shape] + [_P] * 7 + [ctypes.c_size_t, _P]
+        L.fl_head_loss_grad.argtypes = [shape] + [_P] * 9 + [ctypes.c_size_t, _P]
+        L.fl_head_distill.argtypes = ([shape, _P, _P, ctypes.c_int, _P, _P, _P, ctypes.c_float]
+                                      + [_P] * 4 + [ctypes.c_size_t, _P])
+        L.fl_head_distill_grad.argtypes = ([shape, _P, _P, ctypes.c_int, _P, _P, _P,
+                                            ctypes.c_float] + [_P] * 6 + [ctypes.c_size_t, _P])
+        L.fl_top_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int,
+                                             ctypes.c_int]
+        L.fl_top_workspace_bytes.restype = ctypes.c_size_t
+        L.fl_top_logits.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int,
+                                    _P, ctypes.c_int, ctypes.c_float, _P, _P, _P, _P,
+                                    ctypes.c_size_t, _P]
         L.fl_set_blocks_per_cu.argtypes = [ctypes.c_int]
         L.fl_set_blocks_per_cu.restype = ctypes.c_int
         _lib = L
@@ -491,6 +515,196 @@ def fl_round_outer(layout, cfg, outer, grads, replicas, prev, buf, master, m, v,
                               _buf(seg_sumsq, cfg.A * layout.n_seg, 4, "seg_sumsq"),
                               _stream(stream))
     _check(rc, "fl_round_outer")
+
+
+# ---- the output head --------------------------------------------------------
+
+
+def _array(t, shape, dtype, what):
+    """Device address of a contiguous CUDA tensor of this shape and dtype on
+    the current device."""
+    if not getattr(t, "is_cuda", False):
+        raise ValueError("%s must be a CUDA tensor" % what)
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s; got %s of shape %s"
+                         % (what, dtype, shape, t.dtype, tuple(t.shape)))
+    _on_current_device(t, what)
+    return t.data_ptr()
+
+
+def _on_current_device(t, what):
+    import torch
+
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s is on device %d; the current device is %d"
+                         % (what, t.get_device(), torch.cuda.current_device()))
+
+
+def _rows(t, dtypes, what):
+    """(address, elements between rows) of a 2-D CUDA tensor whose rows are
+    contiguous and do not overlap."""
+    if not getattr(t, "is_cuda", False):
+        raise ValueError("%s must be a CUDA tensor" % what)
+    if t.dim() != 2 or t.dtype not in dtypes:
+        raise ValueError("%s must be a 2-D tensor of %s" % (what, " or ".join(map(str, dtypes))))
+    n, d = t.shape
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have contiguous rows" % what)
+    stride = t.stride(0) if n > 1 else d
+    if stride < d:
+        raise ValueError("%s has overlapping rows" % what)
+    _on_current_device(t, what)
+    return t.data_ptr(), stride
+
+
+def _workspace(workspace, nbytes, stream):
+    """(address, bytes) of the workspace: the tensor given, or one from torch's
+    allocator, which reuses it in the order of the stream it was taken on."""
+    import torch
+
+    if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor")
+        _on_current_device(workspace, "workspace")
+        return workspace, workspace.numel() * workspace.element_size()
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
+
+
+def head_workspace_bytes(tokens, vocab, width, k=0, grad=False, weight_stride=0):
+    """Bytes of workspace that fl_head_loss (k = 0) or fl_head_distill and, with
+    grad, their gradients need."""
+    s = HeadShape(tokens, vocab, width, 0, weight_stride)
+    return int(lib().fl_head_workspace_bytes(ctypes.byref(s), k, 1 if grad else 0))
+
+
+def top_workspace_bytes(rows, vocab, k, dtype=FL_BF16):
+    """Bytes of workspace that fl_top_logits needs (0 for many sizes)."""
+    return int(lib().fl_top_workspace_bytes(rows, vocab, dtype, k))
+
+
+class _HeadCall:
+    """The arguments that the head's four functions share, checked."""
+
+    def __init__(self, hidden, weight, k, grad, workspace, stream):
+        import torch
+
+        self.h, ldh = _rows(hidden, (torch.bfloat16,), "hidden")
+        self.w, ldw = _rows(weight, (torch.bfloat16,), "weight")
+        self.T, self.D = hidden.shape
+        self.V = weight.shape[0]
+        if weight.shape[1] != self.D:
+            raise ValueError("hidden is %d wide, weight %d" % (self.D, weight.shape[1]))
+        self.shape = HeadShape(self.T, self.V, self.D, ldh, ldw)
+        need = lib().fl_head_workspace_bytes(ctypes.byref(self.shape), k, grad)
+        self.keep, self.ws_bytes = _workspace(workspace, need, stream)
+        self.ws = self.keep.data_ptr()
+        self.stream = _stream(stream)
+
+    def floats(self, t, what, *shape):
+        import torch
+
+        return _array(t, shape or (self.T,), torch.float32, what)
+
+    def teacher(self, ids, teacher, teacher_lse):
+        import torch
+
+        if ids.dim() != 2:
+            raise ValueError("ids must be a 2-D tensor")
+        self.k = ids.shape[1]
+        return (_array(ids, (self.T, self.k), torch.int32, "ids"),
+                self.floats(teacher, "teacher", self.T, self.k),
+                None if teacher_lse is None else self.floats(teacher_lse, "teacher_lse"))
+
+    def grads(self, dhidden, dweight):
+        import torch
+
+        return (_array(dhidden, (self.T, self.D), torch.bfloat16, "dhidden"),
+                _array(dweight, (self.V, self.D), torch.bfloat16, "dweight"))
+
+
+def fl_head_loss(hidden, weight, labels, loss, lse, target, workspace=None, stream=None):
+    """Cross entropy of hidden (T x D bf16) through weight (V x D bf16) at
+    labels (T int64, negative: the token takes no part).  Writes loss, lse and
+    target (T float32 each); lse and target go to fl_head_loss_grad."""
+    import torch
+
+    c = _HeadCall(hidden, weight, 0, 0, workspace, stream)
+    rc = lib().fl_head_loss(ctypes.byref(c.shape), c.h, c.w,
+                            _array(labels, (c.T,), torch.int64, "labels"), c.floats(loss, "loss"),
+                            c.floats(lse, "lse"), c.floats(target, "target"), c.ws, c.ws_bytes,
+                            c.stream)
+    _check(rc, "fl_head_loss")
+
+
+def fl_head_loss_grad(hidden, weight, labels, lse, target, dloss, dhidden, dweight,
+                      workspace=None, stream=None):
+    """Gradient of sum(dloss * loss): writes dhidden (T x D) and dweight
+    (V x D), bf16.  lse and target as fl_head_loss wrote them."""
+    import torch
+
+    c = _HeadCall(hidden, weight, 0, 1, workspace, stream)
+    dh, dw = c.grads(dhidden, dweight)
+    rc = lib().fl_head_loss_grad(ctypes.byref(c.shape), c.h, c.w,
+                                 _array(labels, (c.T,), torch.int64, "labels"),
+                                 c.floats(lse, "lse"), c.floats(target, "target"),
+                                 c.floats(dloss, "dloss"), dh, dw, c.ws, c.ws_bytes, c.stream)
+    _check(rc, "fl_head_loss_grad")
+
+
+def fl_head_distill(hidden, weight, ids, teacher, teacher_lse, tau, loss, lse, target,
+                    workspace=None, stream=None):
+    """Divergence of the student's distribution from the teacher's over the
+    listed words: ids (T x k int32, negative: absent) and teacher (T x k
+    float32) as fl_top_logits writes them, teacher_lse (T float32) or None to
+    normalise over the listed words.  Writes loss and lse (T float32) and
+    target (T x k float32)."""
+    c = _HeadCall(hidden, weight, ids.shape[-1], 0, workspace, stream)
+    i, a, al = c.teacher(ids, teacher, teacher_lse)
+    rc = lib().fl_head_distill(ctypes.byref(c.shape), c.h, c.w, c.k, i, a, al, float(tau),
+                               c.floats(loss, "loss"), c.floats(lse, "lse"),
+                               c.floats(target, "target", c.T, c.k), c.ws, c.ws_bytes, c.stream)
+    _check(rc, "fl_head_distill")
+
+
+def fl_head_distill_grad(hidden, weight, ids, teacher, teacher_lse, tau, lse, target, dloss,
+                         dhidden, dweight, workspace=None, stream=None):
+    """Gradient of sum(dloss * loss) of fl_head_distill: writes dhidden and
+    dweight, bf16."""
+    c = _HeadCall(hidden, weight, ids.shape[-1], 1, workspace, stream)
+    i, a, al = c.teacher(ids, teacher, teacher_lse)
+    dh, dw = c.grads(dhidden, dweight)
+    rc = lib().fl_head_distill_grad(ctypes.byref(c.shape), c.h, c.w, c.k, i, a, al, float(tau),
+                                    c.floats(lse, "lse"), c.floats(target, "target", c.T, c.k),
+                                    c.floats(dloss, "dloss"), dh, dw, c.ws, c.ws_bytes, c.stream)
+    _check(rc, "fl_head_distill_grad")
+
+
+def fl_top_logits(logits, k, tau, values, ids, lse=None, workspace=None, stream=None):
+    """The k largest of each row of logits (rows x vocab, bf16 or float32, rows
+    may be longer), largest first, ties to the lowest id: writes values
+    (rows x k float32), ids (rows x k int32) and lse (rows float32, or None),
+    the log of the sum of exp(logits / tau)."""
+    import torch
+
+    p, stride = _rows(logits, (torch.bfloat16, torch.float32), "logits")
+    n, v = logits.shape
+    dtype = FL_BF16 if logits.dtype == torch.bfloat16 else FL_F32
+    args = (_array(values, (n, k), torch.float32, "values"),
+            _array(ids, (n, k), torch.int32, "ids"),
+            None if lse is None else _array(lse, (n,), torch.float32, "lse"))
+    need = lib().fl_top_workspace_bytes(n, v, dtype, k)
+    ws, ws_bytes = None, 0
+    if need or workspace is not None:
+        keep, ws_bytes = _workspace(workspace, need, stream)
+        ws = keep.data_ptr()
+    rc = lib().fl_top_logits(n, v, stride, dtype, p, k, float(tau), *args, ws, ws_bytes,
+                             _stream(stream))
+    _check(rc, "fl_top_logits")
 
 
 # ---- HIP events (for fl_round's per-phase timing) -------------------------

@@ -1,0 +1,478 @@
+"""The output head on the GPU against its definition in 64 bits: cross entropy
+and its gradient, distillation from a teacher's top logits and its gradient,
+and the top logits.
+
+Tolerances follow from the arithmetic (u = 2^-24):
+  z:     a sum of D products in fp32 is within (D + 8) u sum |h||w| of the
+         exact one, whatever its order; B is the largest such sum of a row.
+  lse:   off by what z is off by (over tau), by the exponentials' error (the
+         argument's rounding, |y| u for |y| up to 64 in the base-2 exponent that
+         counts, and one ulp), and by the additions (at most 2^7 in a row): 2^-16
+         covers them; and by the result's own rounding, 4 u |lse|.
+  G:     each entry is rounded to bf16 once or twice (the coefficient dloss/scale is
+         exact or fp32): 2^-8 |G|, and its exponential is off by twice what lse
+         is off by, relative to the softmax's share of it.
+  dh, dW: the sum of |entry's error| times |factor|, an fp32 sum of n terms,
+         and the result's rounding to bf16, 2^-8 of it.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_20359_amd as P
+
+    P.lib()
+    return dict(torch=torch, P=P)
+
+
+def say(*a):
+    print("[gpu-head]", *a, flush=True)
+
+
+def make(torch, T, V, D, seed=0, spread=2.5, pad=0, wpad=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed + 1000 * T + V + D)
+    h = torch.randn(T, D + pad, generator=g, device="cuda").bfloat16()[:, :D]
+    w = (torch.randn(V, D + wpad, generator=g, device="cuda") * (spread / math.sqrt(D))).bfloat16()[:, :D]
+    return g, h, w
+
+
+class Case:
+    """Inputs of one call and its results in 64 bits."""
+
+    def __init__(self, torch, T, V, D, K=0, tau=1.0, mass=False, empty=0.2, weighted=True, seed=0,
+                 pad=0, wpad=0, poison=False, spread=2.5):
+        self.torch, self.T, self.V, self.D, self.K, self.tau = torch, T, V, D, K, tau
+        g, self.h, self.w = make(torch, T, V, D, seed, spread, pad, wpad)
+        keep = torch.rand(T, generator=g, device="cuda") >= empty
+        h, w = self.h.double(), self.w.double()
+        z = h @ w.t()
+        if K == 0:
+            y = torch.randint(0, V, (T,), generator=g, device="cuda")
+            self.labels = torch.where(keep, y, -100 - y)
+            self.ids = None
+            there = keep[:, None]
+            ids, logp = y[:, None], torch.zeros(T, 1, dtype=torch.float64, device="cuda")
+        else:
+            az = (z + torch.randn(T, V, generator=g, device="cuda")).float()
+            a, i = az.topk(K, dim=1)
+            there = keep[:, None] & (torch.rand(T, K, generator=g, device="cuda") >= 0.1)
+            self.labels = None
+            self.ids = torch.where(there, i, -1 - i).int()
+            self.a = torch.where(there, a, math.nan)      # what is absent is not looked at
+            if K > 3:
+                # a repeated word, and a word that the teacher rules out
+                self.ids[:, 2] = self.ids[:, 1]
+                self.a[:, 2] = self.a[:, 1]
+                self.a[:, 3] = -math.inf
+                there[:, 2] = there[:, 1]
+                i[:, 2] = i[:, 1]
+            there = there & (self.a > -math.inf)
+            self.alse = torch.logsumexp(az.double() / tau, 1).float() if mass else None
+            x = torch.where(there, self.a.double() / tau, -math.inf)
+            ref = self.alse.double() if mass else torch.logsumexp(x, 1)
+            logp = torch.where(there, x - ref[:, None], -math.inf)
+            keep = there.any(1)
+            ids = i
+        if poison:
+            self.h[~keep] = torch.tensor([math.nan, math.inf, -math.inf, 1e38], device="cuda",
+                                         dtype=torch.bfloat16).repeat(D // 4 + 1)[:D]
+            h = torch.where(keep[:, None], self.h.double(), 0.0)
+            z = h @ w.t()
+        self.keep = keep
+        p = torch.where(there, logp.exp(), 0.0)
+        self.there = there
+        self.z_off = (D + 8) * U * (h.abs() @ w.t().abs()).amax(1)
+        lse = torch.logsumexp(z / tau, 1)
+        target = torch.where(there | (self.ids >= 0 if K else there), z.gather(1, ids), 0.0)
+        safe = torch.where(there, logp, 0.0)
+        loss = tau * tau * (p * (safe - target / tau + lse[:, None])).sum(1)
+        zero = torch.zeros_like(lse)
+        self.loss = torch.where(keep, loss, zero)
+        self.lse = torch.where(keep, lse, zero)
+        self.target = torch.where(keep[:, None], target, 0.0)
+        mass_t = p.sum(1)
+        dl = torch.full((T,), 1.0 / max(1, int(keep.sum())), device="cuda")
+        if weighted:
+            dl = dl * (torch.rand(T, generator=g, device="cuda") - 0.25)
+        self.dloss = dl
+        c = torch.where(keep, dl.double() * tau, 0.0)
+        share = torch.exp(z / tau - lse[:, None]) * (c * mass_t)[:, None]
+        G = share.clone()
+        G.scatter_add_(1, ids, -(c[:, None] * p))
+        self.dh, self.dw = G @ w, G.t() @ h
+        self.lse_off = self.z_off / tau + 2.0 ** -16 + 4 * U * lse.abs()
+        # the teacher's probabilities: exp of a difference in fp32
+        p_off = (8 + 4 * safe.abs()).amax(1) * U if K else zero
+        off = (2.0 ** -8 * 1.01 * G.abs() + (2 * self.lse_off + 2 * p_off + 2.0 ** -20)[:, None] * share.abs())
+        spot = torch.zeros_like(G).scatter_add_(1, ids, (c[:, None] * p).abs())
+        off += (2 * p_off + 2.0 ** -20)[:, None] * spot
+        self.dh_off = off @ w.abs() + (V + 64) * U * (G.abs() @ w.abs()) + 2.0 ** -7.9 * self.dh.abs() + 1e-37
+        self.dw_off = off.t() @ h.abs() + (T + 64) * U * (G.abs().t() @ h.abs()) + 2.0 ** -7.9 * self.dw.abs() + 1e-37
+        scale = (p.sum(1) * (self.lse_off + self.z_off / tau)
+                 + (p * (safe.abs() + (target / tau).abs() + lse.abs()[:, None])).sum(1) * (K + 16) * U
+                 + 2 * p_off * (p * (safe - target / tau + lse[:, None]).abs()).sum(1))
+        self.loss_off = tau * tau * scale + 2.0 ** -22 * self.loss.abs()
+
+    def outputs(self):
+        torch = self.torch
+        f = lambda *s: torch.full(s, -7.0, device="cuda")  # noqa: E731
+        b = lambda *s: torch.full(s, -7.0, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+        t = (self.T,) if self.K == 0 else (self.T, self.K)
+        return f(self.T), f(self.T), f(*t), b(self.T, self.D), b(self.V, self.D)
+
+    def forward(self, P, **kw):
+        loss, lse, target, _, _ = self.outputs()
+        if self.K == 0:
+            P.fl_head_loss(self.h, self.w, self.labels, loss, lse, target, **kw)
+        else:
+            P.fl_head_distill(self.h, self.w, self.ids, self.a, self.alse, self.tau, loss, lse,
+                              target, **kw)
+        return loss, lse, target
+
+    def backward(self, P, lse, target, **kw):
+        _, _, _, dh, dw = self.outputs()
+        if self.K == 0:
+            P.fl_head_loss_grad(self.h, self.w, self.labels, lse, target, self.dloss, dh, dw, **kw)
+        else:
+            P.fl_head_distill_grad(self.h, self.w, self.ids, self.a, self.alse, self.tau, lse,
+                                   target, self.dloss, dh, dw, **kw)
+        return dh, dw
+
+    def check(self, P, **kw):
+        loss, lse, target = self.forward(P, **kw)
+        near("lse", lse, self.lse, self.lse_off)
+        near("target", target.reshape(self.target.shape), self.target, self.z_off[:, None] + 1e-30)
+        near("loss", loss, self.loss, self.loss_off)
+        assert (loss[~self.keep] == 0).all() and (lse[~self.keep] == 0).all()
+        dh, dw = self.backward(P, lse, target, **kw)
+        near("dhidden", dh, self.dh, self.dh_off)
+        near("dweight", dw, self.dw, self.dw_off)
+        assert (dh[~self.keep] == 0).all()
+        return loss, lse, target, dh, dw
+
+
+def near(what, got, want, off):
+    d = (got.double() - want).abs()
+    bad = ~(d <= off)
+    if bool(bad.any()):
+        i = tuple(int(x) for x in bad.nonzero()[0])
+        raise AssertionError("%s: %d of %d off, first at %s: got %.9g, expected %.9g, allowed %.3g"
+                             % (what, int(bad.sum()), bad.numel(), i, got[i], want[i],
+                                off.expand_as(d)[i]))
+
+
+# one token, odd widths, the tiles' edges, both sides of each tile choice
+SIZES = [(1, 1, 1), (1, 7, 3), (2, 300, 8), (7, 1000, 96), (16, 513, 64), (17, 130, 65),
+         (64, 257, 128), (65, 1000, 72), (129, 2049, 130), (256, 512, 192), (300, 5003, 321),
+         (1, 40000, 256), (33, 9000, 1024), (1030, 16500, 136), (2100, 700, 64)]
+
+
+@pytest.mark.parametrize("T,V,D", SIZES)
+def test_loss_and_gradient(env, T, V, D):
+    say("loss", T, V, D)
+    Case(env["torch"], T, V, D).check(env["P"])
+
+
+@pytest.mark.parametrize("T,V,D,K,tau,mass", [
+    (1, 1, 1, 1, 1.0, False), (1, 50, 8, 5, 2.0, True), (9, 700, 96, 64, 1.5, False),
+    (33, 513, 65, 65, 1.0, True), (130, 3000, 128, 128, 4.0, True), (300, 2100, 320, 7, 0.5, False),
+    (1030, 16500, 64, 32, 2.0, True)])
+def test_distillation_and_gradient(env, T, V, D, K, tau, mass):
+    say("distill", T, V, D, K, tau, mass)
+    Case(env["torch"], T, V, D, K=K, tau=tau, mass=mass).check(env["P"])
+
+
+@pytest.mark.parametrize("K", [0, 6])
+def test_tokens_left_out_hold_anything(env, K):
+    """NaN and infinities in the hidden states of tokens that take no part
+    reach nothing."""
+    Case(env["torch"], 200, 900, 128, K=K, empty=0.5, poison=True).check(env["P"])
+
+
+@pytest.mark.parametrize("K", [0, 4])
+@pytest.mark.parametrize("T", [3, 300])
+def test_no_token_takes_part(env, K, T):
+    c = Case(env["torch"], T, 400, 64, K=K, empty=2.0)
+    *_, dh, dw = c.check(env["P"])
+    assert (dh == 0).all() and (dw == 0).all()
+
+
+def test_every_token_takes_part(env):
+    Case(env["torch"], 513, 1024, 128, empty=0.0, weighted=False).check(env["P"])
+
+
+def test_no_tokens(env):
+    c = Case(env["torch"], 0, 100, 64)
+    *_, dw = c.check(env["P"])
+    assert (dw == 0).all()
+
+
+@pytest.mark.parametrize("pad,wpad", [(8, 0), (5, 0), (0, 8), (3, 11)])
+def test_longer_rows(env, pad, wpad):
+    Case(env["torch"], 70, 600, 128, pad=pad, wpad=wpad).check(env["P"])
+    Case(env["torch"], 70, 600, 96, K=5, pad=pad, wpad=wpad).check(env["P"])
+
+
+def test_hidden_states_off_sixteen_bytes(env):
+    torch, P = env["torch"], env["P"]
+    c = Case(torch, 40, 500, 65)
+    base = torch.empty(41 * 65, dtype=torch.bfloat16, device="cuda")
+    view = base[65:].view(40, 65)
+    view.copy_(c.h)
+    c.h = view
+    c.check(P)
+
+
+@pytest.mark.parametrize("K", [0, 5])
+def test_several_pieces_of_the_vocabulary(env, K):
+    """Enough tokens that G is made in two pieces."""
+    Case(env["torch"], 20000, 9001, 64, K=K).check(env["P"])
+
+
+def test_spread_logits(env):
+    """Logits of hundreds: the maximum has to be taken out first."""
+    Case(env["torch"], 40, 700, 64, spread=200.0).check(env["P"])
+
+
+def test_same_bits_twice_and_on_another_stream(env):
+    torch, P = env["torch"], env["P"]
+    c = Case(torch, 300, 5003, 256, K=8, tau=2.0)
+    a = c.check(P)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b = c.check(P)
+    f = c.forward(P, stream=s)
+    g = c.backward(P, f[1], f[2], stream=s)
+    s.synchronize()
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+    for x, y in zip(a, (*f, *g)):
+        assert torch.equal(x, y)
+
+
+def test_labels_past_the_vocabulary_give_nan(env):
+    torch, P = env["torch"], env["P"]
+    c = Case(torch, 5, 100, 64, empty=0.0)
+    c.labels[2] = 100
+    loss, lse, target = c.forward(P)
+    assert torch.isnan(loss).tolist() == [False, False, True, False, False]
+    dh, dw = c.backward(P, lse, target)
+    assert torch.isnan(dh).all(1).tolist() == [False, False, True, False, False]
+    assert torch.isnan(dw).all()
+    c = Case(torch, 5, 100, 64, K=3, empty=0.0)
+    c.ids[1, 2] = 1 << 30
+    loss, lse, target = c.forward(P)
+    assert torch.isnan(loss).tolist() == [False, True, False, False, False]
+    dh, dw = c.backward(P, lse, target)
+    assert torch.isnan(dh).all(1).tolist() == [False, True, False, False, False]
+
+
+@pytest.mark.parametrize("K", [0, 4])
+def test_gradient_against_differences(env, K):
+    """sum(dloss * loss) along a direction, by the forward call on both sides,
+    against the gradient.  Inputs and steps lie on a grid that bf16 holds.  What
+    remains of a central difference of lse is at most a third of the cube of the
+    largest change of a logit."""
+    torch, P = env["torch"], env["P"]
+    T, V, D, tau = 24, 300, 64, 1.0
+    c = Case(torch, T, V, D, K=K, tau=tau, mass=True, empty=0.2)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    c.h = (torch.randint(-28, 29, (T, D), generator=g, device="cuda") / 16).bfloat16()
+    c.w = (torch.randint(-12, 13, (V, D), generator=g, device="cuda") / 32).bfloat16()
+    _, lse, target = c.forward(P)
+    dh, dw = c.backward(P, lse, target)
+    dl = c.dloss.double()
+
+    def total(h, w):
+        c.h, c.w = h, w
+        return (c.forward(P)[0].double() * dl).sum()
+
+    h0, w0 = c.h, c.w
+    sh = (torch.randint(-1, 2, (T, D), generator=g, device="cuda") / 64).bfloat16()
+    sw = (torch.randint(-1, 2, (V, D), generator=g, device="cuda") / 256).bfloat16()
+    off = (D + 8) * U * (h0.double().abs() @ w0.double().abs().t()).amax() * 2 + 2.0 ** -14
+    for name, grad, step, diff, change in (
+            ("dhidden", dh, sh, total(h0 + sh, w0) - total(h0 - sh, w0), (sh.double() @ w0.double().t())),
+            ("dweight", dw, sw, total(h0, w0 + sw) - total(h0, w0 - sw), (h0.double() @ sw.double().t()))):
+        along = 2 * (grad.double() * step.double()).sum()
+        allowed = (dl.abs().sum() * (change.abs().amax() ** 3 / 3 + 2 * off)
+                   + 2.0 ** -6 * (grad.double() * step.double()).abs().sum())
+        assert abs(diff - along) <= allowed, (name, float(diff), float(along), float(allowed))
+        # the bound says something: it is well under what is compared
+        assert allowed < 0.5 * (grad.double() * step.double()).abs().sum()
+
+
+def test_graph_replays(env):
+    """Forward and gradient captured once; replays with other inputs and eager
+    work between them equal the eager results."""
+    torch, P = env["torch"], env["P"]
+    T, V, D = 200, 3000, 128
+    cs = [Case(torch, T, V, D, seed=i) for i in range(3)]
+    c = Case(torch, T, V, D, seed=9)
+    ws_f = torch.empty(P.head_workspace_bytes(T, V, D), dtype=torch.uint8, device="cuda")
+    ws_b = torch.empty(P.head_workspace_bytes(T, V, D, grad=True), dtype=torch.uint8, device="cuda")
+    loss, lse, target, dh, dw = c.outputs()
+
+    def step():
+        P.fl_head_loss(c.h, c.w, c.labels, loss, lse, target, workspace=ws_f)
+        P.fl_head_loss_grad(c.h, c.w, c.labels, lse, target, c.dloss, dh, dw, workspace=ws_b)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for o in cs + cs[:1]:
+        c.h.copy_(o.h), c.w.copy_(o.w), c.labels.copy_(o.labels), c.dloss.copy_(o.dloss)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (loss, lse, target, dh, dw)]
+        want = o.check(P)
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+
+
+# ---- top logits --------------------------------------------------------------
+
+
+def top(P, torch, x, k, tau=1.0, **kw):
+    n = x.shape[0]
+    v = torch.full((n, k), -7.0, device="cuda")
+    i = torch.full((n, k), -7, dtype=torch.int32, device="cuda")
+    s = torch.full((n,), -7.0, device="cuda")
+    P.fl_top_logits(x, k, tau, v, i, s, **kw)
+    return v, i, s
+
+
+def check_top(P, torch, x, k, tau=1.0):
+    v, i, s = top(P, torch, x, k, tau)
+    # a stable sort keeps equal values in the order of their ids; NaN sorts first
+    want, at = torch.sort(x.double() + 0.0, dim=1, descending=True, stable=True)
+    assert torch.equal(i.long(), at[:, :k])
+    assert torch.equal(v.double().nan_to_num(nan=1e300), want[:, :k].nan_to_num(nan=1e300))
+    lse = torch.logsumexp(x.double() / tau, 1)
+    ok = torch.isfinite(lse)
+    d = (s.double() - lse).abs()[ok]
+    assert (d <= 2.0 ** -16 + 4 * U * lse.abs()[ok]).all(), float(d.max())
+    return v, i, s
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,v,k", [
+    (1, 1, 1), (3, 2, 2), (1, 100, 100), (5, 511, 128), (2, 4096, 64), (2, 4097, 64), (3, 8191, 1),
+    (1, 50257, 8), (1, 128256, 128), (100, 100003, 100), (700, 1000, 33), (600, 33000, 16),
+    (520, 70001, 5), (2, 1 << 20, 128)])
+def test_top_logits(env, n, v, k, dtype):
+    torch, P = env["torch"], env["P"]
+    say("top", n, v, k, dtype)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + v + k)
+    x = torch.randn(n, v, generator=g, device="cuda") * 3
+    x = x.bfloat16() if dtype == "bf16" else x
+    check_top(P, torch, x, k, 2.0)
+    check_top(P, torch, torch.sort(x, dim=1).values, k)                    # rising
+    check_top(P, torch, torch.sort(x, dim=1, descending=True).values, k)   # falling
+    check_top(P, torch, x.round(), k)                                      # many ties
+    check_top(P, torch, torch.zeros_like(x), k)                            # nothing but ties
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("pad", [1, 3, 8, 47])
+def test_top_logits_of_padded_rows(env, pad, dtype):
+    torch, P = env["torch"], env["P"]
+    x = torch.randn(37, 5001 + pad, device="cuda")
+    x = x.bfloat16() if dtype == "bf16" else x
+    x[:, 5001:] = math.inf          # what lies between the rows is not looked at
+    check_top(P, torch, x[:, :5001], 20)
+    check_top(P, torch, x[1:, 1:5001], 20)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_top_logits_of_masked_rows(env, dtype):
+    """Rows of which little is left: words ruled out by -inf or by the type's
+    lowest value, NaN, infinities, zeros of both signs."""
+    torch, P = env["torch"], env["P"]
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = torch.randn(8, 40001, device="cuda").to(dt)
+    x[0, 10:] = -math.inf
+    x[1] = -math.inf
+    x[2, 5:] = torch.finfo(dt).min
+    x[3] = torch.finfo(dt).min
+    x[4, 20000:20010] = math.inf
+    x[5, ::1000] = math.nan
+    x[6] = 0.0
+    x[6, ::3] = -0.0
+    x[7, 17] = -math.inf
+    v, i, s = check_top(P, torch, x, 64)
+    assert s[1] == -math.inf
+
+
+def test_top_logits_without_lse_and_twice(env):
+    torch, P = env["torch"], env["P"]
+    x = torch.randn(300, 60000, device="cuda").bfloat16()
+    a = top(P, torch, x, 64)
+    b = top(P, torch, x, 64)
+    for p, q in zip(a, b):
+        assert torch.equal(p, q)
+    v, i = torch.empty_like(a[0]), torch.empty_like(a[1])
+    P.fl_top_logits(x, 64, 1.0, v, i)
+    assert torch.equal(v, a[0]) and torch.equal(i, a[1])
+    P.fl_top_logits(x[:0], 4, 1.0, v[:0, :4].contiguous(), i[:0, :4].contiguous())
+
+
+def test_binding_refuses(env):
+    """Shapes, dtypes and strides that the kernels do not take raise before the
+    library is called."""
+    torch, P = env["torch"], env["P"]
+    c = Case(torch, 6, 50, 16)
+    loss, lse, target, dh, dw = c.outputs()
+    bad = [
+        dict(h=c.h.float()), dict(h=c.h[:, :8]), dict(h=c.h.t().contiguous().t()),
+        dict(h=c.h[:1].expand(6, 16)), dict(h=c.h[0]), dict(w=c.w.float()), dict(w=c.w[:, :8]),
+        dict(y=c.labels.int()), dict(y=c.labels[:5]), dict(y=c.labels.cpu()), dict(o=loss[:5]),
+        dict(o=loss.double())]
+    for b in bad:
+        with pytest.raises(ValueError):
+            P.fl_head_loss(b.get("h", c.h), b.get("w", c.w), b.get("y", c.labels), b.get("o", loss),
+                           lse, target)
+    for b in (dict(dh=dh.float()), dict(dh=dh[:, :8]), dict(dw=dw[:, :8]), dict(dw=dw.t())):
+        with pytest.raises(ValueError):
+            P.fl_head_loss_grad(c.h, c.w, c.labels, lse, target, c.dloss, b.get("dh", dh),
+                                b.get("dw", dw))
+    with pytest.raises(P.FlError):
+        P.fl_head_loss_grad(c.h, c.w, c.labels, lse, target, c.dloss, dh, c.w)
+    with pytest.raises(P.FlError):
+        P.fl_head_loss(c.h, c.w, c.labels, loss, lse, target,
+                       workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    i, f = torch.zeros(6, 3, dtype=torch.int32, device="cuda"), torch.zeros(6, 3, device="cuda")
+    for ids, a, al, t in ((i.long(), f, None, f), (i, f[:, :2], None, f), (i, f, loss[:2], f),
+                          (i, f, None, f[:, :2]), (i[0], f, None, f)):
+        with pytest.raises(ValueError):
+            P.fl_head_distill(c.h, c.w, ids, a, al, 1.0, loss, lse, t)
+    with pytest.raises(P.FlError):
+        P.fl_head_distill(c.h, c.w, i, f, None, 0.0, loss, lse, f)
+    x = torch.zeros(6, 50, device="cuda")
+    for y, k, v, j in ((x.half(), 3, f, i), (x, 4, f, i), (x, 3, f.double(), i), (x, 3, f, i.long()),
+                       (x.t().contiguous().t(), 3, f, i), (x[0], 3, f, i)):
+        with pytest.raises(ValueError):
+            P.fl_top_logits(y, k, 1.0, v, j)
+    v, j = torch.zeros(6, 51, device="cuda"), torch.zeros(6, 51, dtype=torch.int32, device="cuda")
+    with pytest.raises(P.FlError):
+        P.fl_top_logits(x, 51, 1.0, v, j)
