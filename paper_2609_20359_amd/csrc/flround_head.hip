@@ -57,19 +57,33 @@ __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x
 //
 //   rows across it (TR = true): the stage holds 64 rows of B elements.  A
 //   fragment is two transposing reads of 8 bytes: 16 lanes read 4 rows of 16
-//   elements, and lane i gets column i.  The 32-byte pair of chunks c of row k
-//   lies at place c ^ ((k & 3) | (k >> 3 & 3) << 2): the 16 rows that a wave
-//   reads at a time fall on different banks.
+//   elements, and lane i gets column i.  A wave reads 32 bytes of each of 16
+//   rows at a time, 8 (l / 16) + 0..3.  So that these fall on different banks,
+//   what a wave loads at once (1024 B: 2 or 4 rows) is a block of its own, 64 B
+//   on from where the last one ends (and 128 B more after every 8 rows where a
+//   block has 2), and in a block the pairs of chunks of row r lie at place
+//   c ^ r.
 //
 // The loads write LDS in lane order, so the places are permuted by permuting
 // which global chunk a lane asks for.
 
+// The same value, of which the compiler keeps nothing derived: it is to hold few
+// registers across the loop below rather than save an addition in it.
+__device__ __forceinline__ uint32_t pinned(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 template <int B, int NT, bool TR>
 struct Operand {
   static constexpr int kLoads = (B * 8 + NT - 1) / NT;   // 16-byte loads per thread and step
-  static constexpr int kChunks = TR ? B / 8 : 8;   // 16-byte chunks per LDS row
-  static constexpr int kPairs = B / 16;
+  static constexpr int kChunks = TR ? B / 8 : 8;         // 16-byte chunks per row
+  static constexpr int kBlockRows = 64 / kChunks;        // rows per block (TR)
+  static constexpr int kPitch = TR ? 1024 + 64 : 1024;   // bytes from block to block
+  static constexpr int kSkip = TR && B == 256 ? 128 : 0; // and after every 8 rows
+  static constexpr int kBytes = (B / 8 * kPitch + 8 * kSkip + 127) / 128 * 128;
   static_assert(B * 8 % NT == 0 || B * 8 < NT, "whole loads, or the first waves' alone");
+  static_assert(!TR || B == 128 || B == 256, "blocks of whole rows");
 
   const char* base;       // of the tile
   uint32_t at[kLoads];    // byte offset of each load
@@ -78,9 +92,12 @@ struct Operand {
   __device__ __forceinline__ static int row(int tid, int c) { return (tid + c * NT) / kChunks; }
   __device__ __forceinline__ static int chunk(int tid, int c) {
     const int place = (tid + c * NT) % kChunks, r = row(tid, c);
-    if (!TR) return place ^ (r & 7);
-    const int x = ((r & 3) | ((r >> 3) & 3) << 2) & (kPairs - 1);
-    return place ^ (x << 1);
+    return TR ? place ^ (r % kBlockRows) << 1 : place ^ (r & 7);
+  }
+  // Where load c of a wave goes.
+  __device__ __forceinline__ static char* place(char* lds, int wave, int c) {
+    const int m = c * (NT / 64) + wave;
+    return lds + m * kPitch + (m / 4) * kSkip;
   }
 
   // src: row 0 of the tile (TR = false: row b0, column 0; TR = true: row 0,
@@ -100,59 +117,85 @@ struct Operand {
     }
   }
 
-  __device__ __forceinline__ void load(uint16_t* lds, int64_t s, int wave) const {
+  // Loads [c0, c1) of step s.
+  __device__ __forceinline__ void load(char* lds, int s, int wave, int c0, int c1) const {
     const char* b = base + s * step;
 #pragma unroll
-    for (int c = 0; c < kLoads; ++c)
-      if (c * NT + wave * 64 < B * 8)
-        __builtin_amdgcn_global_load_lds((const GLOBAL_SPACE void*)(b + at[c]),
-                                         (LDS_SPACE void*)(lds + (c * NT + wave * 64) * 8), 16, 0, 0);
+    for (int c = c0; c < c1; ++c)
+      if (B * 8 % NT == 0 || wave * 64 < B * 8) {
+        __builtin_amdgcn_global_load_lds((const GLOBAL_SPACE void*)(b + pinned(at[c])),
+                                         (LDS_SPACE void*)place(lds, wave, c), 16, 0, 0);
+      }
   }
 
-  // The last step when the summed axis ends inside it: `left` elements of it
-  // remain (in whole chunks where TR = false), the others are zero.
-  __device__ __forceinline__ void load_tail(uint16_t* lds, int64_t s, int wave, int tid, int left,
+  // The step that the summed axis ends inside: `left` elements of it remain (in
+  // whole chunks where TR = false), the others are zero.
+  __device__ __forceinline__ void load_tail(char* lds, int s, int wave, int tid, int left,
                                             const uint16_t* zero) const {
     const char* b = base + s * step;
 #pragma unroll
     for (int c = 0; c < kLoads; ++c) {
-      if (c * NT + wave * 64 >= B * 8) continue;
+      if (B * 8 % NT != 0 && wave * 64 >= B * 8) continue;
       const bool in = TR ? row(tid, c) < left : chunk(tid, c) * 8 < left;
-      const char* p = in ? b + at[c] : reinterpret_cast<const char*>(zero);
+      const char* p = in ? b + pinned(at[c]) : reinterpret_cast<const char*>(zero);
       __builtin_amdgcn_global_load_lds((const GLOBAL_SPACE void*)p,
-                                       (LDS_SPACE void*)(lds + (c * NT + wave * 64) * 8), 16, 0, 0);
+                                       (LDS_SPACE void*)place(lds, wave, c), 16, 0, 0);
     }
   }
 
-  // Fragment at rows (columns) b0 + 16 i of the tile, half ks of the step.
-  __device__ __forceinline__ static bf16x8 frag(const uint16_t* lds, int b0, int i, int ks, int l) {
-    if (!TR) {
-      const int ch = (ks * 4 + (l >> 4)) ^ (l & 7);
-      return *reinterpret_cast<const bf16x8*>(lds + (b0 + i * 16 + (l & 15)) * kStep + ch * 8);
-    }
-    const int x = (((l & 15) >> 2) | (l >> 4) << 2) & (kPairs - 1);
-    const int k = ks * 32 + 8 * (l >> 4) + ((l & 15) >> 2);
-    const uint16_t* p = lds + k * B + ((b0 / 16 + i) ^ x) * 16 + (l & 3) * 4;
+  // Place of this lane's part of the fragment at rows (columns) b0 of the tile.
+  __device__ __forceinline__ static uint32_t lane_place(int b0, int l) {
+    if (!TR) return (uint32_t)((b0 + (l & 15)) * 128 + (((l >> 4) ^ (l & 7)) * 16));
+    const int g = l >> 4, r = (l & 15) >> 2;   // row 8 g + r, and 4 on
+    const int x = r % kBlockRows;
+    return (uint32_t)((g * 8 / kBlockRows + r / kBlockRows) * kPitch + g * kSkip + x * (B * 2) +
+                      (l & 3) * 8 + ((b0 / 16) ^ x) * 32);
+  }
+  // Fragment 16 i rows (columns) on from 16 f0, lane_place()'s b0, in half ks of
+  // the step.
+  __device__ __forceinline__ static bf16x8 frag(const char* lds, uint32_t lane, int f0, int i, int ks,
+                                                int l) {
+    if (!TR)
+      return *reinterpret_cast<const bf16x8*>(lds + (ks ? lane ^ 64 : lane) + i * 16 * 128);
+    // (f0 + i) ^ x is f0 ^ x and the difference: where f0 is a multiple of
+    // kBlockRows it depends on i's low bits alone
+    const int x = ((l & 15) >> 2) % kBlockRows, low = i % kBlockRows;
+    const int on = f0 % kBlockRows ? ((f0 + i) ^ x) - (f0 ^ x) : i - low + ((low ^ x) - x);
+    const char* p = lds + lane + on * 32 + ks * (32 / kBlockRows * kPitch + 4 * kSkip);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_SPACE s16x4*)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_SPACE s16x4*)(p + 4 * B));
+    const s16x4 hi =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_SPACE s16x4*)(p + 4 / kBlockRows * kPitch));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
 
+// All of this wave's loads to LDS and reads from it are done, and all other
+// waves' too.  (A volatile statement that touches memory: neither the reads nor
+// the loads on either side cross it.)
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 enum Epilogue { kStats, kGrad, kSlab, kOut };
 
-// Tiles are dealt so that the 32 workgroups which an XCD runs at a time share
-// rows: workgroups go to the XCDs in turn, each XCD takes a contiguous range of
-// an order that runs over q within bands of kBand p tiles.
+// Workgroups stay and take one tile after another, so that the loads of the next
+// tile's first steps run under the last products and the epilogue of this one.
+// Tiles are dealt so that the workgroups of an XCD, which share an L2, share
+// rows: workgroups go to the XCDs in turn, and each XCD takes a contiguous range
+// of an order that runs over q within bands of kBand p tiles.
 constexpr int kBand = 4;
 constexpr int kXcds = 8;
 
 template <int WP, int WQ, int FP, int FQ, bool PTR, bool QTR, int EPI>
-__global__ __launch_bounds__(WP* WQ * 64) void k_tile(const TileArgs a) {
+__global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_tile(
+    const TileArgs a) {
   constexpr int NT = WP * WQ * 64, BP = WP * FP * 16, BQ = WQ * FQ * 16;
   using OpP = Operand<BP, NT, PTR>;
   using OpQ = Operand<BQ, NT, QTR>;
-  __shared__ __attribute__((aligned(1024))) uint16_t sm[2][(BP + BQ) * kStep];
+  // Two arrays, and two steps to a turn of the loop below, so that the compiler
+  // sees that reads of one stage need not wait for the loads to the other.
+  __shared__ __attribute__((aligned(128))) char sm0[OpP::kBytes + OpQ::kBytes];
+  __shared__ __attribute__((aligned(128))) char sm1[OpP::kBytes + OpQ::kBytes];
 
   const int tid = threadIdx.x, l = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -163,164 +206,236 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_tile(const TileArgs a) {
   const int tiles_p = (int)((a.np + BP - 1) / BP), tiles_q = (int)((nq + BQ - 1) / BQ);
   const int tiles = tiles_p * tiles_q;
   const int splits = EPI == kSlab ? a.splits : 1;
-  if ((int64_t)blockIdx.x >= (int64_t)tiles * splits) return;
-  const int split = EPI == kSlab ? (int)(blockIdx.x / tiles) : 0;
-  int tp, tq;
+  const int steps_all = (int)((nk + kStep - 1) / kStep);
+  const int left = (int)(nk - (int64_t)(steps_all - 1) * kStep);
+
+  // this workgroup's tiles: id, id + stride, ... below end
+  int id, end;
+  const int stride = gridDim.x / kXcds;
   {
-    int id = (int)(blockIdx.x - split * tiles);
-    const int x = id % kXcds, per = tiles / kXcds, rem = tiles % kXcds;
-    id = x * per + (x < rem ? x : rem) + id / kXcds;
-    const int band = id / (kBand * tiles_q), in = id % (kBand * tiles_q);
+    const int all = tiles * splits, x = blockIdx.x % kXcds;
+    const int per = all / kXcds, rem = all % kXcds;
+    const int start = x * per + (x < rem ? x : rem);
+    id = start + blockIdx.x / kXcds;
+    end = start + per + (x < rem);
+  }
+  if (id >= end) return;
+
+  // A tile's steps, made an even number by a step of zeros.  The step that the
+  // summed axis ends inside and the one of zeros come first, so that the loop
+  // has whole ones only.  (An operand with rows of zeros makes it whole by
+  // itself.)
+  OpP op;
+  OpQ oq;
+  int tp, tq, split, n, shift, first, first_left, second_left;
+  auto aim = [&](int id) {
+    const int t = (int)pinned(tid);
+    split = EPI == kSlab ? id / tiles : 0;
+    const int in_split = id - split * tiles;
+    const int band = in_split / (kBand * tiles_q), in = in_split % (kBand * tiles_q);
     const int width = tiles_p - band * kBand < kBand ? tiles_p - band * kBand : kBand;
     tp = band * kBand + in % width;
     tq = in / width;
-  }
-  const int64_t p0 = (int64_t)tp * BP, q0 = (int64_t)tq * BQ;
-  // the steps of this split
-  const int64_t steps_all = (nk + kStep - 1) / kStep;
-  const int64_t s0 = steps_all * split / splits, s1 = steps_all * (split + 1) / splits;
-  // an operand's rows of zeros make the last step whole, except the weight's
-  const int left = (int)(nk - (steps_all - 1) * kStep);
-  const bool ragged = EPI != kOut && left < kStep;
-
-  OpP op;
-  OpQ oq;
-  op.init(PTR ? a.P + p0 : a.P + p0 * a.ldp, a.ldp, a.np - p0, tid);
-  // the rows of q are padded to whole tiles
-  oq.init(QTR ? a.Q + q0 : a.Q + q0 * a.ldq, a.ldq, BQ, tid);
-  auto load = [&](int st, int64_t s) {
-    if (ragged && s == steps_all - 1)
-      op.load_tail(sm[st], s, w, tid, left, a.zero);
-    else
-      op.load(sm[st], s, w);
-    oq.load(sm[st] + BP * kStep, s, w);
+    const int64_t p0 = (int64_t)tp * BP, q0 = (int64_t)tq * BQ;
+    op.init(PTR ? a.P + p0 : a.P + p0 * a.ldp, a.ldp, a.np - p0, t);
+    // the rows of q are padded to whole tiles
+    oq.init(QTR ? a.Q + q0 : a.Q + q0 * a.ldq, a.ldq, BQ, t);
+    const int s0 = (int)((int64_t)steps_all * split / splits);
+    const int s1 = (int)((int64_t)steps_all * (split + 1) / splits);
+    const int ragged = EPI != kOut && s1 == steps_all && left < kStep;
+    const int zeros = s1 == s0 ? 2 : (s1 - s0) & 1;
+    n = s1 - s0 + zeros;
+    shift = s0 - ragged - (zeros & 1);   // step i of the tile is i + shift, for i > 1
+    first = ragged ? steps_all - 1 : s0;
+    first_left = zeros == 2 ? 0 : ragged ? left : kStep;
+    second_left = zeros ? 0 : kStep;     // and its second is s0 + 1 - ragged
+    n = __builtin_amdgcn_readfirstlane(n);
+    shift = __builtin_amdgcn_readfirstlane(shift);
+    first = __builtin_amdgcn_readfirstlane(first);
+    first_left = __builtin_amdgcn_readfirstlane(first_left);
+    second_left = __builtin_amdgcn_readfirstlane(second_left);
+  };
+  auto load_first = [&](char* to) {
+    op.load_tail(to, first, w, (int)pinned(tid), first_left, a.zero);
+    oq.load_tail(to + OpP::kBytes, first, w, (int)pinned(tid), first_left ? kStep : 0, a.zero);
+  };
+  auto load_second = [&](char* to) {
+    op.load_tail(to, 1 + shift, w, (int)pinned(tid), second_left, a.zero);
+    oq.load_tail(to + OpP::kBytes, 1 + shift, w, (int)pinned(tid), second_left, a.zero);
   };
 
   f32x4 acc[FP][FQ];
+  bf16x8 fp[FP], qa[FQ], qb[FQ];
+  // Half a step: the products of one set of fragments and, as each of P's is
+  // done with, the read of the next; Q's, which all products use, have two
+  // places.
+  const uint32_t lane_p = OpP::lane_place(wp * FP * 16, l), lane_q = OpQ::lane_place(wq * FQ * 16, l);
+  auto half = [&](const bf16x8(&q)[FQ], bf16x8(&qn)[FQ], const char* from, int ks, bool meet,
+                  auto fill) {
+    const uint32_t lp = pinned(lane_p), lq = pinned(lane_q);
 #pragma unroll
-  for (int i = 0; i < FP; ++i)
+    for (int i = 0; i < FP; ++i) {
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < FQ; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i], q[j], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (meet && i == 0) wait_and_meet();
+      fp[i] = OpP::frag(from, lp, wp * FP, i, ks, l);
+#pragma unroll
+      for (int j = i * FQ / FP; j < (i + 1) * FQ / FP; ++j)
+        qn[j] = OpQ::frag(from + OpP::kBytes, lq, wq * FQ, j, ks, l);
+      fill(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // A step in stage `in`, whose successor is in stage `next`; fill(i), part i of
+  // FP, loads what comes after that to `in`.  At the meeting every wave has read
+  // `in`, and `next` is filled.
+  auto step = [&](char* in, char* next, auto fill) {
+    half(qa, qb, in, 1, false, [](int) {});
+    half(qb, qa, next, 0, true, fill);
+  };
 
-  if (s0 < s1) {
-    load(0, s0);
-    __syncthreads();
-  }
+  aim(id);
+  load_first(sm0);
+  load_second(sm1);
+  wait_and_meet();
+#pragma unroll
+  for (int j = 0; j < FQ; ++j) qa[j] = OpQ::frag(sm0 + OpP::kBytes, lane_q, wq * FQ, j, 0, l);
+#pragma unroll
+  for (int i = 0; i < FP; ++i) fp[i] = OpP::frag(sm0, lane_p, wp * FP, i, 0, l);
+
 #pragma unroll 1
-  for (int64_t s = s0; s < s1; ++s) {
-    const int st = (int)((s - s0) & 1);
-    if (s + 1 < s1) load(st ^ 1, s + 1);
-    const uint16_t* lp = sm[st];
-    const uint16_t* lq = sm[st] + BP * kStep;
+  for (;;) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 fp[FP], fq[FQ];
+    for (int i = 0; i < FP; ++i)
 #pragma unroll
-      for (int i = 0; i < FP; ++i) fp[i] = OpP::frag(lp, wp * FP * 16, i, ks, l);
-#pragma unroll
-      for (int j = 0; j < FQ; ++j) fq[j] = OpQ::frag(lq, wq * FQ * 16, j, ks, l);
-#pragma unroll
-      for (int i = 0; i < FP; ++i)
-#pragma unroll
-        for (int j = 0; j < FQ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int s = 2; s < n; s += 2) {
+      auto fill = [&](char* to, int s, int i) {
+        op.load(to, s, w, i * OpP::kLoads / FP, (i + 1) * OpP::kLoads / FP);
+        oq.load(to + OpP::kBytes, s, w, i * OpQ::kLoads / FP, (i + 1) * OpQ::kLoads / FP);
+      };
+      step(sm0, sm1, [&](int i) { fill(sm0, s + shift, i); });
+      step(sm1, sm0, [&](int i) { fill(sm1, s + 1 + shift, i); });
     }
-    __syncthreads();
-  }
+    const int my_split = split;
+    const int64_t p0 = (int64_t)tp * BP, q0 = (int64_t)tq * BQ;
+    const int my_part = tp * WP + wp;
+    // after the last tile: its own first steps again, which nothing reads
+    const bool more = id + stride < end;
+    aim(more ? id + stride : id);
+    step(sm0, sm1, [&](int i) { if (i == 0) load_first(sm0); });
+    step(sm1, sm0, [&](int i) { if (i == 0) load_second(sm1); });
 
-  // lane l holds, of the 16 x 16 outputs (i, j), q = l % 16 and
-  // p = 4 (l / 16) .. + 3
-  const int64_t pw = p0 + wp * FP * 16 + (l >> 4) * 4;
-  const int64_t qw = q0 + wq * FQ * 16 + (l & 15);
+    // lane l holds, of the 16 x 16 outputs (i, j), q = l % 16 and
+    // p = 4 (l / 16) .. + 3
+    const int l = (int)pinned(tid) & 63;
+    const int64_t pw = p0 + wp * FP * 16 + (l >> 4) * 4;
+    const int64_t qw = q0 + wq * FQ * 16 + (l & 15);
 
-  if constexpr (EPI == kStats) {
+    if constexpr (EPI == kStats) {
+      if (p0 + BP > a.np) {
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-      float m = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < FP; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float y = pw + i * 16 + e < a.np ? acc[i][j][e] * a.s2 : -INFINITY;
-          acc[i][j][e] = y;
-          m = fmaxf(m, y);
-        }
-      m = fmaxf(m, __shfl_xor(m, 16));
-      m = fmaxf(m, __shfl_xor(m, 32));
-      // a row of which nothing is there, or only -inf, sums to 0
-      const float ref = m == -INFINITY ? 0.f : m;
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < FP; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum += exp2_(acc[i][j][e] - ref);
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      if (l < 16) a.parts[(int64_t)(tp * WP + wp) * a.parts_ld + qw + j * 16] = make_float2(m, sum);
-    }
-  } else if constexpr (EPI == kGrad) {
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-      const int64_t q = qw + j * 16;
-      const bool live = q < n_live;
-      const float lse2 = live ? a.row_lse2[q] : 0.f, coef = live ? a.row_coef[q] : 0.f;
-      uint16_t* g = a.G + q * a.ldg;
-#pragma unroll
-      for (int i = 0; i < FP; ++i) {
-        const int64_t p = pw + i * 16;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[e] = live && p + e < a.np ? coef * exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -lse2)) : 0.f;
-        if (p < a.ldg) *reinterpret_cast<u32x2*>(g + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
-      }
-    }
-  } else if constexpr (EPI == kSlab) {
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-      const int64_t q = qw + j * 16;
-      if (q >= nq) continue;
-      float* o = a.slab + split * a.slab_stride + q * a.ld_slab;
-#pragma unroll
-      for (int i = 0; i < FP; ++i) {
-        const int64_t p = pw + i * 16;
-        if (p < a.ld_slab) {
-          f32x4* d = reinterpret_cast<f32x4*>(o + p);
-          *d = a.add ? *d + acc[i][j] : acc[i][j];
-        }
-      }
-    }
-  } else {
-    const float f = a.hdr->scale * a.out_scale;
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-      const int64_t q = qw + j * 16;
-      if (q >= nq) continue;
-      uint16_t* o = a.out + q * a.ld_out;
-#pragma unroll
-      for (int i = 0; i < FP; ++i) {
-        const int64_t p = pw + i * 16;
-        const f32x4 v = acc[i][j] * f;
-        if (a.vec_out) {
-          if (p < a.np) *reinterpret_cast<u32x2*>(o + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
-        } else {
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (p + e < a.np) o[p + e] = to_bf16(v[e]);
+            if (pw + i * 16 + e >= a.np)
+#pragma unroll
+              for (int j = 0; j < FQ; ++j) acc[i][j][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+          m = fmaxf(fmaxf(fmaxf(m, acc[i][j][0]), fmaxf(acc[i][j][1], acc[i][j][2])), acc[i][j][3]);
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32)) * a.s2;
+        // a row of which nothing is there, or only -inf, sums to 0
+        const float ref = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum += exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -ref));
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (l < 16) a.parts[(int64_t)my_part * a.parts_ld + qw + j * 16] = make_float2(m, sum);
+      }
+    } else if constexpr (EPI == kGrad) {
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) {
+        const int64_t q = qw + j * 16;
+        const bool live = q < n_live;
+        const float lse2 = live ? a.row_lse2[q] : 0.f, coef = live ? a.row_coef[q] : 0.f;
+        uint16_t* g = a.G + q * a.ldg;
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+          const int64_t p = pw + i * 16;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = live && p + e < a.np ? coef * exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -lse2)) : 0.f;
+          if (p < a.ldg)
+            *reinterpret_cast<u32x2*>(g + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+        }
+      }
+    } else if constexpr (EPI == kSlab) {
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) {
+        const int64_t q = qw + j * 16;
+        if (q >= nq) continue;
+        float* o = a.slab + my_split * a.slab_stride + q * a.ld_slab;
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+          const int64_t p = pw + i * 16;
+          if (p < a.ld_slab) {
+            f32x4* d = reinterpret_cast<f32x4*>(o + p);
+            *d = a.add ? *d + acc[i][j] : acc[i][j];
+          }
+        }
+      }
+    } else {
+      const float f = a.hdr->scale * a.out_scale;
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) {
+        const int64_t q = qw + j * 16;
+        if (q >= nq) continue;
+        uint16_t* o = a.out + q * a.ld_out;
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+          const int64_t p = pw + i * 16;
+          const f32x4 v = acc[i][j] * f;
+          if (a.vec_out) {
+            if (p < a.np)
+              *reinterpret_cast<u32x2*>(o + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (p + e < a.np) o[p + e] = to_bf16(v[e]);
+          }
         }
       }
     }
+    if (!more) break;
+    id += stride;
   }
+  // no load to LDS outlives the workgroup that owns it
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 template <bool PTR, bool QTR, int EPI>
 hipError_t launch_tile(const TileArgs& a, int64_t nq, int shape, hipStream_t st) {
   const int64_t tp = (a.np + tile_p(shape) - 1) / tile_p(shape);
   const int64_t tq = (nq + tile_q(shape) - 1) / tile_q(shape);
-  const int64_t grid = tp * tq * (EPI == kSlab ? a.splits : 1);
-  if (grid <= 0) return hipSuccess;
-  if (grid > (int64_t)1 << 22) return hipErrorInvalidValue;   // x 512 threads: within 2^32
-  const dim3 g((unsigned)grid);
+  const int64_t tiles = tp * tq * (EPI == kSlab ? a.splits : 1);
+  if (tiles <= 0) return hipSuccess;
+  if (tiles > (int64_t)1 << 30) return hipErrorInvalidValue;
+  // as many as the chip holds at a time, by LDS
+  const int64_t fit = 256 * (shape == kTile256 ? 1 : shape == kTile128 ? 2 : shape == kTile64 ? 3 : 4);
+  const dim3 g((unsigned)(((tiles < fit ? tiles : fit) + kXcds - 1) / kXcds * kXcds));
   switch (shape) {
     case kTile256: k_tile<2, 4, 8, 4, PTR, QTR, EPI><<<g, 512, 0, st>>>(a); break;
     case kTile128: k_tile<2, 2, 4, 4, PTR, QTR, EPI><<<g, 256, 0, st>>>(a); break;

@@ -275,7 +275,7 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
     w.P = c.a.hc, w.ldp = p.Dp;
     w.Q = G, w.ldq = ldg;
     w.np = p.D, w.nq = v1 - v0, w.live_k = 1;
-    w.hdr = c.a.hdr;
+    w.hdr = c.a.hdr, w.zero = reinterpret_cast<const uint16_t*>(c.a.hdr->zero);
     w.out = dweight + v0 * p.D, w.ld_out = p.D;
     w.vec_out = (p.D & 3) == 0 && (reinterpret_cast<uintptr_t>(dweight) & 7) == 0;
     w.out_scale = out_scale;
