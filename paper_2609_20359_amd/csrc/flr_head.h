@@ -76,13 +76,13 @@ struct TileArgs {
   const float* row_coef;
   uint16_t* G;
   int64_t ldg;                      // also the columns of G to write
-  float* slab;                      // fp32 sums: slab[split][q][ld_slab]
-  int64_t ld_slab, slab_stride;
+  float* slab;                      // fp32 sums: slab[split][live row][ld_slab]
+  int64_t ld_slab;
   int add;                          // add to the slab
-  int splits;
+  int max_splits;
   uint16_t* out;                    // bf16 output, scaled by hdr->scale * out_scale
   int64_t ld_out;
-  int vec_out;                      // rows of out are 8-byte aligned and whole fours long
+  int vec_out;                      // rows of out are 16-byte aligned and whole eights long
   float out_scale;
 };
 
@@ -92,6 +92,16 @@ inline int tile_q(int s) { return s == kTile256 ? 256 : s == kTile128 ? 128 : s 
 // Rows of statistics that a tile of shape s writes per p tile.
 inline int tile_parts(int s) { return s == kTile256 || s == kTile128 ? 2 : 4; }
 
+inline int tile_fit(int s) {   // tiles that the chip holds at a time, by LDS
+  return 256 * (s == kTile256 ? 1 : s == kTile128 ? 2 : s == kTile64 ? 3 : 4);
+}
+// How many ways the summed axis is split: as many as fill the chip where the
+// live rows make few tiles.
+__host__ __device__ inline int splits_of(int fit, int tiles, int max_splits) {
+  const int s = tiles > 0 ? fit / tiles : 1;
+  return s < 1 ? 1 : s < max_splits ? s : max_splits;
+}
+
 hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_live(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_pack(const HeadArgs& a, bool grad, hipStream_t st);
@@ -99,8 +109,8 @@ hipError_t launch_head_pack_weight(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_finish(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_fix(const HeadArgs& a, uint16_t* G, int64_t ldg, int64_t v0, int64_t v1,
                            hipStream_t st);
-hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab,
-                          int64_t slab_stride, int splits, float out_scale, hipStream_t st);
+hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab, int shape,
+                          int max_splits, float out_scale, hipStream_t st);
 hipError_t launch_logits_stats(const TileArgs& a, int shape, hipStream_t st);
 hipError_t launch_logits_grad(const TileArgs& a, int shape, hipStream_t st);
 hipError_t launch_dhidden(const TileArgs& a, int shape, hipStream_t st);

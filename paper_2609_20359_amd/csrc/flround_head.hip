@@ -176,6 +176,22 @@ __device__ __forceinline__ void wait_and_meet() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// Two 16 x 16 results of a wave, each lane's four (along p) as bf16: a lane gets
+// eight in a row, lanes 16 k .. 16 k + 15 those from 8 k of the 32 on.
+__device__ __forceinline__ u32x4 eight(u32x2 a, u32x2 b) {
+  u32x4 o;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    // rows of 16 lanes: a0 a1 a2 a3, b0 b1 b2 b3 -> a0 a1 b0 b1, a2 a3 b2 b3
+    // -> a0 a2 b0 b2, a1 a3 b1 b3
+    const auto x = __builtin_amdgcn_permlane32_swap(a[h], b[h], false, false);
+    const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
+    o[h] = y[0];
+    o[2 + h] = y[1];
+  }
+  return o;
+}
+
 enum Epilogue { kStats, kGrad, kSlab, kOut };
 
 // Workgroups stay and take one tile after another, so that the loads of the next
@@ -186,7 +202,7 @@ enum Epilogue { kStats, kGrad, kSlab, kOut };
 constexpr int kBand = 4;
 constexpr int kXcds = 8;
 
-template <int WP, int WQ, int FP, int FQ, bool PTR, bool QTR, int EPI>
+template <int WP, int WQ, int FP, int FQ, bool PTR, bool QTR, int EPI, int FIT>
 __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_tile(
     const TileArgs a) {
   constexpr int NT = WP * WQ * 64, BP = WP * FP * 16, BQ = WQ * FQ * 16;
@@ -205,7 +221,7 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
   const int64_t nk = a.live_k ? n_live : a.nk;
   const int tiles_p = (int)((a.np + BP - 1) / BP), tiles_q = (int)((nq + BQ - 1) / BQ);
   const int tiles = tiles_p * tiles_q;
-  const int splits = EPI == kSlab ? a.splits : 1;
+  const int splits = EPI == kSlab ? splits_of(FIT, tiles, a.max_splits) : 1;
   const int steps_all = (int)((nk + kStep - 1) / kStep);
   const int left = (int)(nk - (int64_t)(steps_all - 1) * kStep);
 
@@ -365,21 +381,27 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
         if (l < 16) a.parts[(int64_t)my_part * a.parts_ld + qw + j * 16] = make_float2(m, sum);
       }
     } else if constexpr (EPI == kGrad) {
+      const bool edge = p0 + BP > a.np;
 #pragma unroll
       for (int j = 0; j < FQ; ++j) {
         const int64_t q = qw + j * 16;
         const bool live = q < n_live;
         const float lse2 = live ? a.row_lse2[q] : 0.f, coef = live ? a.row_coef[q] : 0.f;
-        uint16_t* g = a.G + q * a.ldg;
+        uint16_t* g = a.G + q * a.ldg + p0 + wp * FP * 16 + (l >> 4) * 8;
 #pragma unroll
-        for (int i = 0; i < FP; ++i) {
-          const int64_t p = pw + i * 16;
-          float v[4];
+        for (int i = 0; i < FP; i += 2) {
+          u32x2 d[2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            v[e] = live && p + e < a.np ? coef * exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -lse2)) : 0.f;
-          if (p < a.ldg)
-            *reinterpret_cast<u32x2*>(g + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+          for (int h = 0; h < 2; ++h) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = coef * exp2_(__builtin_fmaf(acc[i + h][j][e], a.s2, -lse2));
+              if (!live || (edge && pw + (i + h) * 16 + e >= a.np)) v[e] = 0.f;
+            }
+            d[h] = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+          }
+          *reinterpret_cast<u32x4*>(g + i * 16) = eight(d[0], d[1]);
         }
       }
     } else if constexpr (EPI == kSlab) {
@@ -387,7 +409,7 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
       for (int j = 0; j < FQ; ++j) {
         const int64_t q = qw + j * 16;
         if (q >= nq) continue;
-        float* o = a.slab + my_split * a.slab_stride + q * a.ld_slab;
+        float* o = a.slab + (my_split * nq + q) * a.ld_slab;
 #pragma unroll
         for (int i = 0; i < FP; ++i) {
           const int64_t p = pw + i * 16;
@@ -402,19 +424,24 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
       for (int j = 0; j < FQ; ++j) {
         const int64_t q = qw + j * 16;
-        if (q >= nq) continue;
         uint16_t* o = a.out + q * a.ld_out;
 #pragma unroll
-        for (int i = 0; i < FP; ++i) {
-          const int64_t p = pw + i * 16;
-          const f32x4 v = acc[i][j] * f;
+        for (int i = 0; i < FP; i += 2) {
+          u32x2 d[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 v = acc[i + h][j] * f;
+            d[h] = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+          }
+          const u32x4 x = eight(d[0], d[1]);
+          const int64_t p = p0 + (wp * FP + i) * 16 + (l >> 4) * 8;
+          if (q >= nq || p >= a.np) continue;
           if (a.vec_out) {
-            if (p < a.np)
-              *reinterpret_cast<u32x2*>(o + p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+            *reinterpret_cast<u32x4*>(o + p) = x;
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (p + e < a.np) o[p + e] = to_bf16(v[e]);
+            for (int e = 0; e < 8; ++e)
+              if (p + e < a.np) o[p + e] = (uint16_t)(x[e >> 1] >> (e & 1) * 16);
           }
         }
       }
@@ -430,21 +457,21 @@ template <bool PTR, bool QTR, int EPI>
 hipError_t launch_tile(const TileArgs& a, int64_t nq, int shape, hipStream_t st) {
   const int64_t tp = (a.np + tile_p(shape) - 1) / tile_p(shape);
   const int64_t tq = (nq + tile_q(shape) - 1) / tile_q(shape);
-  const int64_t tiles = tp * tq * (EPI == kSlab ? a.splits : 1);
+  int64_t tiles = tp * tq;
   if (tiles <= 0) return hipSuccess;
-  if (tiles > (int64_t)1 << 30) return hipErrorInvalidValue;
-  // as many as the chip holds at a time, by LDS
-  const int64_t fit = 256 * (shape == kTile256 ? 1 : shape == kTile128 ? 2 : shape == kTile64 ? 3 : 4);
+  if (tiles > (int64_t)1 << 24) return hipErrorInvalidValue;
+  const int64_t fit = tile_fit(shape);
+  if (EPI == kSlab) tiles = fit;   // fewer live rows, more splits
   const dim3 g((unsigned)(((tiles < fit ? tiles : fit) + kXcds - 1) / kXcds * kXcds));
   switch (shape) {
-    case kTile256: k_tile<2, 4, 8, 4, PTR, QTR, EPI><<<g, 512, 0, st>>>(a); break;
-    case kTile128: k_tile<2, 2, 4, 4, PTR, QTR, EPI><<<g, 256, 0, st>>>(a); break;
+    case kTile256: k_tile<2, 4, 8, 4, PTR, QTR, EPI, 256><<<g, 512, 0, st>>>(a); break;
+    case kTile128: k_tile<2, 2, 4, 4, PTR, QTR, EPI, 512><<<g, 256, 0, st>>>(a); break;
     case kTile64:
-      if constexpr (EPI != kOut) k_tile<4, 1, 2, 4, PTR, QTR, EPI><<<g, 256, 0, st>>>(a);
+      if constexpr (EPI != kOut) k_tile<4, 1, 2, 4, PTR, QTR, EPI, 768><<<g, 256, 0, st>>>(a);
       else return hipErrorInvalidValue;
       break;
     default:
-      if constexpr (EPI == kStats) k_tile<4, 1, 2, 1, PTR, QTR, EPI><<<g, 256, 0, st>>>(a);
+      if constexpr (EPI == kStats) k_tile<4, 1, 2, 1, PTR, QTR, EPI, 1024><<<g, 256, 0, st>>>(a);
       else return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -741,16 +768,21 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
 
 // The gradient of the hidden state from the splits' fp32 sums, added in order.
 __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab, int64_t ld_slab,
-                                            int64_t slab_stride, int splits, float out_scale) {
+                                            int bp, int bq, int fit, int max_splits,
+                                            float out_scale) {
   const unsigned blocks = (unsigned)((a.D + 1023) / 1024);
   const int64_t q = blockIdx.x / blocks;
-  if (q >= a.hdr->n_live) return;
+  const int64_t n = a.hdr->n_live;
+  if (q >= n) return;
   const int64_t d = ((int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x) * 4;
   if (d >= a.D) return;
+  const int splits =
+      splits_of(fit, (int)((a.D + bp - 1) / bp) * (int)((n + bq - 1) / bq), max_splits);
   const float f = a.hdr->scale * out_scale;
   const float* p = slab + q * ld_slab + d;
   f32x4 s = *reinterpret_cast<const f32x4*>(p);
-  for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4*>(p + i * slab_stride);
+#pragma unroll 4
+  for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4*>(p + i * (n * ld_slab));
   s *= f;
   uint16_t* o = a.dhidden + (int64_t)a.rows[q] * a.D + d;
   if (((a.D & 3) | (reinterpret_cast<uintptr_t>(a.dhidden) & 7)) == 0) {
@@ -792,10 +824,11 @@ hipError_t launch_head_fix(const HeadArgs& a, uint16_t* G, int64_t ldg, int64_t 
   k_fix<<<(unsigned)((a.T + 3) / 4), 256, 0, st>>>(a, G, ldg, v0, v1);
   return hipGetLastError();
 }
-hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab,
-                          int64_t slab_stride, int splits, float out_scale, hipStream_t st) {
+hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab, int shape,
+                          int max_splits, float out_scale, hipStream_t st) {
   const unsigned blocks = (unsigned)((a.D + 1023) / 1024);
-  k_dh<<<blocks * (unsigned)a.T, 256, 0, st>>>(a, slab, ld_slab, slab_stride, splits, out_scale);
+  k_dh<<<blocks * (unsigned)a.T, 256, 0, st>>>(a, slab, ld_slab, tile_p(shape), tile_q(shape),
+                                               tile_fit(shape), max_splits, out_scale);
   return hipGetLastError();
 }
 hipError_t launch_logits_stats(const TileArgs& a, int shape, hipStream_t st) {

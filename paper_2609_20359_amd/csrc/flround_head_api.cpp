@@ -46,7 +46,8 @@ struct Plan {
   int K;
   bool grad, distill, pack_w;
   int logits_shape, dh_shape, dw_shape;
-  int n_parts, splits;
+  int n_parts, max_splits;
+  int64_t slab_rows;
   int64_t piece, n_pieces;
   // byte offsets into the workspace
   size_t hdr, rows, pos, logp, mass, flag, hc, wc, parts, row_lse2, row_coef, G, slab, bytes;
@@ -72,13 +73,15 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   p.logits_shape = shape_for(p.piece, p.T, true);
   if (grad && p.logits_shape == kTile16) p.logits_shape = kTile64;   // G is read 64 rows at a time
   p.n_parts = (int)(ceil_div(p.V, tile_p(p.logits_shape)) * tile_parts(p.logits_shape));
-  p.dh_shape = p.T <= 64 ? (int)kTile64 : shape_for(p.D, p.T, false);
+  p.dh_shape = p.T <= 64 ? kTile64 : p.T <= 128 ? kTile128 : kTile256;
   p.dw_shape = shape_for(p.D, p.piece, false);
   // The sum over a piece is split where the outputs are too few tiles to fill
-  // the chip, four steps at least to a split.
-  const int64_t dh_tiles = std::max<int64_t>(1, tiles_of(p.dh_shape, p.D, p.T));
-  const int64_t want = (p.dh_shape == kTile256 ? 1 : p.dh_shape == kTile128 ? 2 : 3) * kCus / dh_tiles;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, ceil_div(p.piece, kStep) / 4, 64}));
+  // the chip, four steps at least to a split.  How many tiles there are depends
+  // on the live rows, and the rows of all splits are at most the chip's share.
+  p.max_splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(p.piece, kStep) / 4, 64));
+  p.slab_rows = std::max(p.T, tile_fit(p.dh_shape) * tile_q(p.dh_shape) /
+                                  ceil_div(p.D, tile_p(p.dh_shape)));
+  p.slab_rows = std::min(p.slab_rows, p.T * p.max_splits);
 
   size_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -100,7 +103,7 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
     p.row_lse2 = take(4 * p.rows_pad);
     p.row_coef = take(4 * p.rows_pad);
     p.G = take(2 * p.rows_pad * round_up(p.piece, 256));
-    p.slab = take(4 * (int64_t)p.splits * p.T * p.Dp);
+    p.slab = take(4 * p.slab_rows * p.Dp);
   } else {
     p.parts = take(8 * (int64_t)p.n_parts * p.rows_pad);
   }
@@ -209,7 +212,6 @@ struct Call {
     g.np = v1 - v0, g.nq = p.T, g.nk = a.wc ? p.Dp : p.D;
     g.hdr = a.hdr, g.live_q = 1, g.zero = reinterpret_cast<const uint16_t*>(a.hdr->zero);
     g.s2 = (float)(1.4426950408889634 / (double)a.tau);
-    g.splits = 1;
     return g;
   }
 };
@@ -277,7 +279,7 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
     w.np = p.D, w.nq = v1 - v0, w.live_k = 1;
     w.hdr = c.a.hdr, w.zero = reinterpret_cast<const uint16_t*>(c.a.hdr->zero);
     w.out = dweight + v0 * p.D, w.ld_out = p.D;
-    w.vec_out = (p.D & 3) == 0 && (reinterpret_cast<uintptr_t>(dweight) & 7) == 0;
+    w.vec_out = (p.D & 7) == 0 && (reinterpret_cast<uintptr_t>(dweight) & 15) == 0;
     w.out_scale = out_scale;
     if ((rc = status_of(launch_dweight(w, p.dw_shape, c.st))) != FL_OK) return rc;
     if (p.T > 0) {
@@ -286,13 +288,13 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
       h.Q = G, h.ldq = ldg;
       h.np = p.D, h.nq = p.T, h.live_q = 1, h.nk = v1 - v0;
       h.hdr = c.a.hdr, h.zero = reinterpret_cast<const uint16_t*>(c.a.hdr->zero);
-      h.slab = slab, h.ld_slab = p.Dp, h.slab_stride = p.T * p.Dp;
-      h.add = v0 > 0, h.splits = p.splits;
+      h.slab = slab, h.ld_slab = p.Dp;
+      h.add = v0 > 0, h.max_splits = p.max_splits;
       if ((rc = status_of(launch_dhidden(h, p.dh_shape, c.st))) != FL_OK) return rc;
     }
   }
   if (p.T == 0) return FL_OK;
-  return status_of(launch_head_dh(c.a, slab, p.Dp, p.T * p.Dp, p.splits, out_scale, c.st));
+  return status_of(launch_head_dh(c.a, slab, p.Dp, p.dh_shape, p.max_splits, out_scale, c.st));
 }
 
 // Segments of a row of top logits: the whole row, or as much of it as keeps
