@@ -73,7 +73,9 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   p.logits_shape = shape_for(p.piece, p.T, true);
   if (grad && p.logits_shape == kTile16) p.logits_shape = kTile64;   // G is read 64 rows at a time
   p.n_parts = (int)(ceil_div(p.V, tile_p(p.logits_shape)) * tile_parts(p.logits_shape));
-  p.dh_shape = p.T <= 64 ? kTile64 : p.T <= 128 ? kTile128 : kTile256;
+  // Large tiles where there are enough of them, with eight steps each.
+  p.dh_shape = p.T <= 64 ? kTile64
+               : tiles_of(kTile256, p.D, p.T) * (p.piece / (8 * kStep)) >= kCus ? kTile256 : kTile128;
   p.dw_shape = shape_for(p.D, p.piece, false);
   // The sum over a piece is split where the outputs are too few tiles to fill
   // the chip, four steps at least to a split.  How many tiles there are depends

@@ -2,19 +2,21 @@
 // row with their ids, and the logarithm of the sum of exp(x / tau).
 //
 // One pass over the logits, bound by HBM.  A workgroup of 512 threads takes a
-// segment of a row into registers, so that nothing is read twice:
+// segment of a row into registers:
 //   * the maxima of its 512 threads give a lower bound on the k-th largest (k
 //     threads' maxima are at least their k-th largest), found by bisecting the
 //     leading 16 bits;
-//   * what is not below the bound, a few more than k as a rule, goes to a list
-//     in LDS; where it would not fit (a row of equal values), the exact k-th
-//     largest is found by bisecting (value, id) over the registers;
+//   * the 16-byte chunks whose largest value is not below the bound, a few more
+//     than k as a rule, are listed in LDS; their values are read again, from L2,
+//     and those not below the bound go to a second list; where it would not
+//     fit (a row of equal values), the exact k-th largest is found by bisecting
+//     (value, id);
 //   * a list entry's place is the number of entries above it.
 // Rows longer than a segment are joined by a second kernel, in which an entry's
 // place is the sum of its places in the segments' sorted lists.
 //
 // The order is that of one 64-bit number: the value, then the lower id; so ties
-// go to the lowest id and no result depends on the order of the list.
+// go to the lowest id and no result depends on the order of the lists.
 #include "flr_head.h"
 
 namespace flr {
@@ -36,7 +38,7 @@ __device__ __forceinline__ float value_of(uint32_t k) {
   const int32_t b = (int32_t)(k ^ 0x80000000u);
   return k == 0xFFFFFFFFu ? NAN : __uint_as_float((uint32_t)(b ^ ((b >> 31) & 0x7FFFFFFF)));
 }
-__device__ __forceinline__ uint64_t entry(float x, int64_t id) {
+__device__ __forceinline__ uint64_t entry(float x, int id) {
   return (uint64_t)key_of(x) << 32 | (0xFFFFFFFFu - (uint32_t)id);
 }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -65,43 +67,40 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
   constexpr int E = BF16 ? 8 : 4;        // elements of a chunk
   constexpr int ES = BF16 ? 2 : 4;
   __shared__ uint64_t list[kList];
+  __shared__ uint16_t chunks[kThreads * NC];
   __shared__ uint32_t maxima[kThreads];
   __shared__ float wave_m[kWaves], wave_s[kWaves];
   __shared__ int counts[2][kWaves];
-  __shared__ int n_list;
+  __shared__ int n_list, n_chunks;
   __shared__ float bound;
 
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
   const int64_t row = blockIdx.x / a.segs;
   const int seg = (int)(blockIdx.x % a.segs);
+  const int vocab = (int)a.vocab;
   // chunks are counted from the 16-byte boundary at or before the row
   const char* src = static_cast<const char*>(a.logits) + row * a.stride * ES;
   const int head = (int)(reinterpret_cast<uintptr_t>(src) & 15) / ES;
-  const int64_t first = ((int64_t)seg * kThreads * NC + tid) * E - head;   // id of chunk 0's first
+  const int first = seg * kThreads * NC * E - head;   // id of the segment's first
+  auto element = [&](int id) -> float {
+    return BF16 ? __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(src + (int64_t)id * 2) << 16)
+                : *reinterpret_cast<const float*>(src + (int64_t)id * 4);
+  };
 
   u32x4 d[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const int64_t id = first + (int64_t)c * kThreads * E;
-    // what is not there reads as -inf and is told apart by its id
-    if (id >= 0 && id + E <= a.vocab) {
-      d[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + id * ES));
+    const int id = first + (c * kThreads + tid) * E;
+    if (id >= 0 && id + E <= vocab) {
+      d[c] = *reinterpret_cast<const u32x4*>(src + (int64_t)id * ES);
     } else {
+      // what is not there reads as -inf, and is told apart by its id
+      uint32_t x[E];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (BF16) {
-          uint32_t x[2];
+      for (int e = 0; e < E; ++e)
+        x[e] = id + e >= 0 && id + e < vocab ? __float_as_uint(element(id + e)) : 0xFF800000u;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int64_t j = id + 2 * i + h;
-            x[h] = j >= 0 && j < a.vocab ? *reinterpret_cast<const uint16_t*>(src + j * 2) : 0xFF80u;
-          }
-          d[c][i] = x[0] | x[1] << 16;
-        } else {
-          const int64_t j = id + i;
-          d[c][i] = j >= 0 && j < a.vocab ? *reinterpret_cast<const uint32_t*>(src + j * 4) : 0xFF800000u;
-        }
-      }
+      for (int i = 0; i < 4; ++i) d[c][i] = BF16 ? x[2 * i] >> 16 | x[2 * i + 1] : x[i];
     }
   }
   auto value = [&](int c, int e) -> float {
@@ -110,13 +109,16 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
     return __uint_as_float(e & 1 ? u & 0xFFFF0000u : u << 16);
   };
 
-  float top = -INFINITY;
+  float top = -INFINITY, tops[NC];
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int c = 0; c < NC; ++c) {
+    tops[c] = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = fmaxf(top, value(c, e));
+    for (int e = 0; e < E; ++e) tops[c] = fmaxf(tops[c], value(c, e));
+    top = fmaxf(top, tops[c]);
+  }
   maxima[tid] = key_of(top) >> 16;
-  if (tid == 0) n_list = 0;
+  if (tid == 0) n_list = n_chunks = 0;
   float m = top;
 #pragma unroll
   for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
@@ -137,82 +139,78 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
     }
     // the least value whose key starts with these bits; as a float it may be a
     // NaN's pattern below -inf, where nothing is below the bound
-    const float b = value_of(t << 16);
-    if (l == 0) bound = t <= 0x007Fu ? -INFINITY : b;
+    if (l == 0) bound = t <= 0x007Fu ? -INFINITY : value_of(t << 16);
   }
   m = wave_m[0];
 #pragma unroll
   for (int i = 1; i < kWaves; ++i) m = fmaxf(m, wave_m[i]);
-  const float ref = m == -INFINITY ? 0.f : m;
   float s = 0.f;
+  const float ref = m == -INFINITY ? 0.f : m, ref2 = ref * a.s2;
+  const bool overflow = !(fabsf(ref2) < INFINITY);   // of the scaled maximum
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int c = 0; c < NC; ++c) {
+    // The values are taken from the registers anew: kept, they would be twice
+    // as many, and fewer waves would cover the loads.
+    asm volatile("" : "+v"(d[c]));
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += exp2_((value(c, e) - ref) * a.s2);
+    for (int e = 0; e < E; ++e)
+      s += exp2_(overflow ? (value(c, e) - ref) * a.s2 : __builtin_fmaf(value(c, e), a.s2, -ref2));
+  }
+  const bool odd = s != s;   // a NaN among them, or infinities: no chunk is left out
 #pragma unroll
   for (int x = 32; x; x >>= 1) s += __shfl_xor(s, x);
   if (l == 0) wave_s[w] = s;
   __syncthreads();
 
-  // how many are not below the bound
   const float b = bound;
-  const bool whole = first >= 0 && first + (int64_t)(NC - 1) * kThreads * E + E <= a.vocab;
-  auto there = [&](int c, int e) {
-    const int64_t id = first + (int64_t)c * kThreads * E + e;
-    return id >= 0 && id < a.vocab;
-  };
-  int n = 0;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int e = 0; e < E; ++e) n += !(value(c, e) < b);
-  if (!whole && n) {
-    n = 0;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int e = 0; e < E; ++e) n += !(value(c, e) < b) && there(c, e);
-  }
-  auto total = [&](int mine, int par) {
-#pragma unroll
-    for (int x = 32; x; x >>= 1) mine += __shfl_xor(mine, x);
-    if (l == 0) counts[par][w] = mine;
-    __syncthreads();
-    int t = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) t += counts[par][i];
-    return t;
+    if (odd || !(tops[c] < b)) chunks[atomicAdd(&n_chunks, 1)] = (uint16_t)(c * kThreads + tid);
+  __syncthreads();
+  auto each_above = [&](auto f) {
+    const int n = n_chunks * E;
+    for (int i = tid; i < n; i += kThreads) {
+      const int id = first + chunks[i / E] * E + i % E;
+      if (id < 0 || id >= vocab) continue;
+      const float x = element(id);
+      if (!(x < b)) f(entry(x, id));
+    }
   };
-  int all = total(n, 0);
-  uint64_t least = 0;
+  each_above([&](uint64_t x) {
+    const int at = atomicAdd(&n_list, 1);
+    if (at < kList) list[at] = x;
+  });
+  __syncthreads();
+  int all = n_list;
   if (all > kList) {
-    // the k-th largest entry itself: the largest x that k entries reach
+    // The k-th largest entry itself: the largest number that k entries reach.
+    // Ids are below 2^20, so an entry's bits 31 to 20 are ones.
+    uint64_t least = 0;
     for (int bit = 63; bit >= 0; --bit) {
+      if (bit == 31) {
+        least |= 0xFFF00000u;
+        bit = 19;
+      }
       const uint64_t x = least | (uint64_t)1 << bit;
       int r = 0;
-      if (n) {
+      each_above([&](uint64_t y) { r += y >= x; });
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+      for (int i = 32; i; i >>= 1) r += __shfl_xor(r, i);
+      if (l == 0) counts[bit & 1][w] = r;
+      __syncthreads();
+      r = 0;
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            r += there(c, e) && entry(value(c, e), first + (int64_t)c * kThreads * E + e) >= x;
-      }
-      if (total(r, (bit & 1)) >= a.k) least = x;
+      for (int i = 0; i < kWaves; ++i) r += counts[bit & 1][i];
+      if (r >= a.k) least = x;
     }
-    // counts[] is not read again before the next barrier
+    if (tid == 0) n_list = 0;
+    __syncthreads();
+    each_above([&](uint64_t x) {
+      if (x >= least) list[atomicAdd(&n_list, 1)] = x;
+    });
+    __syncthreads();
     all = a.k;
   }
-  if (n) {
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (!(value(c, e) < b) && there(c, e)) {
-          const uint64_t x = entry(value(c, e), first + (int64_t)c * kThreads * E + e);
-          if (x >= least) list[atomicAdd(&n_list, 1)] = x;
-        }
-  }
-  __syncthreads();
   const bool last = a.segs == 1;
   uint64_t* out = last ? nullptr : a.lists + (row * a.segs + seg) * a.k;
   for (int i = tid; i < all; i += kThreads) {
