@@ -119,7 +119,7 @@ hipError_t launch_dweight(const TileArgs& a, int shape, hipStream_t st);
 // Top logits.
 constexpr int kTopThreads = 512;
 constexpr int kTopMaxChunks = 8;        // 16-byte chunks per thread
-constexpr int64_t kTopMaxEntries = 8192; // of a row's segment lists, held in LDS
+constexpr int64_t kTopMaxEntries = 8192; // of a row's segment lists where shorter segments are chosen (65 x 128 at most)
 
 struct TopArgs {
   const void* logits;

@@ -27,6 +27,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kThreads = kTopThreads;
 constexpr int kWaves = kThreads / 64;
+constexpr int kJoinThreads = 512;
 constexpr int kList = 2048;   // entries of the list in LDS
 
 // Larger floats have larger keys, NaN the largest, and -0 that of +0.
@@ -232,32 +233,24 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
   }
 }
 
-// Joins a row's segments.
-__global__ __launch_bounds__(256) void k_top_join(const TopArgs a) {
-  extern __shared__ uint64_t lists[];
+// Joins a row's segments.  The least of the segments' ceil(k / segs)-th entries
+// has k entries at or above it, so only those, a few more than k, are placed:
+// an entry's place is how many of its own segment and of the others, by
+// bisection, are above it.
+__global__ __launch_bounds__(kJoinThreads) void k_top_join(const TopArgs a) {
+  extern __shared__ uint64_t lists[];   // segs x k entries, then places and numbers of the kept
+  __shared__ int n_kept;
   const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
   const int n = a.segs * a.k;
-  for (int i = tid; i < n; i += 256) lists[i] = a.lists[row * n + i];
-  __syncthreads();
-  for (int i = tid; i < n; i += 256) {
-    const uint64_t x = lists[i];
-    if (x == 0) continue;
-    const int own = i / a.k;
-    int place = i - own * a.k;
-    for (int g = 0; g < a.segs && place < a.k; ++g) {
-      if (g == own) continue;
-      const uint64_t* p = lists + g * a.k;
-      int lo = 0, hi = a.k;   // how many of p are above x
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (p[mid] > x) lo = mid + 1;
-        else hi = mid;
-      }
-      place += lo;
-    }
-    if (place < a.k) emit(a, row, place, x);
+  int* place = reinterpret_cast<int*>(lists + n);
+  uint16_t* kept = reinterpret_cast<uint16_t*>(place + n);
+  for (int i = tid; i < n; i += kJoinThreads) {
+    lists[i] = a.lists[row * n + i];
+    place[i] = 0;
   }
+  if (tid == 0) n_kept = 0;
+  __syncthreads();
   if (a.lse && tid < 64) {
     float m = -INFINITY, s = 0.f;
     for (int g = tid; g < a.segs; g += 64) {
@@ -267,6 +260,33 @@ __global__ __launch_bounds__(256) void k_top_join(const TopArgs a) {
 #pragma unroll
     for (int x = 32; x; x >>= 1) join(m, s, __shfl_xor(m, x), __shfl_xor(s, x), a.s2);
     if (tid == 0) a.lse[row] = lse_of(m, s, a);
+  }
+  const int share = (a.k + a.segs - 1) / a.segs;
+  uint64_t least = ~(uint64_t)0;
+  for (int g = 0; g < a.segs; ++g) {
+    const uint64_t x = lists[g * a.k + share - 1];
+    least = x < least ? x : least;
+  }
+  for (int i = tid; i < n; i += kJoinThreads)
+    if (lists[i] != 0 && lists[i] >= least) kept[atomicAdd(&n_kept, 1)] = (uint16_t)i;
+  __syncthreads();
+  const int pairs = n_kept * a.segs;
+  for (int i = tid; i < pairs; i += kJoinThreads) {
+    const int e = kept[i / a.segs], g = i % a.segs;
+    const uint64_t x = lists[e];
+    const uint64_t* p = lists + g * a.k;
+    int lo = 0, hi = a.k;   // how many of p are above x
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (p[mid] > x) lo = mid + 1;
+      else hi = mid;
+    }
+    if (lo) atomicAdd(&place[e], lo);
+  }
+  __syncthreads();
+  for (int i = tid; i < n_kept; i += kJoinThreads) {
+    const int e = kept[i];
+    if (place[e] < a.k) emit(a, row, place[e], lists[e]);
   }
 }
 
@@ -287,7 +307,7 @@ hipError_t launch_top(const TopArgs& a, hipStream_t st) {
   if (a.bf16) launch_segment<true>(a, grid, st);
   else launch_segment<false>(a, grid, st);
   if (const hipError_t e = hipGetLastError()) return e;
-  if (a.segs > 1) k_top_join<<<(unsigned)a.rows, 256, (size_t)a.segs * a.k * 8, st>>>(a);
+  if (a.segs > 1) k_top_join<<<(unsigned)a.rows, kJoinThreads, (size_t)a.segs * a.k * 14, st>>>(a);
   return hipGetLastError();
 }
 
