@@ -51,6 +51,8 @@ struct HeadArgs {
   uint16_t* wc;                     // weight rows of Dp each, or null: weight is used as it is
   float* row_lse2;                  // gradient, per live row: lse * log2(e)
   float* row_coef;                  // gradient, per live row: dloss / scale * mass
+  int32_t* row_label;               // gradient of the labels' loss, per live row: the label,
+  float* row_spot;                  // and its entry of G
   const float2* parts;              // per (part, live row): running maximum and sum
   int n_parts;
   int64_t rows_pad;                 // T rounded up to kRowPad
@@ -74,6 +76,9 @@ struct TileArgs {
   int64_t parts_ld;
   const float* row_lse2;            // gradient of the logits
   const float* row_coef;
+  const int32_t* row_label;         // or null
+  const float* row_spot;
+  int64_t p_first;                  // the word that p = 0 is
   uint16_t* G;
   int64_t ldg;                      // also the columns of G to write
   float* slab;                      // fp32 sums: slab[split][live row][ld_slab]
@@ -89,8 +94,6 @@ struct TileArgs {
 enum TileShape { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile16 = 3 };
 inline int tile_p(int s) { return s == kTile256 ? 256 : 128; }
 inline int tile_q(int s) { return s == kTile256 ? 256 : s == kTile128 ? 128 : s == kTile64 ? 64 : 16; }
-// Rows of statistics that a tile of shape s writes per p tile.
-inline int tile_parts(int s) { return s == kTile256 || s == kTile128 ? 2 : 4; }
 
 inline int tile_fit(int s) {   // tiles that the chip holds at a time, by LDS
   return 256 * (s == kTile256 ? 1 : s == kTile128 ? 2 : s == kTile64 ? 3 : 4);
@@ -103,7 +106,7 @@ __host__ __device__ inline int splits_of(int fit, int tiles, int max_splits) {
 }
 
 hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st);
-hipError_t launch_head_live(const HeadArgs& a, hipStream_t st);
+// The live tokens and their rows.
 hipError_t launch_head_pack(const HeadArgs& a, bool grad, hipStream_t st);
 hipError_t launch_head_pack_weight(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_finish(const HeadArgs& a, hipStream_t st);

@@ -44,6 +44,13 @@ __device__ __forceinline__ uint16_t to_bf16(float x) { return (uint16_t)pack2(x,
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
+// (m, s) stands for s 2^m; a part of nothing is (-inf, 0).
+__device__ __forceinline__ void join(float& m, float& s, float pm, float ps) {
+  const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
+  s = s * exp2_(m - ref) + ps * exp2_(pm - ref);
+  m = top;
+}
+
 // ---- the tiled product ------------------------------------------------------
 //
 // A workgroup makes BP x BQ outputs, kStep of the summed axis at a time, from
@@ -213,6 +220,8 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
   __shared__ __attribute__((aligned(128))) char sm0[OpP::kBytes + OpQ::kBytes];
   __shared__ __attribute__((aligned(128))) char sm1[OpP::kBytes + OpQ::kBytes];
 
+  __shared__ float2 folded[EPI == kStats ? WP : 1][EPI == kStats ? BQ : 1];
+
   const int tid = threadIdx.x, l = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wp = w % WP, wq = w / WP;
@@ -338,7 +347,7 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
     }
     const int my_split = split;
     const int64_t p0 = (int64_t)tp * BP, q0 = (int64_t)tq * BQ;
-    const int my_part = tp * WP + wp;
+    const int my_tp = tp;
     // after the last tile: its own first steps again, which nothing reads
     const bool more = id + stride < end;
     aim(more ? id + stride : id);
@@ -378,7 +387,15 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
           for (int e = 0; e < 4; ++e) sum += exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -ref));
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (l < 16) a.parts[(int64_t)my_part * a.parts_ld + qw + j * 16] = make_float2(m, sum);
+        if (l < 16) folded[wp][(wq * FQ + j) * 16 + l] = make_float2(m, sum);
+      }
+      __syncthreads();
+      // (The next write here is a tile's steps and their meetings away.)
+      if (tid < BQ) {
+        float2 p = folded[0][tid];
+#pragma unroll
+        for (int i = 1; i < WP; ++i) join(p.x, p.y, folded[i][tid].x, folded[i][tid].y);
+        a.parts[(int64_t)my_tp * a.parts_ld + q0 + tid] = p;
       }
     } else if constexpr (EPI == kGrad) {
       const bool edge = p0 + BP > a.np;
@@ -387,21 +404,33 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
         const int64_t q = qw + j * 16;
         const bool live = q < n_live;
         const float lse2 = live ? a.row_lse2[q] : 0.f, coef = live ? a.row_coef[q] : 0.f;
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = coef * exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -lse2));
+            acc[i][j][e] = !live || (edge && pw + i * 16 + e >= a.np) ? 0.f : v;
+          }
+        if (a.row_label) {
+          // the label's entry, where one of the wave's rows has it among these
+          const int64_t y = live ? a.row_label[q] - a.p_first - pw : -1;
+          const bool here = y >= 0 && y < FP * 16 && (y & 12) == 0;
+          if (__any(here)) {
+            const float spot = here ? a.row_spot[q] : 0.f;
+#pragma unroll
+            for (int i = 0; i < FP; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (here && y == i * 16 + e) acc[i][j][e] = spot;
+          }
+        }
         uint16_t* g = a.G + q * a.ldg + p0 + wp * FP * 16 + (l >> 4) * 8;
 #pragma unroll
         for (int i = 0; i < FP; i += 2) {
-          u32x2 d[2];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              v[e] = coef * exp2_(__builtin_fmaf(acc[i + h][j][e], a.s2, -lse2));
-              if (!live || (edge && pw + (i + h) * 16 + e >= a.np)) v[e] = 0.f;
-            }
-            d[h] = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
-          }
-          *reinterpret_cast<u32x4*>(g + i * 16) = eight(d[0], d[1]);
+          const f32x4 x = acc[i][j], y = acc[i + 1][j];
+          *reinterpret_cast<u32x4*>(g + i * 16) =
+              eight(u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])},
+                    u32x2{pack2(y[0], y[1]), pack2(y[2], y[3])});
         }
       }
     } else if constexpr (EPI == kSlab) {
@@ -581,25 +610,66 @@ __global__ __launch_bounds__(1024) void k_live(const HeadArgs a) {
 __device__ __forceinline__ bool aligned_rows(const uint16_t* p, int64_t ld, int64_t D) {
   return ((reinterpret_cast<uintptr_t>(p) & 15) | (ld & 7) | (D & 7)) == 0;
 }
+__device__ __forceinline__ bool is_live(const HeadArgs& a, int64_t t) {
+  return a.labels ? a.labels[t] >= 0 : a.flag[t] != 0;
+}
 
 // Copies the live tokens' rows to consecutive ones, padded with zeros to Dp
 // and, past the last, to whole tiles of rows.  Forward: also the products with
 // the listed words' rows of the weight (a wave per listed word), and zeros as
 // the results of the other tokens.  Gradient: also the coefficients of the
-// rows, and zeros as the other tokens' gradient.
-template <bool GRAD>
+// rows, and zeros as the other tokens' gradient.  SCAN: of up to kScan tokens
+// every workgroup finds by itself what k_live finds of more.
+constexpr int kScan = 1024;
+
+template <bool GRAD, bool SCAN>
 __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
+  __shared__ int before_[4], all_[4];
+  __shared__ float top_[4];
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
-  int64_t t = blockIdx.x;
+  const int64_t t = blockIdx.x;
   const u32x4 zero = {0, 0, 0, 0};
+  int n;
+  int64_t q;
+  float scale;
+  if (SCAN) {
+    int before = 0, all = 0;
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < kScan / 256; ++i) {
+      const int64_t u = i * 256 + tid;
+      const bool on = u < a.T && is_live(a, u);
+      all += __popcll(__ballot(on));
+      before += __popcll(__ballot(on && u < t));
+      if (GRAD && on) {
+        const float d = fabsf(a.dloss[u]);
+        if (d < INFINITY) top = fmaxf(top, d);
+      }
+    }
+    if (GRAD) top = wave_max(top);
+    if (l == 0) before_[w] = before, all_[w] = all, top_[w] = top;
+    __syncthreads();
+    n = all_[0] + all_[1] + all_[2] + all_[3];
+    top = fmaxf(fmaxf(top_[0], top_[1]), fmaxf(top_[2], top_[3]));
+    scale = top > 0.f ? top : 1.f;
+    q = t < a.T && is_live(a, t) ? before_[0] + before_[1] + before_[2] + before_[3] : -1;
+    if (tid == 0 && q >= 0) a.rows[q] = (int32_t)t;
+    if (tid == 0 && t == a.T) {
+      a.hdr->n_live = n;
+      a.hdr->scale = scale;
+      for (int i = 0; i < 4; ++i) a.hdr->zero[i] = 0;
+    }
+  } else {
+    n = a.hdr->n_live;
+    scale = a.hdr->scale;
+    q = t < a.T ? a.pos[t] : -1;
+  }
   if (t >= a.T) {
-    const int n = a.hdr->n_live;
-    const int64_t q = n + (t - a.T);
-    if (q >= (n + kRowPad - 1) / kRowPad * kRowPad) return;
-    for (int64_t d = tid * 8; d < a.Dp; d += 2048) *reinterpret_cast<u32x4*>(a.hc + q * a.Dp + d) = zero;
+    const int64_t r = n + (t - a.T);
+    if (r >= (int64_t)(n + kRowPad - 1) / kRowPad * kRowPad) return;
+    for (int64_t d = tid * 8; d < a.Dp; d += 2048) *reinterpret_cast<u32x4*>(a.hc + r * a.Dp + d) = zero;
     return;
   }
-  const int64_t q = a.pos[t];
   if (q < 0) {
     if (GRAD) {
       for (int64_t d = tid; d < a.D; d += 256) a.dhidden[t * a.D + d] = 0;
@@ -620,9 +690,16 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
   }
   if (GRAD) {
     if (tid == 0) {
-      const float mass = a.labels ? (a.labels[t] < a.V ? 1.f : NAN) : a.mass[t];
-      a.row_lse2[q] = a.lse_in[t] * kLog2e;
-      a.row_coef[q] = a.dloss[t] / a.hdr->scale * mass;
+      const float ratio = a.dloss[t] / scale, lse = a.lse_in[t];
+      a.row_lse2[q] = lse * kLog2e;
+      if (a.labels) {
+        const int64_t y = a.labels[t];
+        a.row_coef[q] = y < a.V ? ratio : NAN;
+        a.row_label[q] = y < a.V ? (int32_t)y : -1;
+        a.row_spot[q] = ratio * (exp2_((a.target_in[t] - lse) * kLog2e) - 1.f);
+      } else {
+        a.row_coef[q] = ratio * a.mass[t];
+      }
     }
     return;
   }
@@ -673,34 +750,39 @@ __global__ __launch_bounds__(256) void k_pack_weight(const HeadArgs a) {
   }
 }
 
-// lse and loss of 16 live rows: 64 threads fold a row's parts, then a wave
+// lse and loss of C live rows: 1024 / C threads fold a row's parts, then a wave
 // sums over its listed words.
+template <int C>
 __global__ __launch_bounds__(1024) void k_finish(const HeadArgs a) {
-  __shared__ float ms[16][17], ss[16][17];
+  __shared__ float ms[C][17], ss[C][17];
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
   const int n = a.hdr->n_live;
-  const int64_t q0 = (int64_t)blockIdx.x * 16;
+  const int64_t q0 = (int64_t)blockIdx.x * C;
   if (q0 >= n) return;
-  const int c = tid & 15;
+  const int c = tid % C;
   float m = -INFINITY, s = 0.f;
-  // (m, s) stands for s 2^m; a part of nothing is (-inf, 0)
-  auto join = [](float& m, float& s, float pm, float ps) {
-    const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
-    s = s * exp2_(m - ref) + ps * exp2_(pm - ref);
-    m = top;
-  };
-  if (q0 + c < n)
-    for (int i = tid >> 4; i < a.n_parts; i += 64) {
-      const float2 p = a.parts[(int64_t)i * a.rows_pad + q0 + c];
-      join(m, s, p.x, p.y);
+  if (q0 + c < n) {
+    const float2* p = a.parts + q0 + c;
+    int i = tid / C;
+    for (; i + 3 * (1024 / C) < a.n_parts; i += 4 * (1024 / C)) {
+      float2 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = p[(int64_t)(i + k * (1024 / C)) * a.rows_pad];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) join(m, s, x[k].x, x[k].y);
     }
-  join(m, s, __shfl_xor(m, 16), __shfl_xor(s, 16));
-  join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32));
-  if (l < 16) ms[w][l] = m, ss[w][l] = s;
+    for (; i < a.n_parts; i += 1024 / C) {
+      const float2 x = p[(int64_t)i * a.rows_pad];
+      join(m, s, x.x, x.y);
+    }
+  }
+#pragma unroll
+  for (int d = C; d < 64; d <<= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  if (l < C) ms[l][w] = m, ss[l][w] = s;
   __syncthreads();
-  if (q0 + w >= n) return;
-  m = l < 16 ? ms[l][w] : -INFINITY;
-  s = l < 16 ? ss[l][w] : 0.f;
+  if (w >= C || q0 + w >= n) return;
+  m = l < 16 ? ms[w][l] : -INFINITY;
+  s = l < 16 ? ss[w][l] : 0.f;
 #pragma unroll
   for (int d = 8; d; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
   m = __shfl(m, 0);
@@ -726,7 +808,7 @@ __global__ __launch_bounds__(1024) void k_finish(const HeadArgs a) {
   }
 }
 
-// G at the listed words [v0, v1), a wave per live row: the tile's epilogue left
+// Distillation: G at the listed words [v0, v1), a wave per live row: the tile's epilogue left
 // the softmax's share there in bf16; this replaces it by the whole difference,
 // rounded once.  A word that a token lists more than once gets the sum of its
 // probabilities.
@@ -737,12 +819,6 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
   if (q >= a.hdr->n_live) return;
   const int64_t t = a.rows[q];
   const float ratio = a.dloss[t] / a.hdr->scale;
-  if (a.labels) {
-    const int64_t y = a.labels[t];
-    if (l == 0 && y >= v0 && y < v1)
-      G[q * ldg + (y - v0)] = to_bf16(ratio * (exp2_((a.target_in[t] - a.lse_in[t]) * kLog2e) - 1.f));
-    return;
-  }
   const float mass = a.mass[t], lse = a.lse_in[t];
   for (int k0 = 0; k0 < a.K; k0 += 64) {
     const int k = k0 + l;
@@ -800,14 +876,17 @@ hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st) {
   k_teacher<<<(unsigned)((a.T + 3) / 4), 256, 0, st>>>(a);
   return hipGetLastError();
 }
-hipError_t launch_head_live(const HeadArgs& a, hipStream_t st) {
-  k_live<<<1, 1024, 0, st>>>(a);
-  return hipGetLastError();
-}
 hipError_t launch_head_pack(const HeadArgs& a, bool grad, hipStream_t st) {
   const unsigned grid = (unsigned)(a.T + kRowPad);
-  if (grad) k_pack<true><<<grid, 256, 0, st>>>(a);
-  else k_pack<false><<<grid, 256, 0, st>>>(a);
+  if (a.T <= kScan) {
+    if (grad) k_pack<true, true><<<grid, 256, 0, st>>>(a);
+    else k_pack<false, true><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  k_live<<<1, 1024, 0, st>>>(a);
+  if (const hipError_t e = hipGetLastError()) return e;
+  if (grad) k_pack<true, false><<<grid, 256, 0, st>>>(a);
+  else k_pack<false, false><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_head_pack_weight(const HeadArgs& a, hipStream_t st) {
@@ -816,7 +895,9 @@ hipError_t launch_head_pack_weight(const HeadArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_head_finish(const HeadArgs& a, hipStream_t st) {
-  k_finish<<<(unsigned)((a.T + 15) / 16), 1024, 0, st>>>(a);
+  if (a.T == 1) k_finish<1><<<1, 1024, 0, st>>>(a);
+  else if (a.T <= 4) k_finish<4><<<1, 1024, 0, st>>>(a);
+  else k_finish<16><<<(unsigned)((a.T + 15) / 16), 1024, 0, st>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_head_fix(const HeadArgs& a, uint16_t* G, int64_t ldg, int64_t v0, int64_t v1,

@@ -50,7 +50,7 @@ struct Plan {
   int64_t slab_rows;
   int64_t piece, n_pieces;
   // byte offsets into the workspace
-  size_t hdr, rows, pos, logp, mass, flag, hc, wc, parts, row_lse2, row_coef, G, slab, bytes;
+  size_t hdr, rows, pos, logp, mass, flag, hc, wc, parts, row_lse2, row_coef, row_label, row_spot, G, slab, bytes;
 };
 
 Plan plan_for(const fl_head_shape& s, int K, bool grad) {
@@ -72,7 +72,7 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   }
   p.logits_shape = shape_for(p.piece, p.T, true);
   if (grad && p.logits_shape == kTile16) p.logits_shape = kTile64;   // G is read 64 rows at a time
-  p.n_parts = (int)(ceil_div(p.V, tile_p(p.logits_shape)) * tile_parts(p.logits_shape));
+  p.n_parts = (int)ceil_div(p.V, tile_p(p.logits_shape));
   // Large tiles where there are enough of them, with eight steps each.
   p.dh_shape = p.T <= 64 ? kTile64
                : tiles_of(kTile256, p.D, p.T) * (p.piece / (8 * kStep)) >= kCus ? kTile256 : kTile128;
@@ -104,6 +104,8 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   if (grad) {
     p.row_lse2 = take(4 * p.rows_pad);
     p.row_coef = take(4 * p.rows_pad);
+    p.row_label = take(4 * p.rows_pad);
+    p.row_spot = take(4 * p.rows_pad);
     p.G = take(2 * p.rows_pad * round_up(p.piece, 256));
     p.slab = take(4 * p.slab_rows * p.Dp);
   } else {
@@ -185,7 +187,10 @@ struct Call {
     }
     a.hc = at<uint16_t>(p.hc);
     a.wc = p.pack_w ? at<uint16_t>(p.wc) : nullptr;
-    if (grad) a.row_lse2 = at<float>(p.row_lse2), a.row_coef = at<float>(p.row_coef);
+    if (grad) {
+      a.row_lse2 = at<float>(p.row_lse2), a.row_coef = at<float>(p.row_coef);
+      a.row_label = at<int32_t>(p.row_label), a.row_spot = at<float>(p.row_spot);
+    }
     a.n_parts = p.n_parts;
     a.rows_pad = p.rows_pad;
     return FL_OK;
@@ -195,7 +200,6 @@ struct Call {
   int prepare() {
     if (p.distill && p.T > 0)
       if (const hipError_t e = launch_head_teacher(a, st)) return status_of(e);
-    if (const hipError_t e = launch_head_live(a, st)) return status_of(e);
     if (const hipError_t e = launch_head_pack(a, p.grad, st)) return status_of(e);
     if (p.pack_w)
       if (const hipError_t e = launch_head_pack_weight(a, st)) return status_of(e);
@@ -271,9 +275,12 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
     if (p.T > 0) {
       TileArgs g = c.logits(v0, v1);
       g.row_lse2 = c.a.row_lse2, g.row_coef = c.a.row_coef;
+      g.row_label = p.distill ? nullptr : c.a.row_label, g.row_spot = c.a.row_spot;
+      g.p_first = v0;
       g.G = G, g.ldg = ldg;
       if ((rc = status_of(launch_logits_grad(g, p.logits_shape, c.st))) != FL_OK) return rc;
-      if ((rc = status_of(launch_head_fix(c.a, G, ldg, v0, v1, c.st))) != FL_OK) return rc;
+      if (p.distill && (rc = status_of(launch_head_fix(c.a, G, ldg, v0, v1, c.st))) != FL_OK)
+        return rc;
     }
     TileArgs w{};
     w.P = c.a.hc, w.ldp = p.Dp;
