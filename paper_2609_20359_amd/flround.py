@@ -8,6 +8,7 @@ raises FlError.  If the library is missing, importing the symbols raises:
 there is no fallback.
 """
 import ctypes
+import functools
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -520,52 +521,78 @@ def fl_round_outer(layout, cfg, outer, grads, replicas, prev, buf, master, m, v,
 # ---- the output head --------------------------------------------------------
 
 
-def _array(t, shape, dtype, what):
-    """Device address of a contiguous CUDA tensor of this shape and dtype on
-    the current device."""
+_T = None   # torch and the current device's number, looked up once: a call of a few
+_dev = None  # us would spend as long on the module's own way to them
+
+
+def _torch():
+    global _T, _dev
+    if _T is None:
+        import torch
+
+        _dev = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _T = torch
+    return _T
+
+
+def _array(t, shape, dtype, dev, what):
+    """Device address of a contiguous tensor of this shape and dtype on device
+    dev."""
+    try:
+        if (t.dtype is dtype and t.shape == shape and t.get_device() == dev
+                and t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    # something is wrong with it: say what
+    _on_device(t, dev, what)
+    raise ValueError("%s must be a contiguous %s tensor of shape %s; got %s of shape %s"
+                     % (what, dtype, shape, t.dtype, tuple(t.shape)))
+
+
+def _device_of(t, what):
+    """The current device, which has to be t's."""
+    if not getattr(t, "is_cuda", False):   # (where there is no GPU, there is no device to ask for)
+        raise ValueError("%s must be a CUDA tensor" % what)
+    dev = _dev()
+    _on_device(t, dev, what)
+    return dev
+
+
+def _on_device(t, dev, what):
     if not getattr(t, "is_cuda", False):
         raise ValueError("%s must be a CUDA tensor" % what)
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape %s; got %s of shape %s"
-                         % (what, dtype, shape, t.dtype, tuple(t.shape)))
-    _on_current_device(t, what)
-    return t.data_ptr()
-
-
-def _on_current_device(t, what):
-    import torch
-
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise ValueError("%s is on device %d; the current device is %d"
-                         % (what, t.get_device(), torch.cuda.current_device()))
+                         % (what, t.get_device(), dev))
 
 
-def _rows(t, dtypes, what):
-    """(address, elements between rows) of a 2-D CUDA tensor whose rows are
+def _rows(t, dtypes, dev, what):
+    """(address, elements between rows) of a 2-D tensor whose rows are
     contiguous and do not overlap."""
-    if not getattr(t, "is_cuda", False):
-        raise ValueError("%s must be a CUDA tensor" % what)
+    if t.get_device() != dev:
+        _on_device(t, dev, what)
     if t.dim() != 2 or t.dtype not in dtypes:
         raise ValueError("%s must be a 2-D tensor of %s" % (what, " or ".join(map(str, dtypes))))
     n, d = t.shape
-    if d > 1 and t.stride(1) != 1:
+    between, within = t.stride()
+    if d > 1 and within != 1:
         raise ValueError("%s must have contiguous rows" % what)
-    stride = t.stride(0) if n > 1 else d
-    if stride < d:
+    if n <= 1:
+        between = d
+    if between < d:
         raise ValueError("%s has overlapping rows" % what)
-    _on_current_device(t, what)
-    return t.data_ptr(), stride
+    return t.data_ptr(), between
 
 
-def _workspace(workspace, nbytes, stream):
-    """(address, bytes) of the workspace: the tensor given, or one from torch's
+def _workspace(workspace, nbytes, dev, stream):
+    """(tensor, bytes) of the workspace: the tensor given, or one from torch's
     allocator, which reuses it in the order of the stream it was taken on."""
-    import torch
-
+    torch = _T
     if workspace is not None:
-        if not workspace.is_cuda or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous CUDA tensor")
-        _on_current_device(workspace, "workspace")
+        _on_device(workspace, dev, "workspace")
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
         return workspace, workspace.numel() * workspace.element_size()
     if stream is None:
         return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
@@ -573,6 +600,13 @@ def _workspace(workspace, nbytes, stream):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     with torch.cuda.stream(stream):
         return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
+
+
+@functools.lru_cache(maxsize=256)
+def _head_shape(T, V, D, ldh, ldw, k, grad):
+    """The shape as the library takes it, and the bytes of workspace for it."""
+    s = HeadShape(T, V, D, ldh, ldw)
+    return ctypes.byref(s), lib().fl_head_workspace_bytes(ctypes.byref(s), k, grad)
 
 
 def head_workspace_bytes(tokens, vocab, width, k=0, grad=False, weight_stride=0):
@@ -591,51 +625,48 @@ class _HeadCall:
     """The arguments that the head's four functions share, checked."""
 
     def __init__(self, hidden, weight, k, grad, workspace, stream):
-        import torch
-
-        self.h, ldh = _rows(hidden, (torch.bfloat16,), "hidden")
-        self.w, ldw = _rows(weight, (torch.bfloat16,), "weight")
+        torch = _T or _torch()
+        self.dev = dev = _device_of(hidden, "hidden")
+        bf16 = (torch.bfloat16,)
+        self.h, ldh = _rows(hidden, bf16, dev, "hidden")
+        self.w, ldw = _rows(weight, bf16, dev, "weight")
         self.T, self.D = hidden.shape
-        self.V = weight.shape[0]
-        if weight.shape[1] != self.D:
-            raise ValueError("hidden is %d wide, weight %d" % (self.D, weight.shape[1]))
-        self.shape = HeadShape(self.T, self.V, self.D, ldh, ldw)
-        need = lib().fl_head_workspace_bytes(ctypes.byref(self.shape), k, grad)
-        self.keep, self.ws_bytes = _workspace(workspace, need, stream)
+        self.V, width = weight.shape
+        if width != self.D:
+            raise ValueError("hidden is %d wide, weight %d" % (self.D, width))
+        self.shape, need = _head_shape(self.T, self.V, self.D, ldh, ldw, k, grad)
+        self.keep, self.ws_bytes = _workspace(workspace, need, dev, stream)
         self.ws = self.keep.data_ptr()
         self.stream = _stream(stream)
 
-    def floats(self, t, what, *shape):
-        import torch
+    def floats(self, t, what):
+        return _array(t, (self.T,), _T.float32, self.dev, what)
 
-        return _array(t, shape or (self.T,), torch.float32, what)
+    def listed(self, t, what):
+        return _array(t, (self.T, self.k), _T.float32, self.dev, what)
+
+    def labels(self, t):
+        return _array(t, (self.T,), _T.int64, self.dev, "labels")
 
     def teacher(self, ids, teacher, teacher_lse):
-        import torch
-
         if ids.dim() != 2:
             raise ValueError("ids must be a 2-D tensor")
         self.k = ids.shape[1]
-        return (_array(ids, (self.T, self.k), torch.int32, "ids"),
-                self.floats(teacher, "teacher", self.T, self.k),
+        return (_array(ids, (self.T, self.k), _T.int32, self.dev, "ids"),
+                self.listed(teacher, "teacher"),
                 None if teacher_lse is None else self.floats(teacher_lse, "teacher_lse"))
 
     def grads(self, dhidden, dweight):
-        import torch
-
-        return (_array(dhidden, (self.T, self.D), torch.bfloat16, "dhidden"),
-                _array(dweight, (self.V, self.D), torch.bfloat16, "dweight"))
+        return (_array(dhidden, (self.T, self.D), _T.bfloat16, self.dev, "dhidden"),
+                _array(dweight, (self.V, self.D), _T.bfloat16, self.dev, "dweight"))
 
 
 def fl_head_loss(hidden, weight, labels, loss, lse, target, workspace=None, stream=None):
     """Cross entropy of hidden (T x D bf16) through weight (V x D bf16) at
     labels (T int64, negative: the token takes no part).  Writes loss, lse and
     target (T float32 each); lse and target go to fl_head_loss_grad."""
-    import torch
-
     c = _HeadCall(hidden, weight, 0, 0, workspace, stream)
-    rc = lib().fl_head_loss(ctypes.byref(c.shape), c.h, c.w,
-                            _array(labels, (c.T,), torch.int64, "labels"), c.floats(loss, "loss"),
+    rc = lib().fl_head_loss(c.shape, c.h, c.w, c.labels(labels), c.floats(loss, "loss"),
                             c.floats(lse, "lse"), c.floats(target, "target"), c.ws, c.ws_bytes,
                             c.stream)
     _check(rc, "fl_head_loss")
@@ -645,14 +676,11 @@ def fl_head_loss_grad(hidden, weight, labels, lse, target, dloss, dhidden, dweig
                       workspace=None, stream=None):
     """Gradient of sum(dloss * loss): writes dhidden (T x D) and dweight
     (V x D), bf16.  lse and target as fl_head_loss wrote them."""
-    import torch
-
     c = _HeadCall(hidden, weight, 0, 1, workspace, stream)
     dh, dw = c.grads(dhidden, dweight)
-    rc = lib().fl_head_loss_grad(ctypes.byref(c.shape), c.h, c.w,
-                                 _array(labels, (c.T,), torch.int64, "labels"),
-                                 c.floats(lse, "lse"), c.floats(target, "target"),
-                                 c.floats(dloss, "dloss"), dh, dw, c.ws, c.ws_bytes, c.stream)
+    rc = lib().fl_head_loss_grad(c.shape, c.h, c.w, c.labels(labels), c.floats(lse, "lse"),
+                                 c.floats(target, "target"), c.floats(dloss, "dloss"), dh, dw,
+                                 c.ws, c.ws_bytes, c.stream)
     _check(rc, "fl_head_loss_grad")
 
 
@@ -665,9 +693,9 @@ def fl_head_distill(hidden, weight, ids, teacher, teacher_lse, tau, loss, lse, t
     target (T x k float32)."""
     c = _HeadCall(hidden, weight, ids.shape[-1], 0, workspace, stream)
     i, a, al = c.teacher(ids, teacher, teacher_lse)
-    rc = lib().fl_head_distill(ctypes.byref(c.shape), c.h, c.w, c.k, i, a, al, float(tau),
+    rc = lib().fl_head_distill(c.shape, c.h, c.w, c.k, i, a, al, float(tau),
                                c.floats(loss, "loss"), c.floats(lse, "lse"),
-                               c.floats(target, "target", c.T, c.k), c.ws, c.ws_bytes, c.stream)
+                               c.listed(target, "target"), c.ws, c.ws_bytes, c.stream)
     _check(rc, "fl_head_distill")
 
 
@@ -678,8 +706,8 @@ def fl_head_distill_grad(hidden, weight, ids, teacher, teacher_lse, tau, lse, ta
     c = _HeadCall(hidden, weight, ids.shape[-1], 1, workspace, stream)
     i, a, al = c.teacher(ids, teacher, teacher_lse)
     dh, dw = c.grads(dhidden, dweight)
-    rc = lib().fl_head_distill_grad(ctypes.byref(c.shape), c.h, c.w, c.k, i, a, al, float(tau),
-                                    c.floats(lse, "lse"), c.floats(target, "target", c.T, c.k),
+    rc = lib().fl_head_distill_grad(c.shape, c.h, c.w, c.k, i, a, al, float(tau),
+                                    c.floats(lse, "lse"), c.listed(target, "target"),
                                     c.floats(dloss, "dloss"), dh, dw, c.ws, c.ws_bytes, c.stream)
     _check(rc, "fl_head_distill_grad")
 
@@ -689,18 +717,18 @@ def fl_top_logits(logits, k, tau, values, ids, lse=None, workspace=None, stream=
     may be longer), largest first, ties to the lowest id: writes values
     (rows x k float32), ids (rows x k int32) and lse (rows float32, or None),
     the log of the sum of exp(logits / tau)."""
-    import torch
-
-    p, stride = _rows(logits, (torch.bfloat16, torch.float32), "logits")
+    torch = _T or _torch()
+    dev = _device_of(logits, "logits")
+    p, stride = _rows(logits, (torch.bfloat16, torch.float32), dev, "logits")
     n, v = logits.shape
     dtype = FL_BF16 if logits.dtype == torch.bfloat16 else FL_F32
-    args = (_array(values, (n, k), torch.float32, "values"),
-            _array(ids, (n, k), torch.int32, "ids"),
-            None if lse is None else _array(lse, (n,), torch.float32, "lse"))
+    args = (_array(values, (n, k), torch.float32, dev, "values"),
+            _array(ids, (n, k), torch.int32, dev, "ids"),
+            None if lse is None else _array(lse, (n,), torch.float32, dev, "lse"))
     need = lib().fl_top_workspace_bytes(n, v, dtype, k)
     ws, ws_bytes = None, 0
     if need or workspace is not None:
-        keep, ws_bytes = _workspace(workspace, need, stream)
+        keep, ws_bytes = _workspace(workspace, need, dev, stream)
         ws = keep.data_ptr()
     rc = lib().fl_top_logits(n, v, stride, dtype, p, k, float(tau), *args, ws, ws_bytes,
                              _stream(stream))
