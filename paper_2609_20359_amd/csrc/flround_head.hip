@@ -221,11 +221,14 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
   __shared__ __attribute__((aligned(128))) char sm1[OpP::kBytes + OpQ::kBytes];
 
   __shared__ float2 folded[EPI == kStats ? WP : 1][EPI == kStats ? BQ : 1];
+  __shared__ float row_lse2[EPI == kGrad ? BQ : 1], row_coef[EPI == kGrad ? BQ : 1];
+  __shared__ int row_label[EPI == kGrad ? BQ : 1];
 
   const int tid = threadIdx.x, l = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wp = w % WP, wq = w / WP;
   const int n_live = a.hdr->n_live;
+  const float out_factor = EPI == kOut ? a.hdr->scale * a.out_scale : 0.f;
   const int64_t nq = a.live_q ? n_live : a.nq;
   const int64_t nk = a.live_k ? n_live : a.nk;
   const int tiles_p = (int)((a.np + BP - 1) / BP), tiles_q = (int)((nq + BQ - 1) / BQ);
@@ -351,7 +354,21 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
     // after the last tile: its own first steps again, which nothing reads
     const bool more = id + stride < end;
     aim(more ? id + stride : id);
+    // What the epilogue wants of its rows is asked for before the last steps and
+    // passed through LDS between them, behind whose meeting it is there.
+    float lse2_in = 0.f, coef_in = 0.f;
+    int label_in = -1;
+    if (EPI == kGrad && tid < BQ && q0 + tid < n_live) {
+      lse2_in = a.row_lse2[q0 + tid];
+      coef_in = a.row_coef[q0 + tid];
+      if (a.row_label) label_in = a.row_label[q0 + tid];
+    }
     step(sm0, sm1, [&](int i) { if (i == 0) load_first(sm0); });
+    if (EPI == kGrad && tid < BQ) {
+      row_lse2[tid] = lse2_in;
+      row_coef[tid] = coef_in;
+      row_label[tid] = label_in;
+    }
     step(sm1, sm0, [&](int i) { if (i == 0) load_second(sm1); });
 
     // lane l holds, of the 16 x 16 outputs (i, j), q = l % 16 and
@@ -403,7 +420,8 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
       for (int j = 0; j < FQ; ++j) {
         const int64_t q = qw + j * 16;
         const bool live = q < n_live;
-        const float lse2 = live ? a.row_lse2[q] : 0.f, coef = live ? a.row_coef[q] : 0.f;
+        const int r = (wq * FQ + j) * 16 + (l & 15);
+        const float lse2 = row_lse2[r], coef = row_coef[r];
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll
@@ -413,7 +431,7 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
           }
         if (a.row_label) {
           // the label's entry, where one of the wave's rows has it among these
-          const int64_t y = live ? a.row_label[q] - a.p_first - pw : -1;
+          const int64_t y = row_label[r] - a.p_first - pw;
           const bool here = y >= 0 && y < FP * 16 && (y & 12) == 0;
           if (__any(here)) {
             const float spot = here ? a.row_spot[q] : 0.f;
@@ -449,7 +467,6 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
         }
       }
     } else {
-      const float f = a.hdr->scale * a.out_scale;
 #pragma unroll
       for (int j = 0; j < FQ; ++j) {
         const int64_t q = qw + j * 16;
@@ -459,7 +476,7 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
           u32x2 d[2];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const f32x4 v = acc[i + h][j] * f;
+            const f32x4 v = acc[i + h][j] * out_factor;
             d[h] = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
           }
           const u32x4 x = eight(d[0], d[1]);
