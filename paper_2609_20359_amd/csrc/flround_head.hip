@@ -137,11 +137,11 @@ struct Operand {
 
   // The step that the summed axis ends inside: `left` elements of it remain (in
   // whole chunks where TR = false), the others are zero.
-  __device__ __forceinline__ void load_tail(char* lds, int s, int wave, int tid, int left,
-                                            const uint16_t* zero) const {
+  __device__ __forceinline__ void load_tail(char* lds, int s, int wave, int c0, int c1, int tid,
+                                            int left, const uint16_t* zero) const {
     const char* b = base + s * step;
 #pragma unroll
-    for (int c = 0; c < kLoads; ++c) {
+    for (int c = c0; c < c1; ++c) {
       if (B * 8 % NT != 0 && wave * 64 >= B * 8) continue;
       const bool in = TR ? row(tid, c) < left : chunk(tid, c) * 8 < left;
       const char* p = in ? b + pinned(at[c]) : reinterpret_cast<const char*>(zero);
@@ -283,13 +283,19 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
     first_left = __builtin_amdgcn_readfirstlane(first_left);
     second_left = __builtin_amdgcn_readfirstlane(second_left);
   };
-  auto load_first = [&](char* to) {
-    op.load_tail(to, first, w, (int)pinned(tid), first_left, a.zero);
-    oq.load_tail(to + OpP::kBytes, first, w, (int)pinned(tid), first_left ? kStep : 0, a.zero);
+  // Part i of n of the loads of a tile's first and second step.
+  auto load_first = [&](char* to, int i, int n) {
+    const int t = (int)pinned(tid);
+    op.load_tail(to, first, w, i * OpP::kLoads / n, (i + 1) * OpP::kLoads / n, t, first_left, a.zero);
+    oq.load_tail(to + OpP::kBytes, first, w, i * OpQ::kLoads / n, (i + 1) * OpQ::kLoads / n, t,
+                 first_left ? kStep : 0, a.zero);
   };
-  auto load_second = [&](char* to) {
-    op.load_tail(to, 1 + shift, w, (int)pinned(tid), second_left, a.zero);
-    oq.load_tail(to + OpP::kBytes, 1 + shift, w, (int)pinned(tid), second_left, a.zero);
+  auto load_second = [&](char* to, int i, int n) {
+    const int t = (int)pinned(tid);
+    op.load_tail(to, 1 + shift, w, i * OpP::kLoads / n, (i + 1) * OpP::kLoads / n, t, second_left,
+                 a.zero);
+    oq.load_tail(to + OpP::kBytes, 1 + shift, w, i * OpQ::kLoads / n, (i + 1) * OpQ::kLoads / n, t,
+                 second_left, a.zero);
   };
 
   f32x4 acc[FP][FQ];
@@ -325,8 +331,8 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
   };
 
   aim(id);
-  load_first(sm0);
-  load_second(sm1);
+  load_first(sm0, 0, 1);
+  load_second(sm1, 0, 1);
   wait_and_meet();
 #pragma unroll
   for (int j = 0; j < FQ; ++j) qa[j] = OpQ::frag(sm0 + OpP::kBytes, lane_q, wq * FQ, j, 0, l);
@@ -363,13 +369,13 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
       coef_in = a.row_coef[q0 + tid];
       if (a.row_label) label_in = a.row_label[q0 + tid];
     }
-    step(sm0, sm1, [&](int i) { if (i == 0) load_first(sm0); });
+    step(sm0, sm1, [&](int i) { load_first(sm0, i, FP); });
     if (EPI == kGrad && tid < BQ) {
       row_lse2[tid] = lse2_in;
       row_coef[tid] = coef_in;
       row_label[tid] = label_in;
     }
-    step(sm1, sm0, [&](int i) { if (i == 0) load_second(sm1); });
+    step(sm1, sm0, [&](int i) { load_second(sm1, i, FP); });
 
     // lane l holds, of the 16 x 16 outputs (i, j), q = l % 16 and
     // p = 4 (l / 16) .. + 3
@@ -415,40 +421,38 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
         a.parts[(int64_t)my_tp * a.parts_ld + q0 + tid] = p;
       }
     } else if constexpr (EPI == kGrad) {
-      const bool edge = p0 + BP > a.np;
+      const bool inside = p0 + BP <= a.np && q0 + BQ <= n_live;
+      uint16_t* g = a.G + qw * a.ldg + p0 + wp * FP * 16 + (l >> 4) * 8;
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) {
-        const int64_t q = qw + j * 16;
-        const bool live = q < n_live;
+      for (int j = 0; j < FQ; ++j, g += 16 * a.ldg) {
         const int r = (wq * FQ + j) * 16 + (l & 15);
         const float lse2 = row_lse2[r], coef = row_coef[r];
-#pragma unroll
-        for (int i = 0; i < FP; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = coef * exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -lse2));
-            acc[i][j][e] = !live || (edge && pw + i * 16 + e >= a.np) ? 0.f : v;
-          }
-        if (a.row_label) {
-          // the label's entry, where one of the wave's rows has it among these
-          const int64_t y = row_label[r] - a.p_first - pw;
-          const bool here = y >= 0 && y < FP * 16 && (y & 12) == 0;
-          if (__any(here)) {
-            const float spot = here ? a.row_spot[q] : 0.f;
-#pragma unroll
-            for (int i = 0; i < FP; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (here && y == i * 16 + e) acc[i][j][e] = spot;
-          }
-        }
-        uint16_t* g = a.G + q * a.ldg + p0 + wp * FP * 16 + (l >> 4) * 8;
+        // the label's place among this lane's, where one of the wave's rows has
+        // it among the wave's
+        const int64_t y = row_label[r] - a.p_first - pw;
+        const bool here = y >= 0 && y < FP * 16 && (y & 12) == 0;
+        const bool labels = __any(here);
+        const float spot = here ? a.row_spot[qw + j * 16] : 0.f;
 #pragma unroll
         for (int i = 0; i < FP; i += 2) {
-          const f32x4 x = acc[i][j], y = acc[i + 1][j];
-          *reinterpret_cast<u32x4*>(g + i * 16) =
-              eight(u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])},
-                    u32x2{pack2(y[0], y[1]), pack2(y[2], y[3])});
+          u32x2 d[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] = coef * exp2_(__builtin_fmaf(acc[i + h][j][e], a.s2, -lse2));
+            if (!inside)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (qw + j * 16 >= n_live || pw + (i + h) * 16 + e >= a.np) v[e] = 0.f;
+            if (labels)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (here && y == (i + h) * 16 + e) v[e] = spot;
+            d[h] = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+          }
+          *reinterpret_cast<u32x4*>(g + i * 16) = eight(d[0], d[1]);
         }
       }
     } else if constexpr (EPI == kSlab) {
@@ -467,29 +471,34 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
         }
       }
     } else {
+      const bool inside = a.vec_out && p0 + BP <= a.np && q0 + BQ <= nq;
+      uint16_t* o = a.out + qw * a.ld_out + p0 + wp * FP * 16 + (l >> 4) * 8;
+      auto result = [&](int i, int j) {
+        const f32x4 x = acc[i][j] * out_factor, y = acc[i + 1][j] * out_factor;
+        return eight(u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])},
+                     u32x2{pack2(y[0], y[1]), pack2(y[2], y[3])});
+      };
+      if (inside) {
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) {
-        const int64_t q = qw + j * 16;
-        uint16_t* o = a.out + q * a.ld_out;
+        for (int j = 0; j < FQ; ++j, o += 16 * a.ld_out)
 #pragma unroll
-        for (int i = 0; i < FP; i += 2) {
-          u32x2 d[2];
+          for (int i = 0; i < FP; i += 2) *reinterpret_cast<u32x4*>(o + i * 16) = result(i, j);
+      } else {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const f32x4 v = acc[i + h][j] * out_factor;
-            d[h] = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+        for (int j = 0; j < FQ; ++j, o += 16 * a.ld_out)
+#pragma unroll
+          for (int i = 0; i < FP; i += 2) {
+            const u32x4 x = result(i, j);
+            const int64_t p = p0 + (wp * FP + i) * 16 + (l >> 4) * 8;
+            if (qw + j * 16 >= nq || p >= a.np) continue;
+            if (a.vec_out) {
+              *reinterpret_cast<u32x4*>(o + i * 16) = x;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (p + e < a.np) o[i * 16 + e] = (uint16_t)(x[e >> 1] >> (e & 1) * 16);
+            }
           }
-          const u32x4 x = eight(d[0], d[1]);
-          const int64_t p = p0 + (wp * FP + i) * 16 + (l >> 4) * 8;
-          if (q >= nq || p >= a.np) continue;
-          if (a.vec_out) {
-            *reinterpret_cast<u32x4*>(o + p) = x;
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (p + e < a.np) o[p + e] = (uint16_t)(x[e >> 1] >> (e & 1) * 16);
-          }
-        }
       }
     }
     if (!more) break;
