@@ -29,6 +29,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));   // on an element's boundary only
 
 #define LDS_SPACE __attribute__((address_space(3)))
 #define GLOBAL_SPACE __attribute__((address_space(1)))
@@ -36,7 +37,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float bf16_f(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
@@ -633,8 +633,17 @@ __global__ __launch_bounds__(1024) void k_live(const HeadArgs a) {
   }
 }
 
-__device__ __forceinline__ bool aligned_rows(const uint16_t* p, int64_t ld, int64_t D) {
-  return ((reinterpret_cast<uintptr_t>(p) & 15) | (ld & 7) | (D & 7)) == 0;
+// Eight elements of a row of D from d on, those past its end 0.
+__device__ __forceinline__ u32x4 row_chunk(const uint16_t* row, int64_t d, int64_t D) {
+  if (d + 8 <= D) return *reinterpret_cast<const u32x4_at2*>(row + d);
+  u32x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t lo = d + 2 * e < D ? row[d + 2 * e] : 0;
+    const uint32_t hi = d + 2 * e + 1 < D ? row[d + 2 * e + 1] : 0;
+    o[e] = lo | hi << 16;
+  }
+  return o;
 }
 __device__ __forceinline__ bool is_live(const HeadArgs& a, int64_t t) {
   return a.labels ? a.labels[t] >= 0 : a.flag[t] != 0;
@@ -707,13 +716,8 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
   }
   const uint16_t* h = a.hidden + t * a.ldh;
   uint16_t* hc = a.hc + q * a.Dp;
-  const bool vec = aligned_rows(a.hidden, a.ldh, a.D);
-  if (vec) {
-    for (int64_t d = tid * 8; d < a.Dp; d += 2048)
-      *reinterpret_cast<u32x4*>(hc + d) = d < a.D ? *reinterpret_cast<const u32x4*>(h + d) : zero;
-  } else {
-    for (int64_t d = tid; d < a.Dp; d += 256) hc[d] = d < a.D ? h[d] : 0;
-  }
+  for (int64_t d = tid * 8; d < a.Dp; d += 2048)
+    *reinterpret_cast<u32x4*>(hc + d) = row_chunk(h, d, a.D);
   if (GRAD) {
     if (tid == 0) {
       const float ratio = a.dloss[t] / scale, lse = a.lse_in[t];
@@ -729,7 +733,6 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     }
     return;
   }
-  const bool wvec = vec && aligned_rows(a.weight, a.ldw, a.D);
   for (int k = w; k < a.K; k += 4) {
     const int64_t id = a.labels ? a.labels[t] : a.ids[t * a.K + k];
     float s = 0.f;
@@ -737,19 +740,15 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
       s = NAN;
     } else if (id >= 0) {
       const uint16_t* r = a.weight + id * a.ldw;
-      if (wvec) {
-        for (int64_t d = l * 8; d < a.D; d += 512) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(h + d);
-          const u32x4 y = *reinterpret_cast<const u32x4*>(r + d);
+      for (int64_t d = l * 8; d < a.D; d += 512) {
+        const u32x4 x = row_chunk(h, d, a.D);
+        const u32x4 y = row_chunk(r, d, a.D);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s = __builtin_fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
-            s = __builtin_fmaf(__uint_as_float(x[e] & 0xFFFF0000u),
-                               __uint_as_float(y[e] & 0xFFFF0000u), s);
-          }
+        for (int e = 0; e < 4; ++e) {
+          s = __builtin_fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
+          s = __builtin_fmaf(__uint_as_float(x[e] & 0xFFFF0000u),
+                             __uint_as_float(y[e] & 0xFFFF0000u), s);
         }
-      } else {
-        for (int64_t d = l; d < a.D; d += 64) s = __builtin_fmaf(bf16_f(h[d]), bf16_f(r[d]), s);
       }
       s = wave_sum(s);
     }
@@ -764,15 +763,7 @@ __global__ __launch_bounds__(256) void k_pack_weight(const HeadArgs a) {
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n;
        i += (int64_t)gridDim.x * 2048) {
     const int64_t v = i / a.Dp, d = i % a.Dp;
-    const uint16_t* r = a.weight + v * a.ldw;
-    u32x4 o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t lo = d + 2 * e < a.D ? r[d + 2 * e] : 0;
-      const uint32_t hi = d + 2 * e + 1 < a.D ? r[d + 2 * e + 1] : 0;
-      o[e] = lo | hi << 16;
-    }
-    *reinterpret_cast<u32x4*>(a.wc + i) = o;
+    *reinterpret_cast<u32x4*>(a.wc + i) = row_chunk(a.weight + v * a.ldw, d, a.D);
   }
 }
 
