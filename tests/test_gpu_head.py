@@ -194,6 +194,23 @@ def test_distillation_and_gradient(env, T, V, D, K, tau, mass):
     Case(env["torch"], T, V, D, K=K, tau=tau, mass=mass).check(env["P"])
 
 
+def test_listed_words_close_together(env):
+    """Every token lists the same words, next to each other; one past the
+    vocabulary's end, where the last tile still has rows, gives NaN."""
+    torch, P = env["torch"], env["P"]
+    for T, V, D in ((300, 700, 64), (1030, 33100, 64)):
+        c = Case(torch, T, V, D, K=128, tau=1.5, empty=0.1)
+        c.ids = torch.where(c.ids >= 0, torch.arange(128, device="cuda", dtype=torch.int32) + 130, -1)
+        c.ids[5, 0] = V                      # in the last tile, not in the vocabulary
+        z = c.h.double() @ c.w.double().t()
+        loss, lse, target = c.forward(P)
+        live = (c.ids >= 0) & (c.ids < V) & c.keep[:, None]
+        want = torch.where(live, z.gather(1, c.ids.clamp(0, V - 1).long()), 0.0)
+        target[5, 0] = 0.0 if not math.isnan(float(target[5, 0])) else float(want[5, 0])
+        assert math.isnan(float(loss[5])) or not bool(c.keep[5])
+        near("target", target, want, c.z_off[:, None] + 1e-30)
+
+
 @pytest.mark.parametrize("K", [0, 6])
 def test_tokens_left_out_hold_anything(env, K):
     """NaN and infinities in the hidden states of tokens that take no part
