@@ -501,8 +501,8 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *   min(vocab, FL_MAX_TARGETS).  workspace: fl_top_workspace_bytes, NULL where
  *   that is 0.
  *
- * Limits (FL_ERR_INVALID beyond): tokens and rows <= 2^20, vocab <= 2^24
- * (fl_top_logits 2^20), width <= 2^16, strides of hidden and weight <= 2^22,
+ * Limits (FL_ERR_INVALID beyond): tokens and rows <= 2^20, vocab <= 2^21
+ * (fl_top_logits 2^20), width <= 2^15, strides of hidden and weight <= 2^22,
  * ceil(tokens / 128) * ceil(vocab / 128) <= 2^22.
  * ---------------------------------------------------------------------- */
 #define FL_MAX_TARGETS 128

@@ -863,27 +863,27 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
 __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab, int64_t ld_slab,
                                             int bp, int bq, int fit, int max_splits,
                                             float out_scale) {
-  const unsigned blocks = (unsigned)((a.D + 1023) / 1024);
-  const int64_t q = blockIdx.x / blocks;
-  const int64_t n = a.hdr->n_live;
-  if (q >= n) return;
-  const int64_t d = ((int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x) * 4;
-  if (d >= a.D) return;
+  const int64_t n = a.hdr->n_live, chunks = (a.D + 1023) / 1024;
   const int splits =
       splits_of(fit, (int)((a.D + bp - 1) / bp) * (int)((n + bq - 1) / bq), max_splits);
   const float f = a.hdr->scale * out_scale;
-  const float* p = slab + q * ld_slab + d;
-  f32x4 s = *reinterpret_cast<const f32x4*>(p);
+  const bool vec = ((a.D & 3) | (reinterpret_cast<uintptr_t>(a.dhidden) & 7)) == 0;
+  for (int64_t b = blockIdx.x; b < n * chunks; b += gridDim.x) {
+    const int64_t q = b / chunks, d = (b % chunks * 256 + threadIdx.x) * 4;
+    if (d >= a.D) continue;
+    const float* p = slab + q * ld_slab + d;
+    f32x4 s = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
-  for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4*>(p + i * (n * ld_slab));
-  s *= f;
-  uint16_t* o = a.dhidden + (int64_t)a.rows[q] * a.D + d;
-  if (((a.D & 3) | (reinterpret_cast<uintptr_t>(a.dhidden) & 7)) == 0) {
-    *reinterpret_cast<u32x2*>(o) = u32x2{pack2(s[0], s[1]), pack2(s[2], s[3])};
-  } else {
+    for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4*>(p + i * (n * ld_slab));
+    s *= f;
+    uint16_t* o = a.dhidden + (int64_t)a.rows[q] * a.D + d;
+    if (vec) {
+      *reinterpret_cast<u32x2*>(o) = u32x2{pack2(s[0], s[1]), pack2(s[2], s[3])};
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (d + e < a.D) o[e] = to_bf16(s[e]);
+      for (int e = 0; e < 4; ++e)
+        if (d + e < a.D) o[e] = to_bf16(s[e]);
+    }
   }
 }
 
@@ -924,8 +924,8 @@ hipError_t launch_head_fix(const HeadArgs& a, uint16_t* G, int64_t ldg, int64_t 
 }
 hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab, int shape,
                           int max_splits, float out_scale, hipStream_t st) {
-  const unsigned blocks = (unsigned)((a.D + 1023) / 1024);
-  k_dh<<<blocks * (unsigned)a.T, 256, 0, st>>>(a, slab, ld_slab, tile_p(shape), tile_q(shape),
+  const int64_t blocks = (a.D + 1023) / 1024 * a.T;
+  k_dh<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(a, slab, ld_slab, tile_p(shape), tile_q(shape),
                                                tile_fit(shape), max_splits, out_scale);
   return hipGetLastError();
 }

@@ -15,9 +15,9 @@ using namespace flr;
 namespace {
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 20;
-constexpr int64_t kMaxWidth = (int64_t)1 << 16;
+constexpr int64_t kMaxWidth = (int64_t)1 << 15;
 constexpr int64_t kMaxStride = (int64_t)1 << 22;   // 256 rows of it within 32 bits of bytes
-constexpr int64_t kMaxVocab = (int64_t)1 << 24;
+constexpr int64_t kMaxVocab = (int64_t)1 << 21;
 constexpr int64_t kMaxTopVocab = (int64_t)1 << 20;
 constexpr int64_t kMaxTiles = (int64_t)1 << 22;
 constexpr int kCus = 256;
