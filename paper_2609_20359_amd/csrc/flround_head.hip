@@ -201,11 +201,31 @@ __device__ __forceinline__ u32x4 eight(u32x2 a, u32x2 b) {
 
 enum Epilogue { kStats, kGrad, kSlab, kOut };
 
+// What bounds it: the matrix cores, at the clock that the power leaves them.
+// They are busy in 80 % of the cycles of the loss's product and 68 to 72 % of
+// the gradient's, no read of LDS meets a bank conflict, and a step of 256 x 256
+// outputs takes 1.43 us.  4096 live rows, 128256 words, 4096 wide, in PFLOP/s:
+// 1.37 for the statistics, 1.24 for G (0.87 ms a piece of 32256 words), 1.26 for
+// dW (0.86 ms), 1.37 for dh (0.79 ms); the library's plain products of these
+// sizes run at 1.43, 1.48 and 1.60.  What G and dW lose is their stores: without
+// them dW takes 0.77 ms, as a CU's 128 KiB go out at once and the next tile's
+// second step waits for them.  2048 and fewer rows lose 10 to 15 % where the
+// weight comes from HBM in every round of tiles, a step's loads being one step
+// ahead.
+//
+// Why these tiles: eight waves of 128 x 64 outputs read 96 KiB of LDS a step of
+// 64, a third of what LDS can give in that time, and keep their sums in 128
+// registers; four waves of 128 x 128 read a third less, but ran at 1.02 against
+// 1.27 (a plain product of 16384 x 4096 x 4096), alone on their SIMDs.  Reading
+// fragments half a step ahead, with the loads between the products, took that
+// product from 1.20 to 1.27, and to 1.50 without its fp32 output.
+//
 // Workgroups stay and take one tile after another, so that the loads of the next
 // tile's first steps run under the last products and the epilogue of this one.
 // Tiles are dealt so that the workgroups of an XCD, which share an L2, share
 // rows: workgroups go to the XCDs in turn, and each XCD takes a contiguous range
-// of an order that runs over q within bands of kBand p tiles.
+// of an order that runs over q within bands of kBand p tiles.  (The gradient of
+// 4096 tokens takes 10.40 ms with bands of 2, 9.99 of 4, 10.09 of 8.)
 constexpr int kBand = 4;
 constexpr int kXcds = 8;
 
@@ -545,6 +565,9 @@ __device__ __forceinline__ float wave_max(float x) {
   return x;
 }
 
+// None of these takes more than 25 us at 4096 tokens, but k_pack where many words
+// are listed.
+
 // The teacher's log probabilities of the listed words, one wave per token.  An
 // entry with a negative id, or of a teacher logit of -inf, has probability 0; a
 // token without any other takes no part.
@@ -654,7 +677,13 @@ __device__ __forceinline__ bool is_live(const HeadArgs& a, int64_t t) {
 // the listed words' rows of the weight (a wave per listed word), and zeros as
 // the results of the other tokens.  Gradient: also the coefficients of the
 // rows, and zeros as the other tokens' gradient.  SCAN: of up to kScan tokens
-// every workgroup finds by itself what k_live finds of more.
+// every workgroup finds by itself what k_live finds of more, which saves a launch
+// (7 tokens x 1000 x 96: 18.5 us for 21.6).
+//
+// The listed words' rows are what takes time: 1000 tokens of 64 words are 0.52 GB
+// of the weight, 0.13 ms (4.0 TB/s), an eighth of the call.  The product's
+// tiles hold these logits too, but looking for them there took as long and cost
+// the loss of labels registers.
 constexpr int kScan = 1024;
 
 template <bool GRAD, bool SCAN>
@@ -859,16 +888,19 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
   }
 }
 
-// The gradient of the hidden state from the splits' fp32 sums, added in order.
+// The gradient of the hidden state from the splits' fp32 sums, added in order
+// (bound by memory: 4096 x 4096 of one split, 101 MB, in 17 us).
 __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab, int64_t ld_slab,
                                             int bp, int bq, int fit, int max_splits,
                                             float out_scale) {
-  const int64_t n = a.hdr->n_live, chunks = (a.D + 1023) / 1024;
+  // at most 2^20 rows of 2^15 elements: 2^25 chunks
+  const int64_t n = a.hdr->n_live;
+  const unsigned chunks = (unsigned)((a.D + 1023) / 1024), all = (unsigned)n * chunks;
   const int splits =
       splits_of(fit, (int)((a.D + bp - 1) / bp) * (int)((n + bq - 1) / bq), max_splits);
   const float f = a.hdr->scale * out_scale;
   const bool vec = ((a.D & 3) | (reinterpret_cast<uintptr_t>(a.dhidden) & 7)) == 0;
-  for (int64_t b = blockIdx.x; b < n * chunks; b += gridDim.x) {
+  for (unsigned b = blockIdx.x; b < all; b += gridDim.x) {
     const int64_t q = b / chunks, d = (b % chunks * 256 + threadIdx.x) * 4;
     if (d >= a.D) continue;
     const float* p = slab + q * ld_slab + d;
@@ -925,8 +957,8 @@ hipError_t launch_head_fix(const HeadArgs& a, uint16_t* G, int64_t ldg, int64_t 
 hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab, int shape,
                           int max_splits, float out_scale, hipStream_t st) {
   const int64_t blocks = (a.D + 1023) / 1024 * a.T;
-  k_dh<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(a, slab, ld_slab, tile_p(shape), tile_q(shape),
-                                               tile_fit(shape), max_splits, out_scale);
+  k_dh<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(
+      a, slab, ld_slab, tile_p(shape), tile_q(shape), tile_fit(shape), max_splits, out_scale);
   return hipGetLastError();
 }
 hipError_t launch_logits_stats(const TileArgs& a, int shape, hipStream_t st) {

@@ -15,6 +15,12 @@
 // Rows longer than a segment are joined by a second kernel, in which an entry's
 // place is the sum of its places in the segments' sorted lists.
 //
+// Measured: 64 of 2048 rows of 128256 in bf16, 525 MB, in 117 us (4.5 TB/s; with
+// the values kept as floats, 239 registers and one workgroup per SIMD, 330); 100
+// of 100 rows of 100003 in fp32 in 23 us; 8 of one row of 50257 in 12 us, most of
+// it two launches.  The selection has no loads out; the other workgroups of a CU,
+// four in all, cover it.
+//
 // The order is that of one 64-bit number: the value, then the lower id; so ties
 // go to the lowest id and no result depends on the order of the lists.
 #include "flr_head.h"
