@@ -116,8 +116,10 @@ hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab,
                           int max_splits, float out_scale, hipStream_t st);
 hipError_t launch_logits_stats(const TileArgs& a, int shape, hipStream_t st);
 hipError_t launch_logits_grad(const TileArgs& a, int shape, hipStream_t st);
-hipError_t launch_dhidden(const TileArgs& a, int shape, hipStream_t st);
-hipError_t launch_dweight(const TileArgs& a, int shape, hipStream_t st);
+// The sums for the hidden state's gradient (nothing if it has no rows), and the
+// weight's gradient.
+hipError_t launch_grads(const TileArgs& h, int h_shape, const TileArgs& w, int w_shape,
+                        hipStream_t st);
 
 // Top logits.
 constexpr int kTopThreads = 512;

@@ -229,17 +229,28 @@ enum Epilogue { kStats, kGrad, kSlab, kOut };
 constexpr int kBand = 4;
 constexpr int kXcds = 8;
 
-template <int WP, int WQ, int FP, int FQ, bool PTR, bool QTR, int EPI, int FIT>
-__global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_tile(
-    const TileArgs a) {
-  constexpr int NT = WP * WQ * 64, BP = WP * FP * 16, BQ = WQ * FQ * 16;
+template <int WP_, int WQ_, int FP_, int FQ_, bool PTR_, bool QTR_, int EPI_, int FIT_>
+struct Tile {
+  static constexpr int WP = WP_, WQ = WQ_;      // waves along p and q
+  static constexpr int FP = FP_, FQ = FQ_;      // 16 x 16 outputs of a wave along p and q
+  static constexpr bool PTR = PTR_, QTR = QTR_; // orders of the operands
+  static constexpr int EPI = EPI_;
+  static constexpr int FIT = FIT_;              // workgroups that the chip holds
+  static constexpr int NT = WP * WQ * 64, BP = WP * FP * 16, BQ = WQ * FQ * 16;
   using OpP = Operand<BP, NT, PTR>;
   using OpQ = Operand<BQ, NT, QTR>;
-  // Two arrays, and two steps to a turn of the loop below, so that the compiler
-  // sees that reads of one stage need not wait for the loads to the other.
-  __shared__ __attribute__((aligned(128))) char sm0[OpP::kBytes + OpQ::kBytes];
-  __shared__ __attribute__((aligned(128))) char sm1[OpP::kBytes + OpQ::kBytes];
+  static constexpr int kBytes = OpP::kBytes + OpQ::kBytes;   // of a stage
+};
 
+// Workgroup `block` of `blocks` of a tiled product.  sm0, sm1: the stages.
+template <typename S>
+__device__ __forceinline__ void tile_work(const TileArgs& a, int block, int blocks, char* sm0,
+                                          char* sm1) {
+  constexpr int WP = S::WP, FP = S::FP, FQ = S::FQ, EPI = S::EPI, FIT = S::FIT;
+  constexpr bool PTR = S::PTR, QTR = S::QTR;
+  constexpr int BP = S::BP, BQ = S::BQ;
+  using OpP = typename S::OpP;
+  using OpQ = typename S::OpQ;
   __shared__ float2 folded[EPI == kStats ? WP : 1][EPI == kStats ? BQ : 1];
   __shared__ float row_lse2[EPI == kGrad ? BQ : 1], row_coef[EPI == kGrad ? BQ : 1];
   __shared__ int row_label[EPI == kGrad ? BQ : 1];
@@ -259,12 +270,12 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
 
   // this workgroup's tiles: id, id + stride, ... below end
   int id, end;
-  const int stride = gridDim.x / kXcds;
+  const int stride = blocks / kXcds;
   {
-    const int all = tiles * splits, x = blockIdx.x % kXcds;
+    const int all = tiles * splits, x = block % kXcds;
     const int per = all / kXcds, rem = all % kXcds;
     const int start = x * per + (x < rem ? x : rem);
-    id = start + blockIdx.x / kXcds;
+    id = start + block / kXcds;
     end = start + per + (x < rem);
   }
   if (id >= end) return;
@@ -528,27 +539,59 @@ __global__ __launch_bounds__(WP* WQ * 64) __attribute__((amdgpu_waves_per_eu(2))
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
+template <typename S>
+__global__ __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(2))) void k_tile(
+    const TileArgs a) {
+  // Two arrays, and two steps to a turn of the loop, so that the compiler sees
+  // that reads of one stage need not wait for the loads to the other.
+  __shared__ __attribute__((aligned(128))) char sm0[S::kBytes];
+  __shared__ __attribute__((aligned(128))) char sm1[S::kBytes];
+  tile_work<S>(a, blockIdx.x, gridDim.x, sm0, sm1);
+}
+
+// Two products at a time, the first by the first `blocks` workgroups: the
+// gradient's last two read the same G, and where they are short neither fills the
+// chip.
+template <typename S, typename R>
+__global__ __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(2))) void k_tiles(
+    const TileArgs a, const int blocks, const TileArgs b) {
+  static_assert(S::NT == R::NT, "one size of workgroup");
+  constexpr int kBytes = S::kBytes > R::kBytes ? S::kBytes : R::kBytes;
+  __shared__ __attribute__((aligned(128))) char sm0[kBytes];
+  __shared__ __attribute__((aligned(128))) char sm1[kBytes];
+  if ((int)blockIdx.x < blocks)
+    tile_work<S>(a, blockIdx.x, blocks, sm0, sm1);
+  else
+    tile_work<R>(b, blockIdx.x - blocks, gridDim.x - blocks, sm0, sm1);
+}
+
 template <bool PTR, bool QTR, int EPI>
-hipError_t launch_tile(const TileArgs& a, int64_t nq, int shape, hipStream_t st) {
+struct Tiles {
+  using T256 = Tile<2, 4, 8, 4, PTR, QTR, EPI, 256>;
+  using T128 = Tile<2, 2, 4, 4, PTR, QTR, EPI, 512>;
+  using T64 = Tile<4, 1, 2, 4, PTR, QTR, EPI, 768>;
+  using T16 = Tile<4, 1, 2, 1, PTR, QTR, EPI, 1024>;
+};
+using StatsTiles = Tiles<false, false, kStats>;
+using GradTiles = Tiles<false, false, kGrad>;
+using SlabTiles = Tiles<true, false, kSlab>;
+using OutTiles = Tiles<true, true, kOut>;
+
+// Workgroups of a product, 0 if it has no tiles.
+int blocks_of(const TileArgs& a, int shape, bool splits) {
   const int64_t tp = (a.np + tile_p(shape) - 1) / tile_p(shape);
-  const int64_t tq = (nq + tile_q(shape) - 1) / tile_q(shape);
+  const int64_t tq = (a.nq + tile_q(shape) - 1) / tile_q(shape);
   int64_t tiles = tp * tq;
-  if (tiles <= 0) return hipSuccess;
-  if (tiles > (int64_t)1 << 24) return hipErrorInvalidValue;
+  if (tiles <= 0) return 0;
   const int64_t fit = tile_fit(shape);
-  if (EPI == kSlab) tiles = fit;   // fewer live rows, more splits
-  const dim3 g((unsigned)(((tiles < fit ? tiles : fit) + kXcds - 1) / kXcds * kXcds));
-  switch (shape) {
-    case kTile256: k_tile<2, 4, 8, 4, PTR, QTR, EPI, 256><<<g, 512, 0, st>>>(a); break;
-    case kTile128: k_tile<2, 2, 4, 4, PTR, QTR, EPI, 512><<<g, 256, 0, st>>>(a); break;
-    case kTile64:
-      if constexpr (EPI != kOut) k_tile<4, 1, 2, 4, PTR, QTR, EPI, 768><<<g, 256, 0, st>>>(a);
-      else return hipErrorInvalidValue;
-      break;
-    default:
-      if constexpr (EPI == kStats) k_tile<4, 1, 2, 1, PTR, QTR, EPI, 1024><<<g, 256, 0, st>>>(a);
-      else return hipErrorInvalidValue;
-  }
+  if (splits || tiles > fit) tiles = fit;   // fewer live rows, more splits
+  return (int)((tiles + kXcds - 1) / kXcds * kXcds);
+}
+
+template <typename S>
+hipError_t launch_tile(const TileArgs& a, int shape, hipStream_t st) {
+  const int n = blocks_of(a, shape, S::EPI == kSlab);
+  if (n > 0) k_tile<S><<<(unsigned)n, S::NT, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -962,16 +1005,42 @@ hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab,
   return hipGetLastError();
 }
 hipError_t launch_logits_stats(const TileArgs& a, int shape, hipStream_t st) {
-  return launch_tile<false, false, kStats>(a, a.nq, shape, st);
+  switch (shape) {
+    case kTile256: return launch_tile<StatsTiles::T256>(a, shape, st);
+    case kTile128: return launch_tile<StatsTiles::T128>(a, shape, st);
+    case kTile64: return launch_tile<StatsTiles::T64>(a, shape, st);
+    default: return launch_tile<StatsTiles::T16>(a, shape, st);
+  }
 }
 hipError_t launch_logits_grad(const TileArgs& a, int shape, hipStream_t st) {
-  return launch_tile<false, false, kGrad>(a, a.nq, shape, st);
+  switch (shape) {
+    case kTile256: return launch_tile<GradTiles::T256>(a, shape, st);
+    case kTile128: return launch_tile<GradTiles::T128>(a, shape, st);
+    default: return launch_tile<GradTiles::T64>(a, shape, st);
+  }
 }
-hipError_t launch_dhidden(const TileArgs& a, int shape, hipStream_t st) {
-  return launch_tile<true, false, kSlab>(a, a.nq, shape, st);
-}
-hipError_t launch_dweight(const TileArgs& a, int shape, hipStream_t st) {
-  return launch_tile<true, true, kOut>(a, a.nq, shape, st);
+hipError_t launch_grads(const TileArgs& h, int h_shape, const TileArgs& w, int w_shape,
+                        hipStream_t st) {
+  // One launch for both where they are short: the gradients of 333 tokens x 5003 x
+  // 321 in 46 us for 49, of 64 x 50257 x 1024 in 104 for 110, but of 64 x 128256 x
+  // 4096 in 813 for 801.
+  if (w_shape == kTile128 && h_shape != kTile256 && w.np * w.nq <= (int64_t)1 << 26) {
+    const int nh = blocks_of(h, h_shape, true), nw = blocks_of(w, w_shape, false);
+    const dim3 grid((unsigned)(nh + nw));
+    if (h_shape == kTile64)
+      k_tiles<SlabTiles::T64, OutTiles::T128><<<grid, 256, 0, st>>>(h, nh, w);
+    else
+      k_tiles<SlabTiles::T128, OutTiles::T128><<<grid, 256, 0, st>>>(h, nh, w);
+    return hipGetLastError();
+  }
+  const hipError_t e = w_shape == kTile256 ? launch_tile<OutTiles::T256>(w, w_shape, st)
+                                           : launch_tile<OutTiles::T128>(w, w_shape, st);
+  if (e != hipSuccess) return e;
+  switch (h_shape) {
+    case kTile256: return launch_tile<SlabTiles::T256>(h, h_shape, st);
+    case kTile128: return launch_tile<SlabTiles::T128>(h, h_shape, st);
+    default: return launch_tile<SlabTiles::T64>(h, h_shape, st);
+  }
 }
 
 }  // namespace flr

@@ -296,17 +296,17 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
     w.out = dweight + v0 * p.D, w.ld_out = p.D;
     w.vec_out = (p.D & 7) == 0 && (reinterpret_cast<uintptr_t>(dweight) & 15) == 0;
     w.out_scale = out_scale;
-    if ((rc = status_of(launch_dweight(w, p.dw_shape, c.st))) != FL_OK) return rc;
+    TileArgs h{};
+    h.hdr = c.a.hdr;
     if (p.T > 0) {
-      TileArgs h{};
       h.P = c.weight_rows(v0), h.ldp = c.weight_ld();
       h.Q = G, h.ldq = ldg;
       h.np = p.D, h.nq = p.T, h.live_q = 1, h.nk = v1 - v0;
       h.hdr = c.a.hdr, h.zero = reinterpret_cast<const uint16_t*>(c.a.hdr->zero);
       h.slab = slab, h.ld_slab = p.Dp;
       h.add = v0 > 0, h.max_splits = p.max_splits;
-      if ((rc = status_of(launch_dhidden(h, p.dh_shape, c.st))) != FL_OK) return rc;
     }
+    if ((rc = status_of(launch_grads(h, p.dh_shape, w, p.dw_shape, c.st))) != FL_OK) return rc;
   }
   if (p.T == 0) return FL_OK;
   return status_of(launch_head_dh(c.a, slab, p.Dp, p.dh_shape, p.max_splits, out_scale, c.st));
