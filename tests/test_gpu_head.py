@@ -176,7 +176,9 @@ def near(what, got, want, off):
 # one token, odd widths, the tiles' edges, both sides of each tile choice
 SIZES = [(1, 1, 1), (1, 7, 3), (2, 300, 8), (7, 1000, 96), (16, 513, 64), (17, 130, 65),
          (64, 257, 128), (65, 1000, 72), (129, 2049, 130), (256, 512, 192), (300, 5003, 321),
-         (1, 40000, 256), (33, 9000, 1024), (1030, 16500, 136), (2100, 700, 64)]
+         (1, 40000, 256), (33, 9000, 1024), (1030, 16500, 136), (2100, 700, 64),
+         # large tiles of the weight's gradient, and two products apart of few tokens
+         (130, 13400, 1040), (140, 13400, 1041), (33, 33000, 2056), (100, 33000, 2056)]
 
 
 @pytest.mark.parametrize("T,V,D", SIZES)
@@ -186,7 +188,7 @@ def test_loss_and_gradient(env, T, V, D):
 
 
 @pytest.mark.parametrize("T,V,D,K,tau,mass", [
-    (1, 1, 1, 1, 1.0, False), (1, 50, 8, 5, 2.0, True), (9, 700, 96, 64, 1.5, False),
+    (1, 1, 1, 1, 1.0, False), (1, 50, 8, 5, 2.0, True), (150, 13400, 1040, 20, 2.0, True), (9, 700, 96, 64, 1.5, False),
     (33, 513, 65, 65, 1.0, True), (130, 3000, 128, 128, 4.0, True), (300, 2100, 320, 7, 0.5, False),
     (1030, 16500, 64, 32, 2.0, True)])
 def test_distillation_and_gradient(env, T, V, D, K, tau, mass):
@@ -256,6 +258,65 @@ def test_hidden_states_off_sixteen_bytes(env):
 def test_several_pieces_of_the_vocabulary(env, K):
     """Enough tokens that G is made in two pieces."""
     Case(env["torch"], 20000, 9001, 64, K=K).check(env["P"])
+
+
+def test_weight_past_32_bits_of_bytes(env):
+    """A head of 4.3 GB: labels and gradient rows at its end."""
+    torch, P = env["torch"], env["P"]
+    T, V, D = 4, 1050000, 2048
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    h = torch.randn(T, D, generator=g, device="cuda").bfloat16()
+    w = torch.empty(V, D, dtype=torch.bfloat16, device="cuda")
+    step = 50000
+    for v in range(0, V, step):
+        w[v:v + step] = torch.randn(step, D, generator=g, device="cuda") * (2.5 / math.sqrt(D))
+    labels = torch.tensor([V - 1, V - 2, 3, V - 777], device="cuda")
+    z = torch.cat([h.double() @ w[v:v + step].double().t() for v in range(0, V, step)], 1)
+    z_off = torch.cat([(D + 8) * U * (h.double().abs() @ w[v:v + step].double().abs().t())
+                       for v in range(0, V, step)], 1).amax(1)
+    loss, lse, target = (torch.empty(T, device="cuda") for _ in range(3))
+    P.fl_head_loss(h, w, labels, loss, lse, target)
+    want = torch.logsumexp(z, 1)
+    lse_off = z_off + 2.0 ** -16 + 4 * U * want.abs()
+    near("lse", lse, want, lse_off)
+    at = z.gather(1, labels[:, None])[:, 0]
+    near("target", target, at, z_off)
+    near("loss", loss, want - at, lse_off + z_off + 2.0 ** -22 * (want - at).abs())
+    dloss = torch.full((T,), 0.25, device="cuda")
+    dh = torch.empty(T, D, dtype=torch.bfloat16, device="cuda")
+    dw = torch.full((V, D), -7.0, dtype=torch.bfloat16, device="cuda")
+    P.fl_head_loss_grad(h, w, labels, lse, target, dloss, dh, dw)
+    share = torch.exp(z - want[:, None]) * 0.25
+    G = share.clone().scatter_add_(1, labels[:, None], torch.full((T, 1), -0.25, device="cuda").double())
+    off = 2.0 ** -8 * 1.01 * G.abs() + (2 * lse_off + 2.0 ** -20)[:, None] * share
+    off.scatter_add_(1, labels[:, None], torch.full((T, 1), 0.25 * 2.0 ** -20, device="cuda").double())
+    rows = torch.cat([torch.arange(0, 2000), torch.arange(V // 2, V // 2 + 2000),
+                      torch.arange(V - 2000, V)]).cuda()
+    want = G[:, rows].t() @ h.double()
+    near("dweight", dw[rows], want, off[:, rows].t() @ h.double().abs()
+         + (T + 64) * U * (G[:, rows].abs().t() @ h.double().abs()) + 2.0 ** -7.9 * want.abs() + 1e-37)
+    want, allowed = 0.0, 0.0
+    for v in range(0, V, step):
+        x = w[v:v + step].double()
+        want = want + G[:, v:v + step] @ x
+        allowed = allowed + (off[:, v:v + step] + (V // 64 + 64) * U * G[:, v:v + step].abs()) @ x.abs()
+    near("dhidden", dh, want, allowed + 2.0 ** -7.9 * want.abs())
+
+
+def test_top_logits_past_32_bits_of_bytes(env):
+    torch, P = env["torch"], env["P"]
+    n, v = 2200, 1 << 20
+    x = torch.empty(n, v, dtype=torch.bfloat16, device="cuda")
+    x.normal_(generator=torch.Generator(device="cuda").manual_seed(7))
+    got = top(P, torch, x, 32)
+    for r in (0, 1023, 1024, 2047, 2048, n - 1):
+        one = top(P, torch, x[r:r + 1].clone(), 32)
+        for a, b in zip(got[:2], one[:2]):
+            assert torch.equal(a[r:r + 1], b), r
+        # (a row alone is cut into other segments, and its sum runs in another order)
+        assert abs(float(got[2][r]) - float(one[2][0])) <= 2 * (2.0 ** -16 + 4 * U * 15)
+    check_top(P, torch, x[n - 2:].clone(), 32)
 
 
 def test_spread_logits(env):
