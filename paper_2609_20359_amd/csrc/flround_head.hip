@@ -805,26 +805,42 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     }
     return;
   }
-  for (int k = w; k < a.K; k += 4) {
-    const int64_t id = a.labels ? a.labels[t] : a.ids[t * a.K + k];
-    float s = 0.f;
-    if (id >= a.V) {
-      s = NAN;
-    } else if (id >= 0) {
-      const uint16_t* r = a.weight + id * a.ldw;
-      for (int64_t d = l * 8; d < a.D; d += 512) {
-        const u32x4 x = row_chunk(h, d, a.D);
-        const u32x4 y = row_chunk(r, d, a.D);
+  // four listed words of a wave at a time, so that enough loads are out
+  for (int k0 = w * 4; k0 < a.K; k0 += 16) {
+    int64_t id[4];
+    const uint16_t* r[4];
+    float s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      id[i] = k0 + i < a.K ? (a.labels ? a.labels[t] : a.ids[t * a.K + k0 + i]) : -1;
+      s[i] = 0.f;
+      // the others' products, with row 0, are not used
+      r[i] = a.weight + (id[i] >= 0 && id[i] < a.V ? id[i] : 0) * a.ldw;
+    }
+    const int n = a.K - k0 < 4 ? a.K - k0 : 4;
+    for (int64_t d = l * 8; d < a.D; d += 512) {
+      const u32x4 x = row_chunk(h, d, a.D);
+      u32x4 y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < n) y[i] = row_chunk(r[i], d, a.D);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i >= n) break;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s = __builtin_fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
-          s = __builtin_fmaf(__uint_as_float(x[e] & 0xFFFF0000u),
-                             __uint_as_float(y[e] & 0xFFFF0000u), s);
+          s[i] = __builtin_fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[i][e] << 16), s[i]);
+          s[i] = __builtin_fmaf(__uint_as_float(x[e] & 0xFFFF0000u),
+                                __uint_as_float(y[i][e] & 0xFFFF0000u), s[i]);
         }
       }
-      s = wave_sum(s);
     }
-    if (l == 0) a.target[t * a.K + k] = s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i >= n) break;
+      const float z = wave_sum(s[i]);
+      if (l == 0) a.target[t * a.K + k0 + i] = id[i] >= a.V ? NAN : id[i] >= 0 ? z : 0.f;
+    }
   }
 }
 
