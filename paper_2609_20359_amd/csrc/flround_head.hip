@@ -728,6 +728,7 @@ __device__ __forceinline__ bool is_live(const HeadArgs& a, int64_t t) {
 // tiles hold these logits too, but looking for them there took as long and cost
 // the loss of labels registers.
 constexpr int kScan = 1024;
+constexpr int kPackWords = 16;   // listed words of a workgroup
 
 template <bool GRAD, bool SCAN>
 __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
@@ -761,7 +762,7 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     scale = top > 0.f ? top : 1.f;
     q = t < a.T && is_live(a, t) ? before_[0] + before_[1] + before_[2] + before_[3] : -1;
     if (tid == 0 && q >= 0) a.rows[q] = (int32_t)t;
-    if (tid == 0 && t == a.T) {
+    if (tid == 0 && t == a.T && blockIdx.y == 0) {
       a.hdr->n_live = n;
       a.hdr->scale = scale;
       for (int i = 0; i < 4; ++i) a.hdr->zero[i] = 0;
@@ -771,13 +772,16 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     scale = a.hdr->scale;
     q = t < a.T ? a.pos[t] : -1;
   }
+  // (a workgroup of each token's words; the first has the rest to do, too)
+  const bool words_only = !GRAD && blockIdx.y > 0;
   if (t >= a.T) {
     const int64_t r = n + (t - a.T);
-    if (r >= (int64_t)(n + kRowPad - 1) / kRowPad * kRowPad) return;
+    if (words_only || r >= (int64_t)(n + kRowPad - 1) / kRowPad * kRowPad) return;
     for (int64_t d = tid * 8; d < a.Dp; d += 2048) *reinterpret_cast<u32x4*>(a.hc + r * a.Dp + d) = zero;
     return;
   }
   if (q < 0) {
+    if (words_only) return;
     if (GRAD) {
       for (int64_t d = tid; d < a.D; d += 256) a.dhidden[t * a.D + d] = 0;
     } else {
@@ -788,8 +792,9 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
   }
   const uint16_t* h = a.hidden + t * a.ldh;
   uint16_t* hc = a.hc + q * a.Dp;
-  for (int64_t d = tid * 8; d < a.Dp; d += 2048)
-    *reinterpret_cast<u32x4*>(hc + d) = row_chunk(h, d, a.D);
+  if (!words_only)
+    for (int64_t d = tid * 8; d < a.Dp; d += 2048)
+      *reinterpret_cast<u32x4*>(hc + d) = row_chunk(h, d, a.D);
   if (GRAD) {
     if (tid == 0) {
       const float ratio = a.dloss[t] / scale, lse = a.lse_in[t];
@@ -805,8 +810,9 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     }
     return;
   }
-  // four listed words of a wave at a time, so that enough loads are out
-  for (int k0 = w * 4; k0 < a.K; k0 += 16) {
+  // four listed words to a wave, so that enough loads are out
+  const int k0 = blockIdx.y * kPackWords + w * 4;
+  if (k0 < a.K) {
     int64_t id[4];
     const uint16_t* r[4];
     float s[4];
@@ -985,7 +991,7 @@ hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_head_pack(const HeadArgs& a, bool grad, hipStream_t st) {
-  const unsigned grid = (unsigned)(a.T + kRowPad);
+  const dim3 grid((unsigned)(a.T + kRowPad), grad ? 1 : (a.K + kPackWords - 1) / kPackWords);
   if (a.T <= kScan) {
     if (grad) k_pack<true, true><<<grid, 256, 0, st>>>(a);
     else k_pack<false, true><<<grid, 256, 0, st>>>(a);
