@@ -483,7 +483,7 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *   with p = exp(logp): the divergence of the student from the teacher, over the
  *   listed words.  ids: device, T x k int32; an entry < 0 is absent, whatever
  *   its teacher logit; one >= V gives NaN; a repeated one counts each time.  A
- *   teacher logit of -inf has probability 0.  A token with no entry that is
+ *   teacher logit of -inf has probability 0, one of NaN gives NaN.  A token with no entry that is
  *   present and above -inf takes no part.  teacher: T x k floats; teacher_lse:
  *   T floats at the same tau (fl_top_logits gives it) or NULL.  1 <= k <=
  *   FL_MAX_TARGETS; tau finite, > 0.

@@ -35,19 +35,18 @@ typedef u32x4 u32x4_at2 __attribute__((aligned(2)));   // on an element's bounda
 #define GLOBAL_SPACE __attribute__((address_space(1)))
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 __device__ __forceinline__ uint16_t to_bf16(float x) { return (uint16_t)pack2(x, 0.f); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
-// (m, s) stands for s 2^m; a part of nothing is (-inf, 0).
-__device__ __forceinline__ void join(float& m, float& s, float pm, float ps) {
+// (m, s) stands for s exp(m / tau), s2 being log2(e) / tau; a part of nothing is
+// (-inf, 0).
+__device__ __forceinline__ void join(float& m, float& s, float pm, float ps, float s2) {
   const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
-  s = s * exp2_(m - ref) + ps * exp2_(pm - ref);
+  s = s * exp2_((m - ref) * s2) + ps * exp2_((pm - ref) * s2);
   m = top;
 }
 
@@ -431,9 +430,9 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
         for (int i = 0; i < FP; ++i)
           m = fmaxf(fmaxf(fmaxf(m, acc[i][j][0]), fmaxf(acc[i][j][1], acc[i][j][2])), acc[i][j][3]);
         m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32)) * a.s2;
+        m = fmaxf(m, __shfl_xor(m, 32));
         // a row of which nothing is there, or only -inf, sums to 0
-        const float ref = m == -INFINITY ? 0.f : m;
+        const float ref = m == -INFINITY ? 0.f : m * a.s2;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < FP; ++i)
@@ -441,14 +440,16 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
           for (int e = 0; e < 4; ++e) sum += exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -ref));
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (l < 16) folded[wp][(wq * FQ + j) * 16 + l] = make_float2(m, sum);
+        // the sum is over exp(z / tau - ref), and ref is rounded: m's is 2^-rest of it
+        const float rest = m == -INFINITY ? 0.f : __builtin_fmaf(m, a.s2, -ref);
+        if (l < 16) folded[wp][(wq * FQ + j) * 16 + l] = make_float2(m, sum * exp2_(-rest));
       }
       __syncthreads();
       // (The next write here is a tile's steps and their meetings away.)
       if (tid < BQ) {
         float2 p = folded[0][tid];
 #pragma unroll
-        for (int i = 1; i < WP; ++i) join(p.x, p.y, folded[i][tid].x, folded[i][tid].y);
+        for (int i = 1; i < WP; ++i) join(p.x, p.y, folded[i][tid].x, folded[i][tid].y, a.s2);
         a.parts[(int64_t)my_tp * a.parts_ld + q0 + tid] = p;
       }
     } else if constexpr (EPI == kGrad) {
@@ -611,8 +612,8 @@ __device__ __forceinline__ float wave_max(float x) {
 // None of these takes more than 25 us at 4096 tokens, but k_pack where many words
 // are listed.
 
-// The teacher's log probabilities of the listed words, one wave per token.  An
-// entry with a negative id, or of a teacher logit of -inf, has probability 0; a
+// The teacher's log probabilities of the listed words, one wave per token.  NaN,
+// or an id past the vocabulary, makes the token's loss NaN.  An entry with a negative id, or of a teacher logit of -inf, has probability 0; a
 // token without any other takes no part.
 __global__ __launch_bounds__(256) void k_teacher(const HeadArgs a) {
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -627,23 +628,23 @@ __global__ __launch_bounds__(256) void k_teacher(const HeadArgs a) {
     if (k < a.K) {
       const int32_t id = a.ids[t * a.K + k];
       if (id >= 0) x[h] = a.teacher[t * a.K + k] / a.tau;
-      bad |= id >= a.V;
+      bad |= id >= a.V || x[h] != x[h];
     }
   }
   bad = __any(bad);
-  float ref;
+  // log p = (x - ref) - rest: in this order no digits of a small log p are lost
+  float ref, rest = 0.f;
   if (a.teacher_lse) {
     ref = a.teacher_lse[t];
   } else {
-    const float m = wave_max(fmaxf(x[0], x[1]));
-    const float s = wave_sum(m == -INFINITY ? 0.f : expf(x[0] - m) + expf(x[1] - m));
-    ref = m + logf(s);   // NaN where an entry is NaN; -inf where nothing is listed
+    ref = wave_max(fmaxf(x[0], x[1]));
+    rest = logf(wave_sum(ref == -INFINITY ? 0.f : expf(x[0] - ref) + expf(x[1] - ref)));
   }
   const bool any = __any(!(x[0] == -INFINITY) || !(x[1] == -INFINITY)) && ref != -INFINITY;
   float mass = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const float lp = x[h] == -INFINITY ? -INFINITY : x[h] - ref;
+    const float lp = x[h] == -INFINITY ? -INFINITY : x[h] - ref - rest;
     mass += expf(lp);
     const int k = l + 64 * h;
     if (k < a.K) a.logp[t * a.K + k] = lp;
@@ -872,6 +873,7 @@ __global__ __launch_bounds__(1024) void k_finish(const HeadArgs a) {
   if (q0 >= n) return;
   const int c = tid % C;
   float m = -INFINITY, s = 0.f;
+  const float s2 = kLog2e / a.tau;
   if (q0 + c < n) {
     const float2* p = a.parts + q0 + c;
     int i = tid / C;
@@ -880,42 +882,45 @@ __global__ __launch_bounds__(1024) void k_finish(const HeadArgs a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[k] = p[(int64_t)(i + k * (1024 / C)) * a.rows_pad];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) join(m, s, x[k].x, x[k].y);
+      for (int k = 0; k < 4; ++k) join(m, s, x[k].x, x[k].y, s2);
     }
     for (; i < a.n_parts; i += 1024 / C) {
       const float2 x = p[(int64_t)i * a.rows_pad];
-      join(m, s, x.x, x.y);
+      join(m, s, x.x, x.y, s2);
     }
   }
 #pragma unroll
-  for (int d = C; d < 64; d <<= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  for (int d = C; d < 64; d <<= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d), s2);
   if (l < C) ms[l][w] = m, ss[l][w] = s;
   __syncthreads();
   if (w >= C || q0 + w >= n) return;
   m = l < 16 ? ms[w][l] : -INFINITY;
   s = l < 16 ? ss[w][l] : 0.f;
 #pragma unroll
-  for (int d = 8; d; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  for (int d = 8; d; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d), s2);
   m = __shfl(m, 0);
   s = __shfl(s, 0);
-  const float lse = (m + log2_(s)) * kLn2;
+  // A loss is a small difference of these: a row's last steps are in 64 bits.
+  const double lse = (double)m / (double)a.tau + log((double)s);
   const int64_t t = a.rows[q0 + w];
   if (a.labels) {
     if (l == 0) {
-      a.lse[t] = lse;
-      a.loss[t] = lse - a.target[t];
+      a.lse[t] = (float)lse;
+      a.loss[t] = (float)(lse - (double)a.target[t]);
     }
     return;
   }
-  float sum = 0.f;
+  double sum = 0.0;
   for (int k = l; k < a.K; k += 64) {
     const float lp = a.logp[t * a.K + k];
-    if (lp != -INFINITY) sum += expf(lp) * (lp - a.target[t * a.K + k] / a.tau + lse);
+    if (lp != -INFINITY)
+      sum += (double)expf(lp) * ((double)lp - (double)a.target[t * a.K + k] / (double)a.tau + lse);
   }
-  sum = wave_sum(sum);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
   if (l == 0) {
-    a.lse[t] = lse;
-    a.loss[t] = a.tau * a.tau * sum;
+    a.lse[t] = (float)lse;
+    a.loss[t] = (float)((double)a.tau * (double)a.tau * sum);
   }
 }
 

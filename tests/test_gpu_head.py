@@ -357,6 +357,33 @@ def test_labels_past_the_vocabulary_give_nan(env):
     assert torch.isnan(dh).all(1).tolist() == [False, True, False, False, False]
 
 
+@pytest.mark.parametrize("mass", [False, True])
+def test_teachers_odd_values(env, mass):
+    """A teacher logit of NaN gives NaN, even where the others are -inf; a
+    token whose listed words are all ruled out takes no part; teacher logits
+    far below 0 and probabilities down to 0 are as the definition has them."""
+    torch, P = env["torch"], env["P"]
+    c = Case(torch, 6, 300, 64, K=4, mass=mass, empty=0.0, seed=3)
+    c.ids = torch.arange(4, device="cuda", dtype=torch.int32).repeat(6, 1)
+    c.a = torch.tensor([[math.nan, -math.inf, -math.inf, -math.inf], [math.nan, 1.0, 2.0, 3.0],
+                        [-math.inf] * 4, [-1e30, 0.0, -200.0, 1.0], [-5000.0, -5001.0, -5002.0, -5003.0],
+                        [3.0, 2.0, 1.0, 0.0]], device="cuda")
+    if mass:
+        c.alse = torch.logsumexp(c.a.double(), 1).nan_to_num(nan=1.0).float()
+    loss, lse, target = c.forward(P)
+    assert torch.isnan(loss).tolist() == [True, True, False, False, False, False]
+    assert float(loss[2]) == 0.0 and float(lse[2]) == 0.0
+    z = c.h.double() @ c.w.double().t()
+    x = c.a[3:].double()
+    ref = c.alse[3:].double() if mass else torch.logsumexp(x, 1)
+    logp = x - ref[:, None]
+    full = torch.logsumexp(z[3:], 1)
+    want = (logp.exp() * (logp - z[3:, :4] + full[:, None])).sum(1)
+    # as in Case, with log p off by the rounding of x and of ref
+    off = 2 * c.z_off[3:] + 2.0 ** -16 + 4 * U * full.abs() + 64 * U * 5003
+    near("loss", loss[3:], want, off)
+
+
 @pytest.mark.parametrize("K", [0, 4])
 def test_gradient_against_differences(env, K):
     """sum(dloss * loss) along a direction, by the forward call on both sides,
