@@ -45,7 +45,7 @@ struct HeadArgs {
   int32_t* rows;                    // live row -> token
   int32_t* pos;                     // token -> live row, or -1
   float* logp;                      // T x K (distillation), -inf where nothing is listed
-  float* mass;                      // T (distillation): sum of p, NaN for a dead-on-arrival id
+  float* mass;                      // T (distillation): sum of p, NaN for an id past the vocabulary
   uint8_t* flag;                    // T (distillation): token takes part
   uint16_t* hc;                     // compacted hidden rows, Dp each
   uint16_t* wc;                     // weight rows of Dp each, or null: weight is used as it is
@@ -53,7 +53,7 @@ struct HeadArgs {
   float* row_coef;                  // gradient, per live row: dloss / scale * mass
   int32_t* row_label;               // gradient of the labels' loss, per live row: the label,
   float* row_spot;                  // and its entry of G
-  const float2* parts;              // per (part, live row): running maximum and sum
+  const float2* parts;              // per (p tile, live row): maximum, and sum of exp over it
   int n_parts;
   int64_t rows_pad;                 // T rounded up to kRowPad
 };

@@ -22,7 +22,6 @@ namespace flr {
 namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -206,11 +205,11 @@ enum Epilogue { kStats, kGrad, kSlab, kOut };
 // outputs takes 1.43 us.  4096 live rows, 128256 words, 4096 wide, in PFLOP/s:
 // 1.37 for the statistics, 1.24 for G (0.87 ms a piece of 32256 words), 1.26 for
 // dW (0.86 ms), 1.37 for dh (0.79 ms); the library's plain products of these
-// sizes run at 1.43, 1.48 and 1.60.  What G and dW lose is their stores: without
-// them dW takes 0.77 ms, as a CU's 128 KiB go out at once and the next tile's
-// second step waits for them.  2048 and fewer rows lose 10 to 15 % where the
-// weight comes from HBM in every round of tiles, a step's loads being one step
-// ahead.
+// sizes run at 1.43, 1.48 and 1.60.  What G and dW lose is the ends of their
+// tiles: without the stores dW takes 0.77 ms, with all on a few lines 0.80, as a
+// CU's 128 KiB go out at once and the next tile's first step waits for them.  2048
+// and fewer rows lose 10 to 15 % where the weight comes from HBM in every round of
+// tiles, a step's loads being one step ahead.
 //
 // Why these tiles: eight waves of 128 x 64 outputs read 96 KiB of LDS a step of
 // 64, a third of what LDS can give in that time, and keep their sums in 128
@@ -725,9 +724,9 @@ __device__ __forceinline__ bool is_live(const HeadArgs& a, int64_t t) {
 // (7 tokens x 1000 x 96: 18.5 us for 21.6).
 //
 // The listed words' rows are what takes time: 1000 tokens of 64 words are 0.52 GB
-// of the weight, 0.13 ms (4.0 TB/s), an eighth of the call.  The product's
-// tiles hold these logits too, but looking for them there took as long and cost
-// the loss of labels registers.
+// of the weight, 94 us (5.6 TB/s; 130 with one word at a time), a tenth of the
+// call.  The product's tiles hold these logits too, but looking for them there took
+// as long and cost the loss of labels registers.
 constexpr int kScan = 1024;
 constexpr int kPackWords = 16;   // listed words of a workgroup
 
@@ -959,7 +958,7 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
 }
 
 // The gradient of the hidden state from the splits' fp32 sums, added in order
-// (bound by memory: 4096 x 4096 of one split, 101 MB, in 17 us).
+// (bound by memory: 4096 x 4096 of one split, 101 MB, in 22 us).
 __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab, int64_t ld_slab,
                                             int bp, int bq, int fit, int max_splits,
                                             float out_scale) {
