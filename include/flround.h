@@ -482,11 +482,12 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *     loss[t] = tau^2 sum_j p[t][j] (logp[t][j] - target[t][j] / tau + lse[t])
  *   with p = exp(logp): the divergence of the student from the teacher, over the
  *   listed words.  ids: device, T x k int32; an entry < 0 is absent, whatever
- *   its teacher logit; one >= V gives NaN; a repeated one counts each time.  A
- *   teacher logit of -inf has probability 0, one of NaN gives NaN.  A token with no entry that is
- *   present and above -inf takes no part.  teacher: T x k floats; teacher_lse:
- *   T floats at the same tau (fl_top_logits gives it) or NULL.  1 <= k <=
- *   FL_MAX_TARGETS; tau finite, > 0.
+ *   its teacher logit; one >= V gives NaN, whatever its teacher logit; a repeated
+ *   one counts each time.  A teacher logit of -inf has probability 0, one of NaN
+ *   gives NaN.  A token with no entry that is present and above -inf, and none
+ *   >= V, takes no part.  teacher: T x k floats; teacher_lse: T floats at the
+ *   same tau (fl_top_logits gives it) or NULL.  1 <= k <= FL_MAX_TARGETS; tau
+ *   finite, > 0.
  *
  * fl_head_distill_grad -- its gradient, as fl_head_loss_grad with
  *     G[t][v] = dloss[t] tau (exp(z[t][v] / tau - lse[t]) sum_j p[t][j]

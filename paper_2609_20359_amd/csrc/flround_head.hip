@@ -612,8 +612,9 @@ __device__ __forceinline__ float wave_max(float x) {
 // are listed.
 
 // The teacher's log probabilities of the listed words, one wave per token.  NaN,
-// or an id past the vocabulary, makes the token's loss NaN.  An entry with a negative id, or of a teacher logit of -inf, has probability 0; a
-// token without any other takes no part.
+// or an id past the vocabulary, makes the token's loss NaN, by its mass.  An entry
+// with a negative id, or of a teacher logit of -inf, has probability 0; a token
+// without any other takes no part.
 __global__ __launch_bounds__(256) void k_teacher(const HeadArgs a) {
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int l = threadIdx.x & 63;
@@ -919,7 +920,8 @@ __global__ __launch_bounds__(1024) void k_finish(const HeadArgs a) {
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
   if (l == 0) {
     a.lse[t] = (float)lse;
-    a.loss[t] = (float)((double)a.tau * (double)a.tau * sum);
+    // (an id past the vocabulary is one also where the teacher rules the word out)
+    a.loss[t] = a.mass[t] != a.mass[t] ? NAN : (float)((double)a.tau * (double)a.tau * sum);
   }
 }
 

@@ -358,6 +358,23 @@ def test_labels_past_the_vocabulary_give_nan(env):
 
 
 @pytest.mark.parametrize("mass", [False, True])
+def test_words_past_the_vocabulary_give_nan_where_ruled_out(env, mass):
+    """An id past the vocabulary gives NaN, loss and gradient alike, also where
+    its teacher logit is -inf, beside other words and alone."""
+    torch, P = env["torch"], env["P"]
+    c = Case(torch, 5, 100, 64, K=3, mass=mass, empty=0.0, seed=5)
+    c.ids[1, 2], c.a[1, 2] = 100, -math.inf
+    c.ids[3] = torch.tensor([-1, 100, -1], device="cuda", dtype=torch.int32)
+    c.a[3] = -math.inf
+    loss, lse, target = c.forward(P)
+    odd = [False, True, False, True, False]
+    assert torch.isnan(loss).tolist() == odd
+    dh, _ = c.backward(P, lse, target)
+    assert torch.isnan(dh).all(1).tolist() == odd
+    assert torch.isnan(dh).any(1).tolist() == odd
+
+
+@pytest.mark.parametrize("mass", [False, True])
 def test_teachers_odd_values(env, mass):
     """A teacher logit of NaN gives NaN, even where the others are -inf; a
     token whose listed words are all ruled out takes no part; teacher logits
