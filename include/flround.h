@@ -472,7 +472,8 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *   peer gradient that fl_local_step takes for the head's segment.  Both are
  *   written, not added to.  G is made again for a piece of the vocabulary at a
  *   time and rounded to bf16 relative to the largest |dloss|, which leaves a
- *   relative error of up to 2^-8 per term beside that of rounding the results.
+ *   relative error of up to 2^-8 per term beside that of rounding the results
+ *   (2^-16 for up to 32 tokens).
  *   The workspace holds one piece of G (256 MiB, or 8192 words).
  *
  * fl_head_distill -- distillation from a teacher's top logits:

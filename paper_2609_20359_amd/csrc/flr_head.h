@@ -12,21 +12,30 @@ constexpr int kRowPad = 256;      // compacted rows are padded to this many
 constexpr int kStep = 64;         // elements of the summed axis a tile takes at a time
 constexpr int kMaxTargets = 128;  // listed teacher logits per token
 
+// The gradient of up to this many tokens has two rows for each: G rounded to bf16,
+// and what that leaves, rounded too.  A G of few tokens has few large entries, so
+// that one unlucky rounding (2^-9) is the error of a whole result; where they are
+// many, such errors are of both signs and all sizes.  The products' smallest tiles
+// have 64 rows, so the second row costs next to nothing.
+constexpr int kTwiceTokens = 32;
+
 // Written by the first kernel of a call.
 struct HeadHeader {
-  int32_t n_live;   // tokens that take part
+  int32_t n_live;   // rows of the tokens that take part
   float scale;      // largest finite |dloss| among them (1 where that is 0)
   int32_t pad[2];
   uint32_t zero[4]; // what a load past an operand's end reads
 };
 
 // Arguments of the small kernels around the products.  A token that takes
-// part is "live"; the q-th live token is row q of the compacted arrays.
+// part is "live"; the q-th live token is row q of the compacted arrays (rows 2 q and
+// 2 q + 1 where copies is 2).
 struct HeadArgs {
   int64_t T, V, D, Dp;              // Dp: row length of hc (and of wc), a multiple of kStep
   int64_t ldh, ldw;                 // elements between rows of hidden and of weight
   const uint16_t* hidden;
   const uint16_t* weight;
+  int copies;                       // compacted rows per token: 1, or 2 (kTwiceTokens)
   int K;                            // targets per token (1 for labels)
   float tau;
   const int64_t* labels;            // labels, or null:
@@ -81,6 +90,7 @@ struct TileArgs {
   int64_t p_first;                  // the word that p = 0 is
   uint16_t* G;
   int64_t ldg;                      // also the columns of G to write
+  int copies;                       // 2: odd rows hold what rounding left of the even ones
   float* slab;                      // fp32 sums: slab[split][live row][ld_slab]
   int64_t ld_slab;
   int add;                          // add to the slab

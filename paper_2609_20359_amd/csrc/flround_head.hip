@@ -39,6 +39,10 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 __device__ __forceinline__ uint16_t to_bf16(float x) { return (uint16_t)pack2(x, 0.f); }
+// What rounding to bf16 leaves of x.
+__device__ __forceinline__ float rest_of(float x) {
+  return x - __uint_as_float((uint32_t)to_bf16(x) << 16);
+}
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // (m, s) stands for s exp(m / tau), s2 being log2(e) / tau; a part of nothing is
@@ -481,6 +485,10 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (here && y == (i + h) * 16 + e) v[e] = spot;
+            if constexpr (BQ == 64)   // rows of up to kTwiceTokens tokens are one such tile's
+              if (a.copies == 2 && (l & 1))
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = rest_of(v[e]);
             d[h] = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
           }
           *reinterpret_cast<u32x4*>(g + i * 16) = eight(d[0], d[1]);
@@ -764,7 +772,7 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     q = t < a.T && is_live(a, t) ? before_[0] + before_[1] + before_[2] + before_[3] : -1;
     if (tid == 0 && q >= 0) a.rows[q] = (int32_t)t;
     if (tid == 0 && t == a.T && blockIdx.y == 0) {
-      a.hdr->n_live = n;
+      a.hdr->n_live = n * a.copies;
       a.hdr->scale = scale;
       for (int i = 0; i < 4; ++i) a.hdr->zero[i] = 0;
     }
@@ -776,8 +784,8 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
   // (a workgroup of each token's words; the first has the rest to do, too)
   const bool words_only = !GRAD && blockIdx.y > 0;
   if (t >= a.T) {
-    const int64_t r = n + (t - a.T);
-    if (words_only || r >= (int64_t)(n + kRowPad - 1) / kRowPad * kRowPad) return;
+    const int64_t rows = (int64_t)n * (SCAN ? a.copies : 1), r = rows + (t - a.T);
+    if (words_only || r >= (rows + kRowPad - 1) / kRowPad * kRowPad) return;
     for (int64_t d = tid * 8; d < a.Dp; d += 2048) *reinterpret_cast<u32x4*>(a.hc + r * a.Dp + d) = zero;
     return;
   }
@@ -792,12 +800,17 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     return;
   }
   const uint16_t* h = a.hidden + t * a.ldh;
-  uint16_t* hc = a.hc + q * a.Dp;
+  const int copies = GRAD && SCAN ? a.copies : 1;
+  uint16_t* hc = a.hc + q * copies * a.Dp;
   if (!words_only)
-    for (int64_t d = tid * 8; d < a.Dp; d += 2048)
-      *reinterpret_cast<u32x4*>(hc + d) = row_chunk(h, d, a.D);
+    for (int64_t d = tid * 8; d < a.Dp; d += 2048) {
+      const u32x4 x = row_chunk(h, d, a.D);
+      *reinterpret_cast<u32x4*>(hc + d) = x;
+      if (copies == 2) *reinterpret_cast<u32x4*>(hc + a.Dp + d) = x;
+    }
   if (GRAD) {
-    if (tid == 0) {
+    if (tid < copies) {
+      q = q * copies + tid;
       const float ratio = a.dloss[t] / scale, lse = a.lse_in[t];
       a.row_lse2[q] = lse * kLog2e;
       if (a.labels) {
@@ -933,7 +946,7 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
                                              int64_t v1) {
   const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int l = threadIdx.x & 63;
-  if (q >= a.hdr->n_live) return;
+  if (q >= a.hdr->n_live / a.copies) return;
   const int64_t t = a.rows[q];
   const float ratio = a.dloss[t] / a.hdr->scale;
   const float mass = a.mass[t], lse = a.lse_in[t];
@@ -954,7 +967,10 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
     }
     if (id >= v0 && id < v1) {
       const float z = a.target_in[t * a.K + k];
-      G[q * ldg + (id - v0)] = to_bf16(ratio * (mass * exp2_((z / a.tau - lse) * kLog2e) - p));
+      const float g = ratio * (mass * exp2_((z / a.tau - lse) * kLog2e) - p);
+      uint16_t* to = G + q * a.copies * ldg + (id - v0);
+      *to = to_bf16(g);
+      if (a.copies == 2) to[ldg] = to_bf16(rest_of(g));
     }
   }
 }
@@ -966,7 +982,7 @@ __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab,
                                             float out_scale) {
   // at most 2^20 rows of 2^15 elements: 2^25 chunks
   const int64_t n = a.hdr->n_live;
-  const unsigned chunks = (unsigned)((a.D + 1023) / 1024), all = (unsigned)n * chunks;
+  const unsigned chunks = (unsigned)((a.D + 1023) / 1024), all = (unsigned)(n / a.copies) * chunks;
   const int splits =
       splits_of(fit, (int)((a.D + bp - 1) / bp) * (int)((n + bq - 1) / bq), max_splits);
   const float f = a.hdr->scale * out_scale;
@@ -974,10 +990,17 @@ __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab,
   for (unsigned b = blockIdx.x; b < all; b += gridDim.x) {
     const int64_t q = b / chunks, d = (b % chunks * 256 + threadIdx.x) * 4;
     if (d >= a.D) continue;
-    const float* p = slab + q * ld_slab + d;
+    const float* p = slab + q * a.copies * ld_slab + d;
     f32x4 s = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
     for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4*>(p + i * (n * ld_slab));
+    if (a.copies == 2) {
+      f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+      for (int i = 0; i < splits; ++i)
+        r += *reinterpret_cast<const f32x4*>(p + ld_slab + i * (n * ld_slab));
+      s += r;
+    }
     s *= f;
     uint16_t* o = a.dhidden + (int64_t)a.rows[q] * a.D + d;
     if (vec) {

@@ -45,15 +45,15 @@ int shape_for(int64_t np, int64_t nq, bool few_rows) {
 }
 
 struct Plan {
-  int64_t T, V, D, Dp, rows_pad;
-  int K;
+  int64_t T, V, D, Dp, rows, rows_pad;   // rows: compacted ones, of all tokens
+  int copies, K;
   bool grad, distill, pack_w;
   int logits_shape, dh_shape, dw_shape;
   int n_parts, max_splits;
   int64_t slab_rows;
   int64_t piece, n_pieces;
   // byte offsets into the workspace
-  size_t hdr, rows, pos, logp, mass, flag, hc, wc, parts, row_lse2, row_coef, row_label, row_spot, G, slab, bytes;
+  size_t hdr, live, pos, logp, mass, flag, hc, wc, parts, row_lse2, row_coef, row_label, row_spot, G, slab, bytes;
 };
 
 Plan plan_for(const fl_head_shape& s, int K, bool grad) {
@@ -64,7 +64,9 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   p.K = K > 0 ? K : 1;
   p.grad = grad, p.distill = K > 0, p.pack_w = pack_w;
   p.Dp = round_up(p.D, kStep);
-  p.rows_pad = round_up(p.T, kRowPad);
+  p.copies = grad && p.T <= kTwiceTokens ? 2 : 1;
+  p.rows = p.T * p.copies;
+  p.rows_pad = round_up(p.rows, kRowPad);
   p.piece = p.V;
   p.n_pieces = 1;
   if (grad && p.T > 0) {
@@ -73,7 +75,7 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
     p.piece = round_up(ceil_div(p.V, p.n_pieces), 256);
     p.n_pieces = ceil_div(p.V, p.piece);
   }
-  p.logits_shape = shape_for(p.piece, p.T, true);
+  p.logits_shape = shape_for(p.piece, p.rows, true);
   if (grad && p.logits_shape == kTile16) p.logits_shape = kTile64;   // G is read 64 rows at a time
   p.n_parts = (int)ceil_div(p.V, tile_p(p.logits_shape));
   // Large tiles where there are enough of them, with eight steps each.
@@ -87,9 +89,9 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   // the chip, four steps at least to a split.  How many tiles there are depends
   // on the live rows, and the rows of all splits are at most the chip's share.
   p.max_splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(p.piece, kStep) / 4, 64));
-  p.slab_rows = std::max(p.T, tile_fit(p.dh_shape) * tile_q(p.dh_shape) /
+  p.slab_rows = std::max(p.rows, tile_fit(p.dh_shape) * tile_q(p.dh_shape) /
                                   ceil_div(p.D, tile_p(p.dh_shape)));
-  p.slab_rows = std::min(p.slab_rows, p.T * p.max_splits);
+  p.slab_rows = std::min(p.slab_rows, p.rows * p.max_splits);
 
   size_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -98,7 +100,7 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
     return o;
   };
   p.hdr = take(sizeof(HeadHeader));
-  p.rows = take(4 * p.T);
+  p.live = take(4 * p.T);
   p.pos = take(4 * p.T);
   if (p.distill) {
     p.logp = take(4 * p.T * p.K);
@@ -183,11 +185,11 @@ struct Call {
     a.T = p.T, a.V = p.V, a.D = p.D, a.Dp = p.Dp;
     a.ldh = ldh, a.ldw = ldw;
     a.hidden = hidden, a.weight = weight;
-    a.K = p.K, a.tau = t.K ? t.tau : 1.f;
+    a.copies = p.copies, a.K = p.K, a.tau = t.K ? t.tau : 1.f;
     a.labels = t.K ? nullptr : t.labels;
     a.ids = t.ids, a.teacher = t.teacher, a.teacher_lse = t.teacher_lse;
     a.hdr = at<HeadHeader>(p.hdr);
-    a.rows = at<int32_t>(p.rows), a.pos = at<int32_t>(p.pos);
+    a.rows = at<int32_t>(p.live), a.pos = at<int32_t>(p.pos);
     if (p.distill) {
       a.logp = at<float>(p.logp), a.mass = at<float>(p.mass), a.flag = at<uint8_t>(p.flag);
     }
@@ -221,7 +223,7 @@ struct Call {
     TileArgs g{};
     g.P = weight_rows(v0), g.ldp = weight_ld();
     g.Q = a.hc, g.ldq = p.Dp;
-    g.np = v1 - v0, g.nq = p.T, g.nk = a.wc ? p.Dp : p.D;
+    g.np = v1 - v0, g.nq = p.rows, g.nk = a.wc ? p.Dp : p.D;
     g.hdr = a.hdr, g.live_q = 1, g.zero = reinterpret_cast<const uint16_t*>(a.hdr->zero);
     g.s2 = (float)(1.4426950408889634 / (double)a.tau);
     return g;
@@ -283,7 +285,7 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
       g.row_lse2 = c.a.row_lse2, g.row_coef = c.a.row_coef;
       g.row_label = p.distill ? nullptr : c.a.row_label, g.row_spot = c.a.row_spot;
       g.p_first = v0;
-      g.G = G, g.ldg = ldg;
+      g.G = G, g.ldg = ldg, g.copies = p.copies;
       if ((rc = status_of(launch_logits_grad(g, p.logits_shape, c.st))) != FL_OK) return rc;
       if (p.distill && (rc = status_of(launch_head_fix(c.a, G, ldg, v0, v1, c.st))) != FL_OK)
         return rc;
@@ -301,7 +303,7 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
     if (p.T > 0) {
       h.P = c.weight_rows(v0), h.ldp = c.weight_ld();
       h.Q = G, h.ldq = ldg;
-      h.np = p.D, h.nq = p.T, h.live_q = 1, h.nk = v1 - v0;
+      h.np = p.D, h.nq = p.rows, h.live_q = 1, h.nk = v1 - v0;
       h.hdr = c.a.hdr, h.zero = reinterpret_cast<const uint16_t*>(c.a.hdr->zero);
       h.slab = slab, h.ld_slab = p.Dp;
       h.add = v0 > 0, h.max_splits = p.max_splits;
