@@ -153,7 +153,10 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
   for (int i = 1; i < kWaves; ++i) m = fmaxf(m, wave_m[i]);
   float s = 0.f;
   const float ref = m == -INFINITY ? 0.f : m, ref2 = ref * a.s2;
-  const bool overflow = !(fabsf(ref2) < INFINITY);   // of the scaled maximum
+  // The scaled maximum is rounded, by up to 1/2 where it is 2^24 and by 2^103 in a row
+  // of the type's lowest values: from there on (or where it overflows) the difference
+  // is taken first.
+  const bool far = !(fabsf(ref2) < 0x1p24f);
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     // The values are taken from the registers anew: kept, they would be twice
@@ -161,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
     asm volatile("" : "+v"(d[c]));
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      s += exp2_(overflow ? (value(c, e) - ref) * a.s2 : __builtin_fmaf(value(c, e), a.s2, -ref2));
+      s += exp2_(far ? (value(c, e) - ref) * a.s2 : __builtin_fmaf(value(c, e), a.s2, -ref2));
   }
   const bool odd = s != s;   // a NaN among them, or infinities: no chunk is left out
 #pragma unroll
