@@ -497,8 +497,9 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *
  * fl_top_logits -- the k largest of each row of logits, largest first, ties to
  *   the lowest id, and lse[row] = log sum_v exp(logits[row][v] / tau) (lse may
- *   be NULL).  logits: rows x vocab of dtype FL_BF16 or FL_F32, `stride`
- *   elements between rows (0: vocab).  NaN counts as larger than any number,
+ *   be NULL; +inf for a row with a logit of +inf, NaN for one with NaN).  logits:
+ *   rows x vocab of dtype FL_BF16 or FL_F32, `stride` elements between rows (0:
+ *   vocab).  NaN counts as larger than any number,
  *   -0 as 0.  values: rows x k floats; ids: rows x k int32.  1 <= k <=
  *   min(vocab, FL_MAX_TARGETS).  workspace: fl_top_workspace_bytes, NULL where
  *   that is 0.

@@ -51,12 +51,13 @@ __device__ __forceinline__ uint64_t entry(float x, int id) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
-// (m, s) stands for s exp(m / tau); nothing is (-inf, 0).  Differences are taken
-// before they are scaled: a row masked by the type's lowest value would
-// overflow the other way round.
+// (m, s) stands for s exp(m / tau); nothing is (-inf, 0), and a maximum of +inf has
+// an s > 0.  Differences are taken before they are scaled: a row masked by the type's
+// lowest value would overflow the other way round.  The maximum itself counts whole:
+// infinities have no difference.
 __device__ __forceinline__ void join(float& m, float& s, float pm, float ps, float s2) {
-  const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
-  s = s * exp2_((m - ref) * s2) + ps * exp2_((pm - ref) * s2);
+  const float top = fmaxf(m, pm);
+  s = s * (m == top ? 1.f : exp2_((m - top) * s2)) + ps * (pm == top ? 1.f : exp2_((pm - top) * s2));
   m = top;
 }
 __device__ __forceinline__ float lse_of(float m, float s, const TopArgs& a) {
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
 #pragma unroll
   for (int i = 1; i < kWaves; ++i) m = fmaxf(m, wave_m[i]);
   float s = 0.f;
-  const float ref = m == -INFINITY ? 0.f : m, ref2 = ref * a.s2;
+  const float ref = fabsf(m) == INFINITY ? 0.f : m, ref2 = ref * a.s2;
   // The scaled maximum is rounded, by up to 1/2 where it is 2^24 and by 2^103 in a row
   // of the type's lowest values: from there on (or where it overflows) the difference
   // is taken first.
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
     for (int e = 0; e < E; ++e)
       s += exp2_(far ? (value(c, e) - ref) * a.s2 : __builtin_fmaf(value(c, e), a.s2, -ref2));
   }
-  const bool odd = s != s;   // a NaN among them, or infinities: no chunk is left out
+  const bool odd = s != s;   // a NaN among them: no chunk is left out
 #pragma unroll
   for (int x = 32; x; x >>= 1) s += __shfl_xor(s, x);
   if (l == 0) wave_s[w] = s;
@@ -237,6 +238,7 @@ __global__ __launch_bounds__(kThreads) void k_top_segment(const TopArgs a) {
   if (tid == 0) {
     s = 0.f;
     for (int i = 0; i < kWaves; ++i) s += wave_s[i];
+    if (m == INFINITY && s > 0.f) s = 1.f;   // (a NaN stays)
     if (!last) a.parts[row * a.segs + seg] = make_float2(m, s);
     else if (a.lse) a.lse[row] = lse_of(m, s, a);
   }

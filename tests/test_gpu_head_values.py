@@ -79,3 +79,26 @@ def test_top_lse_of_rows_far_from_zero(env, tau, dtype):
         x[:, 1] = -math.inf
         x[:, 2] = torch.finfo(dt).min
         check_top(P, torch, x, 3, tau)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [6, 700, 40001])
+def test_top_lse_of_rows_with_infinities(env, vocab, dtype):
+    """+inf among the logits gives +inf, NaN gives NaN beside anything, and a
+    row of -inf alone gives -inf."""
+    torch, P = env["torch"], env["P"]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(vocab)
+    x = torch.randn(8, vocab, generator=g, device="cuda").to(
+        torch.bfloat16 if dtype == "bf16" else torch.float32)
+    x[0, vocab - 1] = math.inf
+    x[1, 0] = x[1, vocab // 2] = x[1, vocab - 2] = math.inf
+    x[2] = math.inf
+    x[3] = -math.inf
+    x[3, 4] = math.inf
+    x[4, 1], x[4, vocab - 1] = math.inf, math.nan
+    x[5, 3] = math.nan
+    x[6] = -math.inf
+    x[7, ::2] = -math.inf
+    for tau in (1.0, 2.0):
+        check_top(P, torch, x, 4, tau)
