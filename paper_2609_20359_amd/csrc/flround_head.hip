@@ -434,18 +434,18 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
           m = fmaxf(fmaxf(fmaxf(m, acc[i][j][0]), fmaxf(acc[i][j][1], acc[i][j][2])), acc[i][j][3]);
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        // a row of which nothing is there, or only -inf, sums to 0
-        const float ref = m == -INFINITY ? 0.f : m * a.s2;
+        // A row of which nothing is there, or only -inf, sums to 0.  The difference
+        // is taken before it is scaled: the scaled maximum's rounding is more than an
+        // exponent holds from 2^32 on.
+        const float ref = m == -INFINITY ? 0.f : m;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum += exp2_(__builtin_fmaf(acc[i][j][e], a.s2, -ref));
+          for (int e = 0; e < 4; ++e) sum += exp2_((acc[i][j][e] - ref) * a.s2);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        // the sum is over exp(z / tau - ref), and ref is rounded: m's is 2^-rest of it
-        const float rest = m == -INFINITY ? 0.f : __builtin_fmaf(m, a.s2, -ref);
-        if (l < 16) folded[wp][(wq * FQ + j) * 16 + l] = make_float2(m, sum * exp2_(-rest));
+        if (l < 16) folded[wp][(wq * FQ + j) * 16 + l] = make_float2(m, sum);
       }
       __syncthreads();
       // (The next write here is a tile's steps and their meetings away.)

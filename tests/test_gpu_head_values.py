@@ -102,3 +102,45 @@ def test_top_lse_of_rows_with_infinities(env, vocab, dtype):
     x[7, ::2] = -math.inf
     for tau in (1.0, 2.0):
         check_top(P, torch, x, 4, tau)
+
+
+# ---- the head's statistics -----------------------------------------------------
+
+# (tokens, words): each of the four tiles of the statistics
+TILES = [(5, 300), (40, 300), (100, 500), (256, 66000)]
+
+
+def forward(P, torch, h, w, labels):
+    T = h.shape[0]
+    out = [torch.full((T,), -7.0, device="cuda") for _ in range(3)]
+    P.fl_head_loss(h, w, labels, *out)
+    return out
+
+
+@pytest.mark.parametrize("T,V", TILES)
+def test_logits_far_from_zero(env, T, V):
+    """A token's logits are a power of two, up to 2^110 and of both signs, times
+    small whole numbers: every one is exact, and so is what is expected."""
+    torch, P = env["torch"], env["P"]
+    D = 16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    power = torch.randint(-4, 111, (T,), generator=g, device="cuda").double()
+    h = torch.zeros(T, D, device="cuda", dtype=torch.bfloat16)
+    sign = torch.randint(0, 2, (T,), generator=g, device="cuda").double() * 2 - 1
+    h[:, 0] = (2.0 ** power * sign).bfloat16()
+    w = torch.zeros(V, D, device="cuda", dtype=torch.bfloat16)
+    w[:, 0] = torch.randint(-100, 101, (V,), generator=g, device="cuda").bfloat16()
+    labels = torch.randint(0, V, (T,), generator=g, device="cuda")
+    labels[::2] = torch.where(sign[::2] > 0, w[:, 0].float().argmax(), w[:, 0].float().argmin())
+    z = h[:, :1].double() @ w[:, :1].double().t()
+    lse = torch.logsumexp(z, 1)
+    at = z.gather(1, labels[:, None])[:, 0]
+    # (as a difference from the maximum: lse in 64 bits has lost the sum's logarithm)
+    m = z.amax(1)
+    want = torch.log(torch.exp(z - m[:, None]).sum(1)) + (m - at)
+    loss, got, target = forward(P, torch, h, w, labels)
+    same(torch, "lse", got, lse, 2.0 ** -16 + 4 * U * lse.abs())
+    same(torch, "target", target, at, 0.0 * at)
+    # what the kernel's sum in 64 bits holds beside so large a maximum
+    same(torch, "loss", loss, want, 2.0 ** -16 + 2.0 ** -22 * want.abs() + 2.0 ** -50 * m.abs())
