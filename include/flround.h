@@ -462,7 +462,8 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *     loss[t] = lse[t] - target[t]
  *   labels: device, T int64.  A token with a negative label takes no part: its
  *   three results are 0 and its hidden state is not looked at.  A label >= V
- *   gives NaN.  lse and target are what the gradient needs.
+ *   gives NaN.  A logit of +inf makes lse +inf.  lse and target are what the
+ *   gradient needs.
  *
  * fl_head_loss_grad -- gradient of sum_t dloss[t] * loss[t]:
  *     G[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - (v == labels[t]))

@@ -46,10 +46,11 @@ __device__ __forceinline__ float rest_of(float x) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // (m, s) stands for s exp(m / tau), s2 being log2(e) / tau; a part of nothing is
-// (-inf, 0).
+// (-inf, 0), and a maximum of +inf has an s > 0.  The maximum itself counts whole:
+// infinities have no difference.
 __device__ __forceinline__ void join(float& m, float& s, float pm, float ps, float s2) {
-  const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
-  s = s * exp2_((m - ref) * s2) + ps * exp2_((pm - ref) * s2);
+  const float top = fmaxf(m, pm);
+  s = s * (m == top ? 1.f : exp2_((m - top) * s2)) + ps * (pm == top ? 1.f : exp2_((pm - top) * s2));
   m = top;
 }
 
@@ -437,7 +438,7 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
         // A row of which nothing is there, or only -inf, sums to 0.  The difference
         // is taken before it is scaled: the scaled maximum's rounding is more than an
         // exponent holds from 2^32 on.
-        const float ref = m == -INFINITY ? 0.f : m;
+        const float ref = fabsf(m) == INFINITY ? 0.f : m;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < FP; ++i)
@@ -445,6 +446,7 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
           for (int e = 0; e < 4; ++e) sum += exp2_((acc[i][j][e] - ref) * a.s2);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
+        if (m == INFINITY && sum > 0.f) sum = 1.f;   // (a NaN stays)
         if (l < 16) folded[wp][(wq * FQ + j) * 16 + l] = make_float2(m, sum);
       }
       __syncthreads();

@@ -144,3 +144,33 @@ def test_logits_far_from_zero(env, T, V):
     same(torch, "target", target, at, 0.0 * at)
     # what the kernel's sum in 64 bits holds beside so large a maximum
     same(torch, "loss", loss, want, 2.0 ** -16 + 2.0 ** -22 * want.abs() + 2.0 ** -50 * m.abs())
+
+
+@pytest.mark.parametrize("T,V", TILES)
+def test_infinite_logits(env, T, V):
+    """A logit of +inf gives an lse and a loss of +inf, one of -inf is a word of
+    no probability, NaN gives NaN."""
+    torch, P = env["torch"], env["P"]
+    D = 16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V)
+    h = torch.randn(T, D, generator=g, device="cuda").bfloat16()
+    h[h == 0] = 1.0
+    w = torch.randn(V, D, generator=g, device="cuda").bfloat16()
+    w[V - 3, 0] = math.inf
+    w[1, 0] = math.inf
+    h[3, 1] = math.nan
+    labels = torch.randint(2, V - 3, (T,), generator=g, device="cuda")
+    # each product by itself, in 64 bits, with the infinite ones put in by sign
+    clean = torch.where(torch.isfinite(w), w, 0.0).double()
+    z = h.double() @ clean.t()
+    for v in (V - 3, 1):
+        z[:, v] = torch.where(z[:, v].isnan(), math.nan, h[:, 0].double().sign() * math.inf)
+    lse = torch.logsumexp(z, 1)
+    at = z.gather(1, labels[:, None])[:, 0]
+    z_off = (D + 8) * U * (h.double().abs().nan_to_num(nan=0.0) @ clean.abs().t()).amax(1)
+    loss, got, target = forward(P, torch, h, w, labels)
+    assert bool(torch.isinf(lse).any()) and bool(torch.isfinite(lse).any())
+    off = z_off + 2.0 ** -16
+    same(torch, "lse", got, lse, off + 4 * U * lse.abs().nan_to_num(posinf=0.0))
+    same(torch, "loss", loss, lse - at, off + z_off + 2.0 ** -22 * (lse - at).abs().nan_to_num(posinf=0.0))
