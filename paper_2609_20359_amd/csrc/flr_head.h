@@ -60,7 +60,7 @@ struct HeadArgs {
   uint8_t* flag;                    // T (distillation): token takes part
   uint16_t* hc;                     // compacted hidden rows, Dp each
   uint16_t* wc;                     // weight rows of Dp each, or null: weight is used as it is
-  float* row_lse2;                  // gradient, per live row: lse * log2(e)
+  float* row_lse;                   // gradient, per live row: lse
   float* row_coef;                  // gradient, per live row: dloss / scale * mass
   int32_t* row_label;               // gradient of the labels' loss, per live row: the label,
   float* row_spot;                  // and its entry of G
@@ -85,7 +85,8 @@ struct TileArgs {
   float s2;                         // logits: log2(e) / tau
   float2* parts;                    // statistics
   int64_t parts_ld;
-  const float* row_lse2;            // gradient of the logits
+  float inv_tau;                    // gradient of the logits: 1 / tau
+  const float* row_lse;
   const float* row_coef;
   const int32_t* row_label;         // or null
   const float* row_spot;

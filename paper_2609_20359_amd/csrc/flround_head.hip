@@ -255,7 +255,7 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
   using OpP = typename S::OpP;
   using OpQ = typename S::OpQ;
   __shared__ float2 folded[EPI == kStats ? WP : 1][EPI == kStats ? BQ : 1];
-  __shared__ float row_lse2[EPI == kGrad ? BQ : 1], row_coef[EPI == kGrad ? BQ : 1];
+  __shared__ float row_lse[EPI == kGrad ? BQ : 1], row_coef[EPI == kGrad ? BQ : 1];
   __shared__ int row_label[EPI == kGrad ? BQ : 1];
 
   const int tid = threadIdx.x, l = tid & 63;
@@ -396,16 +396,16 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
     aim(more ? id + stride : id);
     // What the epilogue wants of its rows is asked for before the last steps and
     // passed through LDS between them, behind whose meeting it is there.
-    float lse2_in = 0.f, coef_in = 0.f;
+    float lse_in = 0.f, coef_in = 0.f;
     int label_in = -1;
     if (EPI == kGrad && tid < BQ && q0 + tid < n_live) {
-      lse2_in = a.row_lse2[q0 + tid];
+      lse_in = a.row_lse[q0 + tid];
       coef_in = a.row_coef[q0 + tid];
       if (a.row_label) label_in = a.row_label[q0 + tid];
     }
     step(sm0, sm1, [&](int i) { load_first(sm0, i, FP); });
     if (EPI == kGrad && tid < BQ) {
-      row_lse2[tid] = lse2_in;
+      row_lse[tid] = lse_in;
       row_coef[tid] = coef_in;
       row_label[tid] = label_in;
     }
@@ -463,7 +463,7 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
 #pragma unroll
       for (int j = 0; j < FQ; ++j, g += 16 * a.ldg) {
         const int r = (wq * FQ + j) * 16 + (l & 15);
-        const float lse2 = row_lse2[r], coef = row_coef[r];
+        const float lse = row_lse[r], coef = row_coef[r];
         // the label's place among this lane's, where one of the wave's rows has
         // it among the wave's
         const int64_t y = row_label[r] - a.p_first - pw;
@@ -476,9 +476,11 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float v[4];
+            // (lse is taken off before the scaling to base 2: of a large lse the
+            // scaled value's rounding would be a factor of the softmax)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              v[e] = coef * exp2_(__builtin_fmaf(acc[i + h][j][e], a.s2, -lse2));
+              v[e] = coef * exp2_(__builtin_fmaf(acc[i + h][j][e], a.inv_tau, -lse) * kLog2e);
             if (!inside)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
@@ -814,7 +816,7 @@ __global__ __launch_bounds__(256) void k_pack(const HeadArgs a) {
     if (tid < copies) {
       q = q * copies + tid;
       const float ratio = a.dloss[t] / scale, lse = a.lse_in[t];
-      a.row_lse2[q] = lse * kLog2e;
+      a.row_lse[q] = lse;
       if (a.labels) {
         const int64_t y = a.labels[t];
         a.row_coef[q] = y < a.V ? ratio : NAN;

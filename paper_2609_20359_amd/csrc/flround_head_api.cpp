@@ -53,7 +53,7 @@ struct Plan {
   int64_t slab_rows;
   int64_t piece, n_pieces;
   // byte offsets into the workspace
-  size_t hdr, live, pos, logp, mass, flag, hc, wc, parts, row_lse2, row_coef, row_label, row_spot, G, slab, bytes;
+  size_t hdr, live, pos, logp, mass, flag, hc, wc, parts, row_lse, row_coef, row_label, row_spot, G, slab, bytes;
 };
 
 Plan plan_for(const fl_head_shape& s, int K, bool grad) {
@@ -110,7 +110,7 @@ Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   p.hc = take(2 * p.rows_pad * p.Dp);
   if (pack_w) p.wc = take(2 * p.V * p.Dp);
   if (grad) {
-    p.row_lse2 = take(4 * p.rows_pad);
+    p.row_lse = take(4 * p.rows_pad);
     p.row_coef = take(4 * p.rows_pad);
     p.row_label = take(4 * p.rows_pad);
     p.row_spot = take(4 * p.rows_pad);
@@ -196,7 +196,7 @@ struct Call {
     a.hc = at<uint16_t>(p.hc);
     a.wc = p.pack_w ? at<uint16_t>(p.wc) : nullptr;
     if (grad) {
-      a.row_lse2 = at<float>(p.row_lse2), a.row_coef = at<float>(p.row_coef);
+      a.row_lse = at<float>(p.row_lse), a.row_coef = at<float>(p.row_coef);
       a.row_label = at<int32_t>(p.row_label), a.row_spot = at<float>(p.row_spot);
     }
     a.n_parts = p.n_parts;
@@ -282,7 +282,8 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
     const int64_t v1 = std::min(v0 + p.piece, p.V);
     if (p.T > 0) {
       TileArgs g = c.logits(v0, v1);
-      g.row_lse2 = c.a.row_lse2, g.row_coef = c.a.row_coef;
+      g.inv_tau = (float)(1.0 / (double)c.a.tau);
+      g.row_lse = c.a.row_lse, g.row_coef = c.a.row_coef;
       g.row_label = p.distill ? nullptr : c.a.row_label, g.row_spot = c.a.row_spot;
       g.p_first = v0;
       g.G = G, g.ldg = ldg, g.copies = p.copies;

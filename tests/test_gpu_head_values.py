@@ -174,3 +174,37 @@ def test_infinite_logits(env, T, V):
     off = z_off + 2.0 ** -16
     same(torch, "lse", got, lse, off + 4 * U * lse.abs().nan_to_num(posinf=0.0))
     same(torch, "loss", loss, lse - at, off + z_off + 2.0 ** -22 * (lse - at).abs().nan_to_num(posinf=0.0))
+
+
+@pytest.mark.parametrize("T,V", [(5, 300), (40, 300), (100, 500), (1030, 16500)])
+def test_gradient_of_logits_far_from_zero(env, T, V):
+    """Where one logit is far above the others, the softmax is 1 there and 0
+    elsewhere, however large the logits are; G and its products are whole
+    numbers times the tokens' weight."""
+    torch, P = env["torch"], env["P"]
+    D = 16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T + V)
+    h = torch.zeros(T, D, device="cuda", dtype=torch.bfloat16)
+    power = torch.randint(0, 100, (T,), generator=g, device="cuda").double()
+    h[:, 0] = (2.0 ** power).bfloat16()
+    h[:, 1:] = torch.randint(-3, 4, (T, D - 1), generator=g, device="cuda").bfloat16()
+    w = torch.zeros(V, D, device="cuda", dtype=torch.bfloat16)
+    w[:, 0] = torch.randint(-100, 1, (V,), generator=g, device="cuda").bfloat16() * 4
+    best = V // 2
+    w[best, 0] = 101.0
+    labels = torch.randint(0, V, (T,), generator=g, device="cuda")
+    labels[::3] = best
+    loss, lse, target = forward(P, torch, h, w, labels)
+    dl = torch.full((T,), 0.25, device="cuda")
+    dh = torch.full((T, D), -7.0, device="cuda", dtype=torch.bfloat16)
+    dw = torch.full((V, D), -7.0, device="cuda", dtype=torch.bfloat16)
+    P.fl_head_loss_grad(h, w, labels, lse, target, dl, dh, dw)
+    G = torch.zeros(T, V, device="cuda", dtype=torch.float64)
+    G[:, best] = 0.25
+    G[torch.arange(T, device="cuda"), labels] -= 0.25
+    for what, got, want, size in (("dhidden", dh, G @ w.double(), G.abs() @ w.double().abs()),
+                                  ("dweight", dw, G.t() @ h.double(), G.abs().t() @ h.double().abs())):
+        # sums in fp32, the results' rounding, and what is left of the other words
+        off = 2.0 ** -7.9 * want.abs() + (T + V) * U * size + math.exp(-500.0)
+        same(torch, what, got, want, off)
