@@ -639,24 +639,26 @@ __global__ __launch_bounds__(256) void k_teacher(const HeadArgs a) {
     x[h] = -INFINITY;
     if (k < a.K) {
       const int32_t id = a.ids[t * a.K + k];
-      if (id >= 0) x[h] = a.teacher[t * a.K + k] / a.tau;
+      if (id >= 0) x[h] = a.teacher[t * a.K + k];
       bad |= id >= a.V || x[h] != x[h];
     }
   }
   bad = __any(bad);
-  // log p = (x - ref) - rest: in this order no digits of a small log p are lost
-  float ref, rest = 0.f;
+  bool any = __any(!(x[0] == -INFINITY) || !(x[1] == -INFINITY));
+  // log p = (x - ref) / tau - rest: in this order no digits of a small log p are
+  // lost, and a logit at fp32's lowest value, finite as it is, does not overflow
+  float ref = 0.f, rest = 0.f;
   if (a.teacher_lse) {
-    ref = a.teacher_lse[t];
-  } else {
+    rest = a.teacher_lse[t];
+    any = any && rest != -INFINITY;
+  } else if (any) {
     ref = wave_max(fmaxf(x[0], x[1]));
-    rest = logf(wave_sum(ref == -INFINITY ? 0.f : expf(x[0] - ref) + expf(x[1] - ref)));
+    rest = logf(wave_sum(expf((x[0] - ref) / a.tau) + expf((x[1] - ref) / a.tau)));
   }
-  const bool any = __any(!(x[0] == -INFINITY) || !(x[1] == -INFINITY)) && ref != -INFINITY;
   float mass = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const float lp = x[h] == -INFINITY ? -INFINITY : x[h] - ref - rest;
+    const float lp = x[h] == -INFINITY ? -INFINITY : (x[h] - ref) / a.tau - rest;
     mass += expf(lp);
     const int k = l + 64 * h;
     if (k < a.K) a.logp[t * a.K + k] = lp;

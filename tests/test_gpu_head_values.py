@@ -208,3 +208,53 @@ def test_gradient_of_logits_far_from_zero(env, T, V):
         # sums in fp32, the results' rounding, and what is left of the other words
         off = 2.0 ** -7.9 * want.abs() + (T + V) * U * size + math.exp(-500.0)
         same(torch, what, got, want, off)
+
+
+# ---- the teacher ---------------------------------------------------------------
+
+
+def teacher_case(torch, P, a, alse, tau):
+    """Loss and gradients of len(a) tokens that list the first words."""
+    T, K = a.shape
+    V, D = 200, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(31)
+    h = torch.randn(T, D, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(V, D, generator=g, device="cuda") * 0.3).bfloat16()
+    ids = torch.arange(K, device="cuda", dtype=torch.int32).repeat(T, 1)
+    loss, lse = torch.full((T,), -7.0, device="cuda"), torch.full((T,), -7.0, device="cuda")
+    target = torch.full((T, K), -7.0, device="cuda")
+    dh = torch.full((T, D), -7.0, device="cuda", dtype=torch.bfloat16)
+    dw = torch.full((V, D), -7.0, device="cuda", dtype=torch.bfloat16)
+    P.fl_head_distill(h, w, ids, a, alse, tau, loss, lse, target)
+    dl = torch.full((T,), 0.25, device="cuda")
+    P.fl_head_distill_grad(h, w, ids, a, alse, tau, lse, target, dl, dh, dw)
+    z = h.double() @ w.double().t()
+    z_off = (D + 8) * U * (h.double().abs() @ w.double().abs().t()).amax(1)
+    return dict(h=h, w=w, z=z, z_off=z_off, dl=dl, loss=loss, lse=lse, dh=dh, dw=dw)
+
+
+@pytest.mark.parametrize("tau", [0.25, 0.5, 1.0, 2.0])
+def test_teachers_at_the_ends_of_the_range(env, tau):
+    """Teacher logits at fp32's lowest and largest value are finite: a token that
+    lists nothing else takes part, with the probabilities of the formula."""
+    torch, P = env["torch"], env["P"]
+    lo, hi = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+    a = torch.tensor([[lo, lo, lo, lo], [hi, lo, 0.0, hi], [lo, lo, -math.inf, lo], [hi, hi, hi, hi],
+                      [-math.inf, -math.inf, lo, -math.inf], [1.0, 2.0, 3.0, lo]], device="cuda")
+    c = teacher_case(torch, P, a, None, tau)
+    x = (a.double() - a.double().amax(1, keepdim=True)) / tau
+    logp = x - torch.logsumexp(x, 1, keepdim=True)
+    p = logp.exp()
+    full = torch.logsumexp(c["z"] / tau, 1)
+    terms = torch.where(p > 0, p * (logp - c["z"][:, :4] / tau + full[:, None]), 0.0)
+    off = tau * tau * (2 * c["z_off"] / tau + 2.0 ** -16 + 4 * U * full.abs() + 64 * U * 16)
+    same(torch, "loss", c["loss"], tau * tau * terms.sum(1), off)
+    same(torch, "lse", c["lse"], full, c["z_off"] / tau + 2.0 ** -16 + 4 * U * full.abs())
+    G = torch.exp(c["z"] / tau - full[:, None])
+    G[:, :4] -= p
+    G *= (c["dl"].double() * tau)[:, None]
+    want = G @ c["w"].double()
+    # 2^-8 of each entry of G for its rounding, as much again for the softmax's error
+    allowed = 2.0 ** -7 * (G.abs() @ c["w"].double().abs()) + 2.0 ** -7.9 * want.abs()
+    same(torch, "dhidden", c["dh"], want, allowed)
