@@ -487,8 +487,9 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *   its teacher logit; one >= V gives NaN, whatever its teacher logit; a repeated
  *   one counts each time.  A teacher logit of -inf has probability 0, one of NaN
  *   gives NaN.  A token with no entry that is present and above -inf, and none
- *   >= V, takes no part.  teacher: T x k floats; teacher_lse: T floats at the
- *   same tau (fl_top_logits gives it) or NULL.  1 <= k <= FL_MAX_TARGETS; tau
+ *   >= V, takes no part; a teacher_lse of -inf beside an entry above -inf has
+ *   no finite result.  teacher: T x k floats; teacher_lse: T floats at the same
+ *   tau (fl_top_logits gives it) or NULL.  1 <= k <= FL_MAX_TARGETS; tau
  *   finite, > 0.
  *
  * fl_head_distill_grad -- its gradient, as fl_head_loss_grad with

@@ -644,13 +644,12 @@ __global__ __launch_bounds__(256) void k_teacher(const HeadArgs a) {
     }
   }
   bad = __any(bad);
-  bool any = __any(!(x[0] == -INFINITY) || !(x[1] == -INFINITY));
+  const bool any = __any(!(x[0] == -INFINITY) || !(x[1] == -INFINITY));
   // log p = (x - ref) / tau - rest: in this order no digits of a small log p are
   // lost, and a logit at fp32's lowest value, finite as it is, does not overflow
   float ref = 0.f, rest = 0.f;
   if (a.teacher_lse) {
     rest = a.teacher_lse[t];
-    any = any && rest != -INFINITY;
   } else if (any) {
     ref = wave_max(fmaxf(x[0], x[1]));
     rest = logf(wave_sum(expf((x[0] - ref) / a.tau) + expf((x[1] - ref) / a.tau)));

@@ -258,3 +258,19 @@ def test_teachers_at_the_ends_of_the_range(env, tau):
     # 2^-8 of each entry of G for its rounding, as much again for the softmax's error
     allowed = 2.0 ** -7 * (G.abs() @ c["w"].double().abs()) + 2.0 ** -7.9 * want.abs()
     same(torch, "dhidden", c["dh"], want, allowed)
+
+
+def test_teachers_lse_of_minus_infinity(env):
+    """A teacher_lse of -inf beside a logit above it has no finite result, and
+    none is made up: loss and gradient say so.  Beside logits of -inf alone the
+    token takes no part."""
+    torch, P = env["torch"], env["P"]
+    a = torch.tensor([[1.0, 2.0, 3.0], [-math.inf] * 3, [-math.inf, 0.5, -math.inf], [3.0, 2.0, 1.0]],
+                     device="cuda")
+    alse = torch.tensor([-math.inf, -math.inf, -math.inf, 4.0], device="cuda")
+    c = teacher_case(torch, P, a, alse, 2.0)
+    assert torch.isfinite(c["loss"]).tolist() == [False, True, False, True]
+    assert torch.isfinite(c["lse"]).all()
+    assert torch.isfinite(c["dh"]).any(1).tolist() == [False, True, False, True]
+    assert float(c["loss"][1]) == 0.0 and float(c["lse"][1]) == 0.0 and not c["dh"][1].any()
+    assert not torch.isfinite(c["dw"]).any()
