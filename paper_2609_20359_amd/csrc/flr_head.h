@@ -118,6 +118,19 @@ __host__ __device__ inline int splits_of(int fit, int tiles, int max_splits) {
   return s < 1 ? 1 : s < max_splits ? s : max_splits;
 }
 
+// Enqueues a kernel.  The status is this launch's own: an error that an earlier call
+// of the runtime left behind is not this one's, and stays for who asks for it.
+template <typename T>
+struct Same {
+  using type = T;
+};
+template <typename... P>
+hipError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t lds, hipStream_t st,
+                  typename Same<P>::type... args) {
+  void* at[] = {static_cast<void*>(&args)...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, lds, st);
+}
+
 hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st);
 // The live tokens and their rows.
 hipError_t launch_head_pack(const HeadArgs& a, bool grad, hipStream_t st);

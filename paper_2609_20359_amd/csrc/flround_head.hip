@@ -603,8 +603,7 @@ int blocks_of(const TileArgs& a, int shape, bool splits) {
 template <typename S>
 hipError_t launch_tile(const TileArgs& a, int shape, hipStream_t st) {
   const int n = blocks_of(a, shape, S::EPI == kSlab);
-  if (n > 0) k_tile<S><<<(unsigned)n, S::NT, 0, st>>>(a);
-  return hipGetLastError();
+  return n > 0 ? launch(k_tile<S>, dim3((unsigned)n), S::NT, 0, st, a) : hipSuccess;
 }
 
 // ---- small kernels ------------------------------------------------------------
@@ -1021,44 +1020,35 @@ __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab,
 }  // namespace
 
 hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st) {
-  k_teacher<<<(unsigned)((a.T + 3) / 4), 256, 0, st>>>(a);
-  return hipGetLastError();
+  return launch(k_teacher, dim3((unsigned)((a.T + 3) / 4)), 256, 0, st, a);
 }
 hipError_t launch_head_pack(const HeadArgs& a, bool grad, hipStream_t st) {
   const dim3 grid((unsigned)(a.T + kRowPad), grad ? 1 : (a.K + kPackWords - 1) / kPackWords);
-  if (a.T <= kScan) {
-    if (grad) k_pack<true, true><<<grid, 256, 0, st>>>(a);
-    else k_pack<false, true><<<grid, 256, 0, st>>>(a);
-    return hipGetLastError();
-  }
-  k_live<<<1, 1024, 0, st>>>(a);
-  if (const hipError_t e = hipGetLastError()) return e;
-  if (grad) k_pack<true, false><<<grid, 256, 0, st>>>(a);
-  else k_pack<false, false><<<grid, 256, 0, st>>>(a);
-  return hipGetLastError();
+  if (a.T <= kScan)
+    return grad ? launch(k_pack<true, true>, grid, 256, 0, st, a)
+                : launch(k_pack<false, true>, grid, 256, 0, st, a);
+  if (const hipError_t e = launch(k_live, dim3(1), 1024, 0, st, a)) return e;
+  return grad ? launch(k_pack<true, false>, grid, 256, 0, st, a)
+              : launch(k_pack<false, false>, grid, 256, 0, st, a);
 }
 hipError_t launch_head_pack_weight(const HeadArgs& a, hipStream_t st) {
   const int64_t blocks = (a.V * a.Dp / 8 + 255) / 256;
-  k_pack_weight<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(a);
-  return hipGetLastError();
+  return launch(k_pack_weight, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), 256, 0, st, a);
 }
 hipError_t launch_head_finish(const HeadArgs& a, hipStream_t st) {
-  if (a.T == 1) k_finish<1><<<1, 1024, 0, st>>>(a);
-  else if (a.T <= 4) k_finish<4><<<1, 1024, 0, st>>>(a);
-  else k_finish<16><<<(unsigned)((a.T + 15) / 16), 1024, 0, st>>>(a);
-  return hipGetLastError();
+  if (a.T == 1) return launch(k_finish<1>, dim3(1), 1024, 0, st, a);
+  if (a.T <= 4) return launch(k_finish<4>, dim3(1), 1024, 0, st, a);
+  return launch(k_finish<16>, dim3((unsigned)((a.T + 15) / 16)), 1024, 0, st, a);
 }
 hipError_t launch_head_fix(const HeadArgs& a, uint16_t* G, int64_t ldg, int64_t v0, int64_t v1,
                            hipStream_t st) {
-  k_fix<<<(unsigned)((a.T + 3) / 4), 256, 0, st>>>(a, G, ldg, v0, v1);
-  return hipGetLastError();
+  return launch(k_fix, dim3((unsigned)((a.T + 3) / 4)), 256, 0, st, a, G, ldg, v0, v1);
 }
 hipError_t launch_head_dh(const HeadArgs& a, const float* slab, int64_t ld_slab, int shape,
                           int max_splits, float out_scale, hipStream_t st) {
   const int64_t blocks = (a.D + 1023) / 1024 * a.T;
-  k_dh<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(
-      a, slab, ld_slab, tile_p(shape), tile_q(shape), tile_fit(shape), max_splits, out_scale);
-  return hipGetLastError();
+  return launch(k_dh, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), 256, 0, st, a, slab, ld_slab,
+                tile_p(shape), tile_q(shape), tile_fit(shape), max_splits, out_scale);
 }
 hipError_t launch_logits_stats(const TileArgs& a, int shape, hipStream_t st) {
   switch (shape) {
@@ -1083,11 +1073,9 @@ hipError_t launch_grads(const TileArgs& h, int h_shape, const TileArgs& w, int w
   if (w_shape == kTile128 && h_shape != kTile256 && w.np * w.nq <= (int64_t)1 << 26) {
     const int nh = blocks_of(h, h_shape, true), nw = blocks_of(w, w_shape, false);
     const dim3 grid((unsigned)(nh + nw));
-    if (h_shape == kTile64)
-      k_tiles<SlabTiles::T64, OutTiles::T128><<<grid, 256, 0, st>>>(h, nh, w);
-    else
-      k_tiles<SlabTiles::T128, OutTiles::T128><<<grid, 256, 0, st>>>(h, nh, w);
-    return hipGetLastError();
+    return h_shape == kTile64
+               ? launch(k_tiles<SlabTiles::T64, OutTiles::T128>, grid, 256, 0, st, h, nh, w)
+               : launch(k_tiles<SlabTiles::T128, OutTiles::T128>, grid, 256, 0, st, h, nh, w);
   }
   const hipError_t e = w_shape == kTile256 ? launch_tile<OutTiles::T256>(w, w_shape, st)
                                            : launch_tile<OutTiles::T128>(w, w_shape, st);

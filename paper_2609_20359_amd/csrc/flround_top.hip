@@ -302,24 +302,22 @@ __global__ __launch_bounds__(kJoinThreads) void k_top_join(const TopArgs a) {
 }
 
 template <bool BF16>
-void launch_segment(const TopArgs& a, unsigned grid, hipStream_t st) {
+hipError_t launch_segment(const TopArgs& a, dim3 grid, hipStream_t st) {
   switch (a.chunks) {
-    case 1: k_top_segment<BF16, 1><<<grid, kThreads, 0, st>>>(a); break;
-    case 2: k_top_segment<BF16, 2><<<grid, kThreads, 0, st>>>(a); break;
-    case 4: k_top_segment<BF16, 4><<<grid, kThreads, 0, st>>>(a); break;
-    default: k_top_segment<BF16, 8><<<grid, kThreads, 0, st>>>(a); break;
+    case 1: return launch(k_top_segment<BF16, 1>, grid, kThreads, 0, st, a);
+    case 2: return launch(k_top_segment<BF16, 2>, grid, kThreads, 0, st, a);
+    case 4: return launch(k_top_segment<BF16, 4>, grid, kThreads, 0, st, a);
+    default: return launch(k_top_segment<BF16, 8>, grid, kThreads, 0, st, a);
   }
 }
 
 }  // namespace
 
 hipError_t launch_top(const TopArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)(a.rows * a.segs);
-  if (a.bf16) launch_segment<true>(a, grid, st);
-  else launch_segment<false>(a, grid, st);
-  if (const hipError_t e = hipGetLastError()) return e;
-  if (a.segs > 1) k_top_join<<<(unsigned)a.rows, kJoinThreads, (size_t)a.segs * a.k * 14, st>>>(a);
-  return hipGetLastError();
+  const dim3 grid((unsigned)(a.rows * a.segs));
+  const hipError_t e = a.bf16 ? launch_segment<true>(a, grid, st) : launch_segment<false>(a, grid, st);
+  if (e != hipSuccess || a.segs == 1) return e;
+  return launch(k_top_join, dim3((unsigned)a.rows), kJoinThreads, (size_t)a.segs * a.k * 14, st, a);
 }
 
 }  // namespace flr

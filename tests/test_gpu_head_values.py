@@ -9,6 +9,7 @@ power of two times a bf16 number):
   loss: the difference in 64 bits of what lse is before its rounding and the
         target, so 2^-16 and its own rounding, 2^-22 |loss|.
 """
+import ctypes
 import math
 
 import pytest
@@ -274,3 +275,61 @@ def test_teachers_lse_of_minus_infinity(env):
     assert torch.isfinite(c["dh"]).any(1).tolist() == [False, True, False, True]
     assert float(c["loss"][1]) == 0.0 and float(c["lse"][1]) == 0.0 and not c["dh"][1].any()
     assert not torch.isfinite(c["dw"]).any()
+
+
+# ---- after another call's error -------------------------------------------------
+
+
+def test_an_earlier_error_is_not_this_calls(env):
+    """An error that an earlier call of the runtime left behind neither stops a
+    call that has nothing to do with it nor makes it fail."""
+    torch, P = env["torch"], env["P"]
+    from paper_2609_20359_amd import flround as F
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    T, V, D, K = 40, 500, 64, 4
+    h = torch.randn(T, D, generator=g, device="cuda").bfloat16()
+    w = torch.randn(V, D, generator=g, device="cuda").bfloat16()
+    labels = torch.randint(0, V, (T,), generator=g, device="cuda")
+    x = torch.randn(T, 60000, generator=g, device="cuda")
+    dl = torch.full((T,), 0.25, device="cuda")
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    hip = F.hip_runtime()
+
+    def leave_error():
+        assert hip.hipSetDevice(ctypes.c_int(1 << 20)) != 0    # no such device; nothing is changed
+
+    def calls(before):
+        out = dict(f=[torch.zeros(T, device="cuda") for _ in range(3)],
+                   b=[torch.zeros(T, D, device="cuda", dtype=torch.bfloat16),
+                      torch.zeros(V, D, device="cuda", dtype=torch.bfloat16)],
+                   t=[torch.zeros(T, K, device="cuda"),
+                      torch.zeros(T, K, device="cuda", dtype=torch.int32),
+                      torch.zeros(T, device="cuda")],
+                   d=[torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda"),
+                      torch.zeros(T, K, device="cuda")],
+                   e=[torch.zeros(T, D, device="cuda", dtype=torch.bfloat16),
+                      torch.zeros(V, D, device="cuda", dtype=torch.bfloat16)])
+        words = torch.randint(0, V, (T, K), device="cuda",
+                              generator=torch.Generator(device="cuda").manual_seed(4)).int()
+        torch.cuda.synchronize()
+        before()
+        P.fl_head_loss(h, w, labels, *out["f"], workspace=ws)
+        before()
+        P.fl_head_loss_grad(h, w, labels, out["f"][1], out["f"][2], dl, *out["b"], workspace=ws)
+        before()
+        P.fl_top_logits(x, K, 1.0, *out["t"], workspace=ws)
+        before()
+        P.fl_head_distill(h, w, words, out["t"][0], None, 1.0, *out["d"], workspace=ws)
+        before()
+        P.fl_head_distill_grad(h, w, words, out["t"][0], None, 1.0, out["d"][1], out["d"][2], dl,
+                               *out["e"], workspace=ws)
+        hip.hipGetLastError()                 # nothing is left for the calls of others
+        torch.cuda.synchronize()
+        return [t for k in sorted(out) for t in out[k]]
+
+    want = calls(lambda: None)
+    got = calls(leave_error)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
