@@ -445,11 +445,11 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  * at the top of this file do not apply to them.
  *
  * Conventions that differ from those at the top: there is no layout handle; the
- * device is the current one.  weight and workspace need 16-byte alignment
- * (workspace: any; it is rounded up), the others that of their elements.  hidden
- * and weight may have longer rows than they use (the strides, in elements; 0:
- * rows follow each other).  Weight rows of a width or stride that is not a
- * multiple of 8 are copied to the workspace by every call.
+ * device is the current one.  Pointers are aligned to their elements (workspace:
+ * in any way), and weight to 16 bytes where width and stride are multiples of 8.
+ * hidden and weight may have longer rows than they use (the strides, in elements;
+ * 0: rows follow each other).  Weight rows of another width or stride are copied
+ * to the workspace by every call.
  *
  * workspace: device memory, fl_head_workspace_bytes(shape, k, grad) bytes
  *   (k = 0 for fl_head_loss and its gradient; grad nonzero for the gradients;

@@ -56,10 +56,15 @@ struct Plan {
   size_t hdr, live, pos, logp, mass, flag, hc, wc, parts, row_lse, row_coef, row_label, row_spot, G, slab, bytes;
 };
 
+// The tiles' loads take 16 bytes; rows of another length are copied first, from any
+// element's boundary.
+bool copies_weight(const fl_head_shape& s) {
+  return (((s.weight_stride ? s.weight_stride : s.width) | s.width) & 7) != 0;
+}
+
 Plan plan_for(const fl_head_shape& s, int K, bool grad) {
   Plan p{};
-  // The tiles' loads take 16 bytes; rows of another length are copied first.
-  const bool pack_w = (((s.weight_stride ? s.weight_stride : s.width) | s.width) & 7) != 0;
+  const bool pack_w = copies_weight(s);
   p.T = s.tokens, p.V = s.vocab, p.D = s.width;
   p.K = K > 0 ? K : 1;
   p.grad = grad, p.distill = K > 0, p.pack_w = pack_w;
@@ -237,7 +242,7 @@ int forward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* weig
   if (!shape_ok(s)) return FL_ERR_INVALID;
   if ((rc = check_targets(*s, t)) != FL_OK) return rc;
   if ((rc = elem_ptr(hidden, s->tokens, 2)) != FL_OK) return rc;
-  if ((rc = elem_ptr(weight, 1, 16)) != FL_OK) return rc;
+  if ((rc = elem_ptr(weight, 1, copies_weight(*s) ? 2 : 16)) != FL_OK) return rc;
   for (const void* o : {(const void*)loss, (const void*)lse, (const void*)target})
     if ((rc = elem_ptr(o, s->tokens, 4)) != FL_OK) return rc;
   Call c;
@@ -260,7 +265,7 @@ int backward(const fl_head_shape* s, const uint16_t* hidden, const uint16_t* wei
   if (!shape_ok(s)) return FL_ERR_INVALID;
   if ((rc = check_targets(*s, t)) != FL_OK) return rc;
   if ((rc = elem_ptr(hidden, s->tokens, 2)) != FL_OK) return rc;
-  if ((rc = elem_ptr(weight, 1, 16)) != FL_OK) return rc;
+  if ((rc = elem_ptr(weight, 1, copies_weight(*s) ? 2 : 16)) != FL_OK) return rc;
   for (const void* i : {(const void*)lse, (const void*)target, (const void*)dloss})
     if ((rc = elem_ptr(i, s->tokens, 4)) != FL_OK) return rc;
   if ((rc = elem_ptr(dhidden, s->tokens, 2)) != FL_OK) return rc;

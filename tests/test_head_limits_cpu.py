@@ -1,0 +1,29 @@
+"""Limits of the output head's entry points and what lies just inside them,
+without a GPU: a call that passes the checks of its arguments goes on to its
+workspace, so a workspace of no bytes shows which check comes first."""
+import ctypes
+
+import paper_2609_20359_amd as P
+from paper_2609_20359_amd import flround as F
+
+INVALID, ALIGN, SCRATCH = F.FL_ERR_INVALID, F.FL_ERR_ALIGN, F.FL_ERR_SCRATCH
+A = 1 << 20   # an address that is aligned to anything; never dereferenced
+
+
+def calls(s, weight=2 * A, k=4, nbytes=0):
+    """The status of each of the head's four calls with a workspace of nbytes."""
+    L, s = P.lib(), ctypes.byref(s)
+    return [L.fl_head_loss(s, A, weight, A, A, A, A, A, nbytes, None),
+            L.fl_head_loss_grad(s, A, weight, A, A, A, A, 3 * A, 4 * A, A, nbytes, None),
+            L.fl_head_distill(s, A, weight, k, A, A, None, 1.0, A, A, A, A, nbytes, None),
+            L.fl_head_distill_grad(s, A, weight, k, A, A, None, 1.0, A, A, A, 3 * A, 4 * A, A, nbytes,
+                                   None)]
+
+
+def test_weight_rows_that_are_copied_may_start_anywhere():
+    for T, V, D, ldw in ((8, 100, 63, 0), (8, 100, 64, 65), (8, 100, 65, 72)):
+        s = F.HeadShape(T, V, D, 0, ldw)
+        assert calls(s, weight=2 * A + 2) == [SCRATCH] * 4
+        assert calls(s, weight=2 * A + 1) == [ALIGN] * 4
+    for D, ldw in ((64, 0), (64, 72)):    # these are read as they are
+        assert calls(F.HeadShape(8, 100, D, 0, ldw), weight=2 * A + 2) == [ALIGN] * 4
