@@ -507,8 +507,8 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *   that is 0.
  *
  * Limits (FL_ERR_INVALID beyond): tokens and rows <= 2^20, vocab <= 2^21
- * (fl_top_logits 2^20), width <= 2^15, strides of hidden and weight <= 2^22,
- * ceil(tokens / 128) * ceil(vocab / 128) <= 2^22.
+ * (fl_top_logits 2^20), width <= 2^15, hidden_stride <= 2^40, weight_stride <=
+ * 2^22, ceil(tokens / 128) * ceil(vocab / 128) <= 2^22.
  * ---------------------------------------------------------------------- */
 #define FL_MAX_TARGETS 128
 

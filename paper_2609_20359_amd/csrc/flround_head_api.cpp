@@ -16,7 +16,8 @@ namespace {
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 20;
 constexpr int64_t kMaxWidth = (int64_t)1 << 15;
-constexpr int64_t kMaxStride = (int64_t)1 << 22;   // 256 rows of it within 32 bits of bytes
+constexpr int64_t kMaxHiddenStride = (int64_t)1 << 40;   // all rows within 62 bits of bytes
+constexpr int64_t kMaxWeightStride = (int64_t)1 << 22;   // 256 rows of it within 32
 constexpr int64_t kMaxVocab = (int64_t)1 << 21;
 constexpr int64_t kMaxTopVocab = (int64_t)1 << 20;
 constexpr int64_t kMaxTiles = (int64_t)1 << 22;
@@ -132,8 +133,9 @@ bool shape_ok(const fl_head_shape* s) {
   if (!s || s->tokens < 0 || s->tokens > kMaxTokens || s->vocab < 1 || s->vocab > kMaxVocab ||
       s->width < 1 || s->width > kMaxWidth)
     return false;
-  for (int64_t ld : {s->hidden_stride, s->weight_stride})
-    if (ld != 0 && (ld < s->width || ld > kMaxStride)) return false;
+  const int64_t ldh = s->hidden_stride, ldw = s->weight_stride;
+  if (ldh != 0 && (ldh < s->width || ldh > kMaxHiddenStride)) return false;
+  if (ldw != 0 && (ldw < s->width || ldw > kMaxWeightStride)) return false;
   return ceil_div(s->tokens, 128) * ceil_div(s->vocab, 128) <= kMaxTiles;
 }
 

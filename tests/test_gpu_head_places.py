@@ -1,5 +1,5 @@
 """The output head with inputs at places of their own: a weight that starts
-between two 16-byte boundaries."""
+between two 16-byte boundaries, hidden states far apart."""
 import pytest
 
 from test_gpu_head import Case
@@ -31,4 +31,18 @@ def test_weight_rows_off_sixteen_bytes(env, V, D, ld, off, K):
     view = flat[off:].view(V, ld)[:, :D]
     view.copy_(c.w)
     c.w = view
+    c.check(env["P"])
+
+
+@pytest.mark.parametrize("K", [0, 5])
+def test_last_tokens_of_long_sequences(env, K):
+    """hidden[:, -1] of 3-D states: rows a whole sequence apart, some of them
+    past 32 bits of bytes."""
+    torch = env["torch"]
+    T, D, length = 40, 64, 1 << 20
+    c = Case(torch, T, 300, D, K=K)
+    states = torch.empty(T, length, D, dtype=torch.bfloat16, device="cuda")
+    states[:, -1] = c.h
+    c.h = states[:, -1]
+    assert c.h.stride(0) == length * D > 1 << 22
     c.check(env["P"])

@@ -27,3 +27,13 @@ def test_weight_rows_that_are_copied_may_start_anywhere():
         assert calls(s, weight=2 * A + 1) == [ALIGN] * 4
     for D, ldw in ((64, 0), (64, 72)):    # these are read as they are
         assert calls(F.HeadShape(8, 100, D, 0, ldw), weight=2 * A + 2) == [ALIGN] * 4
+
+
+def test_hidden_rows_may_be_far_apart():
+    """One row of each of many long sequences: only the weight's rows are held to
+    32 bits of bytes a tile."""
+    for ld in ((1 << 22) + 8, 131072 * 4096, 1 << 40):
+        assert calls(F.HeadShape(8, 100, 64, ld, 0)) == [SCRATCH] * 4
+    assert calls(F.HeadShape(8, 100, 64, (1 << 40) + 1, 0)) == [INVALID] * 4
+    assert calls(F.HeadShape(8, 100, 64, 0, 1 << 22)) == [SCRATCH] * 4
+    assert calls(F.HeadShape(8, 100, 64, 0, (1 << 22) + 8)) == [INVALID] * 4
