@@ -489,8 +489,8 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *   gives NaN.  A token with no entry that is present and above -inf, and none
  *   >= V, takes no part; a teacher_lse of -inf beside an entry above -inf has
  *   no finite result.  teacher: T x k floats; teacher_lse: T floats at the same
- *   tau (fl_top_logits gives it) or NULL.  1 <= k <= FL_MAX_TARGETS; tau
- *   finite, > 0.
+ *   tau (fl_top_logits gives it) or NULL.  1 <= k <= FL_MAX_TARGETS; tau finite,
+ *   > 0, and no smaller than where log2(e) / tau overflows (4.3e-39).
  *
  * fl_head_distill_grad -- its gradient, as fl_head_loss_grad with
  *     G[t][v] = dloss[t] tau (exp(z[t][v] / tau - lse[t]) sum_j p[t][j]

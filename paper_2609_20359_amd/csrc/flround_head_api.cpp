@@ -151,6 +151,11 @@ int status_of(hipError_t e) {
   return e == hipSuccess ? FL_OK : e == hipErrorOutOfMemory ? FL_ERR_NOMEM : FL_ERR_HIP;
 }
 
+// log2(e) / tau, by which the kernels scale, has to be finite in 32 bits.
+bool tau_ok(float tau) {
+  return std::isfinite(tau) && tau > 0.f && std::isfinite((float)(1.4426950408889634 / (double)tau));
+}
+
 struct Targets {
   const int64_t* labels;
   const int32_t* ids;
@@ -163,7 +168,7 @@ struct Targets {
 int check_targets(const fl_head_shape& s, const Targets& t) {
   int rc;
   if (t.K == 0) return elem_ptr(t.labels, s.tokens, 8);
-  if (t.K < 1 || t.K > kMaxTargets || !std::isfinite(t.tau) || !(t.tau > 0.f)) return FL_ERR_INVALID;
+  if (t.K < 1 || t.K > kMaxTargets || !tau_ok(t.tau)) return FL_ERR_INVALID;
   if ((rc = elem_ptr(t.ids, s.tokens, 4)) != FL_OK) return rc;
   if ((rc = elem_ptr(t.teacher, s.tokens, 4)) != FL_OK) return rc;
   return t.teacher_lse ? elem_ptr(t.teacher_lse, s.tokens, 4) : FL_OK;
@@ -401,7 +406,7 @@ int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const 
                   float tau, float* values, int32_t* ids, float* lse, void* workspace,
                   size_t workspace_bytes, void* stream) {
   int rc;
-  if (!top_ok(rows, vocab, dtype, k) || !std::isfinite(tau) || !(tau > 0.f)) return FL_ERR_INVALID;
+  if (!top_ok(rows, vocab, dtype, k) || !tau_ok(tau)) return FL_ERR_INVALID;
   if (stride != 0 && stride < vocab) return FL_ERR_INVALID;
   if (rows == 0) return FL_OK;
   if ((rc = elem_ptr(logits, rows, dtype == FL_BF16 ? 2 : 4)) != FL_OK) return rc;

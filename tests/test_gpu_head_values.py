@@ -211,6 +211,45 @@ def test_gradient_of_logits_far_from_zero(env, T, V):
         same(torch, what, got, want, off)
 
 
+@pytest.mark.parametrize("tau", [2.0 ** -127, 2.0 ** -100, 1e-20, 1e20, 2.0 ** 100])
+def test_temperatures_at_both_ends(env, tau):
+    """Close to 0 all probability is at the largest logit, far from it all words have
+    the same; the results are those, as far as fp32 holds them."""
+    torch, P = env["torch"], env["P"]
+    T, V, D, K = 40, 300, 16, 3
+    tau = float(torch.tensor(tau, dtype=torch.float32))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    h = torch.zeros(T, D, device="cuda", dtype=torch.bfloat16)
+    h[:, 0] = torch.randint(1, 9, (T,), generator=g, device="cuda").bfloat16()
+    w = torch.zeros(V, D, device="cuda", dtype=torch.bfloat16)
+    w[:, 0] = torch.randint(-60, 60, (V,), generator=g, device="cuda").bfloat16()
+    w[17, 0] = 64.0
+    z = h.double() @ w.double().t()
+    x = z.float()
+    values, ids, alse = top(P, torch, x, K, tau)
+    want = torch.logsumexp(z / tau, 1)
+    same(torch, "teacher's lse", alse, want, 2.0 ** -16 + 4 * U * want.abs())
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    target = torch.empty(T, K, device="cuda")
+    dh = torch.empty(T, D, device="cuda", dtype=torch.bfloat16)
+    dw = torch.empty(V, D, device="cuda", dtype=torch.bfloat16)
+    P.fl_head_distill(h, w, ids, values, None, tau, loss, lse, target)
+    same(torch, "lse", lse, want, 2.0 ** -16 + 4 * U * want.abs())
+    if not bool(torch.isfinite(lse).all()):
+        return                       # 2^-127: the quotient itself overflows
+    dl = torch.ones(T, device="cuda")
+    P.fl_head_distill_grad(h, w, ids, values, None, tau, lse, target, dl, dh, dw)
+    p = torch.zeros(T, V, device="cuda", dtype=torch.float64)
+    p.scatter_(1, ids.long(), torch.softmax(values.double() / tau, 1))
+    # the softmax of z / tau, from lse as fp32 holds it where that is exact
+    soft = torch.softmax(z / tau, 1)
+    G = tau * (soft - p)
+    # both sides 1 at the same word, or 1 / V and 1 / K; each is off by 2^-8 at most
+    off = tau * 2.0 ** -7 * ((soft + p) @ w.double().abs())
+    same(torch, "dhidden", dh, G @ w.double(), off)
+
+
 # ---- the teacher ---------------------------------------------------------------
 
 

@@ -10,13 +10,13 @@ INVALID, ALIGN, SCRATCH = F.FL_ERR_INVALID, F.FL_ERR_ALIGN, F.FL_ERR_SCRATCH
 A = 1 << 20   # an address that is aligned to anything; never dereferenced
 
 
-def calls(s, weight=2 * A, k=4, nbytes=0):
+def calls(s, weight=2 * A, k=4, nbytes=0, tau=1.0):
     """The status of each of the head's four calls with a workspace of nbytes."""
     L, s = P.lib(), ctypes.byref(s)
     return [L.fl_head_loss(s, A, weight, A, A, A, A, A, nbytes, None),
             L.fl_head_loss_grad(s, A, weight, A, A, A, A, 3 * A, 4 * A, A, nbytes, None),
-            L.fl_head_distill(s, A, weight, k, A, A, None, 1.0, A, A, A, A, nbytes, None),
-            L.fl_head_distill_grad(s, A, weight, k, A, A, None, 1.0, A, A, A, 3 * A, 4 * A, A, nbytes,
+            L.fl_head_distill(s, A, weight, k, A, A, None, tau, A, A, A, A, nbytes, None),
+            L.fl_head_distill_grad(s, A, weight, k, A, A, None, tau, A, A, A, 3 * A, 4 * A, A, nbytes,
                                    None)]
 
 
@@ -37,3 +37,16 @@ def test_hidden_rows_may_be_far_apart():
     assert calls(F.HeadShape(8, 100, 64, (1 << 40) + 1, 0)) == [INVALID] * 4
     assert calls(F.HeadShape(8, 100, 64, 0, 1 << 22)) == [SCRATCH] * 4
     assert calls(F.HeadShape(8, 100, 64, 0, (1 << 22) + 8)) == [INVALID] * 4
+
+
+def test_temperatures_whose_reciprocal_overflows():
+    """The kernels scale by log2(e) / tau: where that is not finite in 32 bits no
+    result would be."""
+    top = P.lib().fl_top_logits
+    s = F.HeadShape(8, 100, 64, 0, 0)
+    for tau in (2.0 ** -149, 2.0 ** -128):
+        assert calls(s, tau=tau)[2:] == [INVALID] * 2
+        assert top(4, 100000, 0, F.FL_BF16, A, 5, tau, A, A, A, A, 0, None) == INVALID
+    for tau in (2.0 ** -127, 2.0 ** -126, 1e-30, 3e38):
+        assert calls(s, tau=tau)[2:] == [SCRATCH] * 2
+        assert top(4, 100000, 0, F.FL_BF16, A, 5, tau, A, A, A, A, 0, None) == SCRATCH
