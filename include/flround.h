@@ -474,8 +474,10 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  *   written, not added to.  G is made again for a piece of the vocabulary at a
  *   time and rounded to bf16 relative to the largest |dloss|, which leaves a
  *   relative error of up to 2^-8 per term beside that of rounding the results
- *   (2^-16 for up to 32 tokens).
- *   The workspace holds one piece of G (256 MiB, or 8192 words).
+ *   (2^-16 in a call of up to 32 tokens, those that take no part among them).
+ *   exp(z - lse) is taken from lse in fp32, so a large lse leaves it a relative
+ *   error of its own, 2^-23 |lse| (and as much of |z / tau| where 1 / tau is not
+ *   exact).  The workspace holds one piece of G (256 MiB, or 8192 words).
  *
  * fl_head_distill -- distillation from a teacher's top logits:
  *     logp[t][j] = teacher[t][j] / tau - A[t], A[t] = teacher_lse[t], or, where

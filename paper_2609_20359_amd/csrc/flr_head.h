@@ -12,13 +12,14 @@ constexpr int kRowPad = 256;      // compacted rows are padded to this many
 constexpr int kStep = 64;         // elements of the summed axis a tile takes at a time
 constexpr int kMaxTargets = 128;  // listed teacher logits per token
 
-// The gradient of up to this many tokens has two rows for each: G rounded to bf16,
-// and what that leaves, rounded too.  A G of few tokens has few large entries, so
-// that one unlucky rounding (2^-9) is the error of a whole result; where they are
-// many, such errors are of both signs and all sizes.  The products' smallest tiles
-// have 64 rows, so the second row costs little (of 50257 words, 1024 wide: 102 us
-// for 32 tokens, off by 1.7e-3, the results' own rounding; 96 us for 33, off by
-// 2.3e-3).
+// The gradient of a call of up to this many tokens, whether they take part or not,
+// has two rows for each: G rounded to bf16, and what that leaves, rounded too, which
+// makes G's error 2^-16 of an entry instead of 2^-8.  Off by, in the 2-norm, of 50257
+// words, 1024 wide: 1.7e-3 of 32 tokens, which is the results' own rounding, and
+// 2.3e-3 of 33 with one row each.  Both rows of 32 tokens fit the products' smallest
+// tiles, of 64 rows (102 us, 96 for 33); beyond, they would be two products more for
+// the three that there are.  The choice is the host's, which does not know how many
+// tokens take part.
 constexpr int kTwiceTokens = 32;
 
 // Written by the first kernel of a call.

@@ -458,6 +458,11 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
         a.parts[(int64_t)my_tp * a.parts_ld + q0 + tid] = p;
       }
     } else if constexpr (EPI == kGrad) {
+      // G is rounded to bf16, what the matrix cores multiply with bf16 hidden states
+      // and weights: its entries' error, up to 2^-8, takes the gradients' in the
+      // 2-norm from the results' own rounding, 1.7e-3, to 1.8e-3 to 2.4e-3.  With a
+      // second row for what that leaves (copies) the two products that follow would
+      // be twice as long; up to kTwiceTokens tokens have it.
       const bool inside = p0 + BP <= a.np && q0 + BQ <= n_live;
       uint16_t* g = a.G + qw * a.ldg + p0 + wp * FP * 16 + (l >> 4) * 8;
 #pragma unroll
