@@ -50,3 +50,55 @@ def test_temperatures_whose_reciprocal_overflows():
     for tau in (2.0 ** -127, 2.0 ** -126, 1e-30, 3e38):
         assert calls(s, tau=tau)[2:] == [SCRATCH] * 2
         assert top(4, 100000, 0, F.FL_BF16, A, 5, tau, A, A, A, A, 0, None) == SCRATCH
+
+
+def test_both_sides_of_the_limits():
+    L = P.lib()
+    K, V, D = F.FL_MAX_TARGETS, 1 << 21, 1 << 15
+    T = 1 << 20
+    inside = [(T, 100, 64), (T - 1, 65536, 64), (T, 65536, 64), (T, 65536, D), (256, V, 64), (256, V - 1, D),
+              (8, 100, D), (8, 100, D - 1), (8, V, D), (0, V, D), (32, V, D), (33, V, 65), (1, 1, 1)]
+    outside = [(T + 1, 100, 64), (8, V + 1, 64), (8, 100, D + 1), (T, 65537, 64), (T - 127, 65537, 64),
+               (262145, V, 64)]
+    for t, v, d in inside:
+        s = F.HeadShape(t, v, d, 0, 0)
+        assert calls(s, k=K) == [SCRATCH] * 4, (t, v, d)
+        for k in (0, 1, K):
+            forward = L.fl_head_workspace_bytes(ctypes.byref(s), k, 0)
+            grad = L.fl_head_workspace_bytes(ctypes.byref(s), k, 1)
+            copied = 2 * v * d if d % 8 else 0      # the weight's rows
+            listed = 4 * t * k                      # the teacher's probabilities
+            # statistics of each word tile; G of 8192 words, or all, and a row of sums per token
+            assert forward >= 2 * t * d + copied + listed + 8 * t * (v // 256), (t, v, d, k)
+            assert grad >= 2 * t * d + copied + listed + 2 * t * min(v, 8192) + 4 * t * d, (t, v, d, k)
+            assert max(forward, grad) < 1 << 42, (t, v, d, k)
+    for t, v, d in outside:
+        s = F.HeadShape(t, v, d, 0, 0)
+        assert calls(s, k=K) == [INVALID] * 4, (t, v, d)
+        assert L.fl_head_workspace_bytes(ctypes.byref(s), 0, 0) == 0
+        assert L.fl_head_workspace_bytes(ctypes.byref(s), K, 1) == 0
+    s = F.HeadShape(8, 200, 64, 0, 0)
+    assert calls(s, k=K)[2:] == [SCRATCH] * 2 and calls(s, k=K + 1)[2:] == [INVALID] * 2
+    assert L.fl_head_workspace_bytes(ctypes.byref(s), K + 1, 0) == 0
+    assert L.fl_head_workspace_bytes(ctypes.byref(s), -1, 0) == 0
+
+
+def test_both_sides_of_the_limits_of_top_logits():
+    L = P.lib()
+
+    def top(rows, vocab, k, dtype):
+        return L.fl_top_logits(rows, vocab, 0, dtype, A, k, 1.0, A, A, A, A, 0, None)
+
+    for dtype in (F.FL_BF16, F.FL_F32):
+        for rows, vocab, k in ((1 << 20, 1 << 20, 128), (1, 1 << 20, 128), (1 << 20, 50000, 1),
+                               (4, 100000, 128)):
+            need = L.fl_top_workspace_bytes(rows, vocab, dtype, k)
+            # where a row is cut, an entry for each of k of each segment, two at least
+            assert need == 0 or need >= 2 * rows * 8 * k, (rows, vocab, k)
+            if need:
+                assert top(rows, vocab, k, dtype) == SCRATCH
+        for rows, vocab, k in (((1 << 20) + 1, 100, 1), (4, (1 << 20) + 1, 1), (4, 1000, 129), (4, 127, 128),
+                               (4, 128, 0)):
+            assert L.fl_top_workspace_bytes(rows, vocab, dtype, k) == 0
+            assert top(rows, vocab, k, dtype) == INVALID
+        assert L.fl_top_workspace_bytes(1, 1 << 20, dtype, 128) > 0
