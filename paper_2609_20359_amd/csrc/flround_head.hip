@@ -46,11 +46,11 @@ __device__ __forceinline__ float rest_of(float x) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // (m, s) stands for s exp(m / tau), s2 being log2(e) / tau; a part of nothing is
-// (-inf, 0), and a maximum of +inf has an s > 0.  The maximum itself counts whole:
-// infinities have no difference.
+// (-inf, 0).  Infinities have no difference: a maximum of +inf has an s > 0, here
+// +inf, whose logarithm changes nothing.
 __device__ __forceinline__ void join(float& m, float& s, float pm, float ps, float s2) {
-  const float top = fmaxf(m, pm);
-  s = s * (m == top ? 1.f : exp2_((m - top) * s2)) + ps * (pm == top ? 1.f : exp2_((pm - top) * s2));
+  const float top = fmaxf(m, pm), ref = fabsf(top) == INFINITY ? 0.f : top;
+  s = s * exp2_((m - ref) * s2) + ps * exp2_((pm - ref) * s2);
   m = top;
 }
 

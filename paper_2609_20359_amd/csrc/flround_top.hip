@@ -51,13 +51,13 @@ __device__ __forceinline__ uint64_t entry(float x, int id) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
-// (m, s) stands for s exp(m / tau); nothing is (-inf, 0), and a maximum of +inf has
-// an s > 0.  Differences are taken before they are scaled: a row masked by the type's
-// lowest value would overflow the other way round.  The maximum itself counts whole:
-// infinities have no difference.
+// (m, s) stands for s exp(m / tau); nothing is (-inf, 0).  Differences are taken
+// before they are scaled: a row masked by the type's lowest value would overflow the
+// other way round.  Infinities have none: a maximum of +inf has an s > 0, here +inf,
+// whose logarithm changes nothing.
 __device__ __forceinline__ void join(float& m, float& s, float pm, float ps, float s2) {
-  const float top = fmaxf(m, pm);
-  s = s * (m == top ? 1.f : exp2_((m - top) * s2)) + ps * (pm == top ? 1.f : exp2_((pm - top) * s2));
+  const float top = fmaxf(m, pm), ref = fabsf(top) == INFINITY ? 0.f : top;
+  s = s * exp2_((m - ref) * s2) + ps * exp2_((pm - ref) * s2);
   m = top;
 }
 __device__ __forceinline__ float lse_of(float m, float s, const TopArgs& a) {
