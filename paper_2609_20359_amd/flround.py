@@ -621,6 +621,13 @@ def top_workspace_bytes(rows, vocab, k, dtype=FL_BF16):
     return int(lib().fl_top_workspace_bytes(rows, vocab, dtype, k))
 
 
+def _listed_words(ids):
+    """The k of ids (T x k)."""
+    if ids.dim() != 2:
+        raise ValueError("ids must be a 2-D tensor")
+    return ids.shape[1]
+
+
 class _HeadCall:
     """The arguments that the head's four functions share, checked."""
 
@@ -649,9 +656,7 @@ class _HeadCall:
         return _array(t, (self.T,), _T.int64, self.dev, "labels")
 
     def teacher(self, ids, teacher, teacher_lse):
-        if ids.dim() != 2:
-            raise ValueError("ids must be a 2-D tensor")
-        self.k = ids.shape[1]
+        self.k = _listed_words(ids)
         return (_array(ids, (self.T, self.k), _T.int32, self.dev, "ids"),
                 self.listed(teacher, "teacher"),
                 None if teacher_lse is None else self.floats(teacher_lse, "teacher_lse"))
@@ -691,7 +696,7 @@ def fl_head_distill(hidden, weight, ids, teacher, teacher_lse, tau, loss, lse, t
     float32) as fl_top_logits writes them, teacher_lse (T float32) or None to
     normalise over the listed words.  Writes loss and lse (T float32) and
     target (T x k float32)."""
-    c = _HeadCall(hidden, weight, ids.shape[-1], 0, workspace, stream)
+    c = _HeadCall(hidden, weight, _listed_words(ids), 0, workspace, stream)
     i, a, al = c.teacher(ids, teacher, teacher_lse)
     rc = lib().fl_head_distill(c.shape, c.h, c.w, c.k, i, a, al, float(tau),
                                c.floats(loss, "loss"), c.floats(lse, "lse"),
@@ -703,7 +708,7 @@ def fl_head_distill_grad(hidden, weight, ids, teacher, teacher_lse, tau, lse, ta
                          dhidden, dweight, workspace=None, stream=None):
     """Gradient of sum(dloss * loss) of fl_head_distill: writes dhidden and
     dweight, bf16."""
-    c = _HeadCall(hidden, weight, ids.shape[-1], 1, workspace, stream)
+    c = _HeadCall(hidden, weight, _listed_words(ids), 1, workspace, stream)
     i, a, al = c.teacher(ids, teacher, teacher_lse)
     dh, dw = c.grads(dhidden, dweight)
     rc = lib().fl_head_distill_grad(c.shape, c.h, c.w, c.k, i, a, al, float(tau),

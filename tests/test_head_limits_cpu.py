@@ -3,6 +3,8 @@ without a GPU: a call that passes the checks of its arguments goes on to its
 workspace, so a workspace of no bytes shows which check comes first."""
 import ctypes
 
+import pytest
+
 import paper_2609_20359_amd as P
 from paper_2609_20359_amd import flround as F
 
@@ -102,3 +104,15 @@ def test_both_sides_of_the_limits_of_top_logits():
             assert L.fl_top_workspace_bytes(rows, vocab, dtype, k) == 0
             assert top(rows, vocab, k, dtype) == INVALID
         assert L.fl_top_workspace_bytes(1, 1 << 20, dtype, 128) > 0
+
+
+def test_binding_refuses_listed_words_that_are_no_matrix():
+    import torch
+
+    b, f = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(4)
+    for ids in (torch.tensor(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32),
+                torch.zeros(4, 2, 1, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="2-D"):
+            P.fl_head_distill(b, b, ids, f, None, 1.0, f, f, f)
+        with pytest.raises(ValueError, match="2-D"):
+            P.fl_head_distill_grad(b, b, ids, f, None, 1.0, f, f, f, b, b)
