@@ -205,7 +205,7 @@ __device__ __forceinline__ u32x4 eight(u32x2 a, u32x2 b) {
 enum Epilogue { kStats, kGrad, kSlab, kOut };
 
 // What bounds it: the matrix cores, at the clock that the power leaves them.
-// They are busy in 80 % of the cycles of the loss's product and 68 to 72 % of
+// They are busy in 78 % of the cycles of the loss's product and 66 to 68 % of
 // the gradient's, no read of LDS meets a bank conflict, and a step of 256 x 256
 // outputs takes 1.43 us.  4096 live rows, 128256 words, 4096 wide, in PFLOP/s:
 // 1.37 for the statistics, 1.24 for G (0.87 ms a piece of 32256 words), 1.26 for
@@ -215,6 +215,11 @@ enum Epilogue { kStats, kGrad, kSlab, kOut };
 // CU's 128 KiB go out at once and the next tile's first step waits for them.  2048
 // and fewer rows lose 10 to 15 % where the weight comes from HBM in every round of
 // tiles, a step's loads being one step ahead.
+//
+// The 256 x 256 tiles take all 256 registers of a lane and spill some: 15 of the
+// statistics', 17 of G's, 4 of dW's, 8 of the sums', to 20 to 72 bytes of scratch.
+// All of it is in a tile's last two steps and its epilogue, where the next tile's
+// addresses are alive beside this one's; the loop over the steps has none.
 //
 // Why these tiles: eight waves of 128 x 64 outputs read 96 KiB of LDS a step of
 // 64, a third of what LDS can give in that time, and keep their sums in 128
@@ -742,7 +747,7 @@ __device__ __forceinline__ bool is_live(const HeadArgs& a, int64_t t) {
 // (7 tokens x 1000 x 96: 18.5 us for 21.6).
 //
 // The listed words' rows are what takes time: 1000 tokens of 64 words are 0.52 GB
-// of the weight, 94 us (5.6 TB/s; 130 with one word at a time), a tenth of the
+// of the weight, 91 us (5.8 TB/s; 130 with one word at a time), a tenth of the
 // call.  The product's tiles hold these logits too, but looking for them there took
 // as long and cost the loss of labels registers.
 constexpr int kScan = 1024;

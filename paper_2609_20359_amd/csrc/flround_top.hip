@@ -15,7 +15,7 @@
 // Rows longer than a segment are joined by a second kernel, in which an entry's
 // place is the sum of its places in the segments' sorted lists.
 //
-// Measured: 64 of 2048 rows of 128256 in bf16, 525 MB, in 117 us (4.5 TB/s; with
+// Measured: 64 of 2048 rows of 128256 in bf16, 525 MB, in 119 us (4.4 TB/s; with
 // the values kept as floats, 239 registers and one workgroup per SIMD, 330); 100
 // of 100 rows of 100003 in fp32 in 23 us; 8 of one row of 50257 in 12 us, most of
 // it two launches.  The selection has no loads out; the other workgroups of a CU,
