@@ -14,12 +14,13 @@ constexpr int kMaxTargets = 128;  // listed teacher logits per token
 
 // The gradient of a call of up to this many tokens, whether they take part or not,
 // has two rows for each: G rounded to bf16, and what that leaves, rounded too, which
-// makes G's error 2^-16 of an entry instead of 2^-8.  Off by, in the 2-norm, of 50257
-// words, 1024 wide: 1.7e-3 of 32 tokens, which is the results' own rounding, and
-// 2.3e-3 of 33 with one row each.  Both rows of 32 tokens fit the products' smallest
-// tiles, of 64 rows (102 us, 96 for 33); beyond, they would be two products more for
-// the three that there are.  The choice is the host's, which does not know how many
-// tokens take part.
+// makes G's error 2^-16 of an entry instead of 2^-8.  Of 50257 words, 1024 wide, the
+// gradients of 32 tokens are off by at most 1.7e-3 in the 2-norm, the results' own
+// rounding; those of 33 tokens, with one row each, by 1.8e-3 to 1.9e-3 with labels and
+// 2.3e-3 to 2.5e-3 with 16 listed words.  Both rows of 32 tokens fit the products'
+// smallest tiles, of 64 rows (102 and 110 us; 33 tokens 97 and 105); beyond, the two
+// products after G would be twice as long.  The choice is the host's, which does not
+// know how many tokens take part.
 constexpr int kTwiceTokens = 32;
 
 // Written by the first kernel of a call.

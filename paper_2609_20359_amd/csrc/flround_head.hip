@@ -465,7 +465,7 @@ __device__ __forceinline__ void tile_work(const TileArgs& a, int block, int bloc
     } else if constexpr (EPI == kGrad) {
       // G is rounded to bf16, what the matrix cores multiply with bf16 hidden states
       // and weights: its entries' error, up to 2^-8, takes the gradients' in the
-      // 2-norm from the results' own rounding, 1.7e-3, to 1.8e-3 to 2.4e-3.  With a
+      // 2-norm from the results' own rounding, 1.7e-3, to 1.8e-3 to 2.5e-3.  With a
       // second row for what that leaves (copies) the two products that follow would
       // be twice as long; up to kTwiceTokens tokens have it.
       const bool inside = p0 + BP <= a.np && q0 + BQ <= n_live;
@@ -629,7 +629,7 @@ __device__ __forceinline__ float wave_max(float x) {
   return x;
 }
 
-// None of these takes more than 25 us at 4096 tokens, but k_pack where many words
+// None of these takes more than 27 us at 4096 tokens, but k_pack where many words
 // are listed.
 
 // The teacher's log probabilities of the listed words, one wave per token.  NaN,
@@ -990,7 +990,7 @@ __global__ __launch_bounds__(256) void k_fix(const HeadArgs a, uint16_t* G, int6
 }
 
 // The gradient of the hidden state from the splits' fp32 sums, added in order
-// (bound by memory: 4096 x 4096 of one split, 101 MB, in 22 us).
+// (bound by memory: 4096 x 4096 of one split, 101 MB, in 26 us).
 __global__ __launch_bounds__(256) void k_dh(const HeadArgs a, const float* slab, int64_t ld_slab,
                                             int bp, int bq, int fit, int max_splits,
                                             float out_scale) {
