@@ -449,7 +449,8 @@ int fl_round_hsdp(const fl_layout* layout, const fl_round_cfg* cfg, const fl_hsd
  * in any way), and weight to 16 bytes where width and stride are multiples of 8.
  * hidden and weight may have longer rows than they use (the strides, in elements;
  * 0: rows follow each other).  Weight rows of another width or stride are copied
- * to the workspace by every call.
+ * to the workspace by every call.  Outputs and the workspace overlap neither each
+ * other nor an input (a gradient at an input's own address is refused).
  *
  * workspace: device memory, fl_head_workspace_bytes(shape, k, grad) bytes
  *   (k = 0 for fl_head_loss and its gradient; grad nonzero for the gradients;
