@@ -60,7 +60,8 @@ typedef enum {
   FL_ERR_NOMEM = -6,   /* host or device allocation failed                      */
   FL_ERR_SCRATCH = -7  /* fl_round_noalloc: the layout's per-segment workspace
                           exceeds the library's static scratch; fl_head_*,
-                          fl_top_logits: the workspace given is too small      */
+                          fl_top_logits, fl_embed_grad, fl_layer_norm_grad: the
+                          workspace given is too small                         */
 } fl_status;
 
 #define FL_MAX_PEERS 64  /* upper bound on R */
@@ -75,7 +76,8 @@ const char* fl_status_string(int status);
  * points; 2: the outer step; 3: fl_lr_cosine and fl_round_cfg.step_lr;
  * 4: fl_round_cfg.max_grad_norm and the clipping entry points;
  * 5: fl_round_cfg.grad_scratch; 8: the output head (fl_head_*,
- * fl_top_logits). */
+ * fl_top_logits); 9: the embedding and the layer norm (fl_embed*,
+ * fl_layer_norm*). */
 int fl_version(void);
 
 /* ------------------------------------------------------------------------
@@ -547,6 +549,80 @@ size_t fl_top_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int k);
 int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const void* logits, int k,
                   float tau, float* values, int32_t* ids, float* lse, void* workspace,
                   size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The embedding and the layer norm: the two ends of a model beside its output head.
+ *
+ * The conventions of the output head hold (no layout handle; pointers aligned to
+ * their elements; strides in elements, 0: rows follow each other; outputs and the
+ * workspace overlap neither each other nor an input; no call allocates or
+ * synchronises, and all may be captured into a HIP graph).  dtype is that of the
+ * rows and weights, FL_BF16 or FL_F32; sums are in fp32 in an order that is fixed
+ * for given sizes (the same call gives the same bits), and a result is rounded once.
+ *
+ * fl_embed -- the embedding's rows of T tokens:
+ *     out[t][d] = scale * weight[ids[t]][d]
+ *   ids: device, T int64.  A negative id takes no part: its row is 0.  One >= V gives
+ *   a row of NaN.  weight: V x D (stride: elements between its rows); out: T x D.
+ *   scale finite.
+ *
+ * fl_embed_grad -- gradient of sum_td dout[t][d] * out[t][d]:
+ *     dweight[v][d] = scale * sum over t with ids[t] == v of dout[t][d]
+ *   summed in ascending order of t (in parts of 16 or 64 tokens of the sorted ones).
+ *   add == 0: all V x D of it are written; else the sum is added to what stands in
+ *   the rows of the words that occur, rounded once, and the other rows are left alone
+ *   (tied weights, several batches).  A negative id, or one >= V, takes no part: its
+ *   row of dout is not looked at.  dout: T x D (stride: elements between its rows).
+ *   workspace: fl_embed_workspace_bytes (0 is returned for an invalid shape); less:
+ *   FL_ERR_SCRATCH.
+ *
+ * fl_layer_norm -- with E(.) the mean over a row's D elements:
+ *     mean[r] = E(x[r]);  rstd[r] = 1 / sqrt(E((x[r] - mean[r])^2) + eps)
+ *     y[r][d] = (x[r][d] - mean[r]) * rstd[r] * weight[d] + bias[d]
+ *   rms nonzero: the mean is taken as 0 (root mean square norm).  weight, bias: D
+ *   values of dtype, or NULL (1 and 0).  x: R rows (x_stride); y: R x D; mean, rstd: R
+ *   floats (mean may be NULL), which the gradient needs.  eps finite, >= 0.
+ *
+ * fl_layer_norm_grad -- gradient of sum_rd dy[r][d] * y[r][d], at mean and rstd as
+ *   fl_layer_norm wrote them; with xh = (x[r] - mean[r]) * rstd[r], c = dy[r] * weight:
+ *     dx[r] = rstd[r] * (c - E(c) - xh * E(c * xh))     (rms: without E(c))
+ *     dweight = sum_r dy[r] * xh;  dbias = sum_r dy[r]
+ *   dx: R x D; dweight, dbias: D values of dtype, or NULL; all are written, not added
+ *   to.  dy: R rows (dy_stride).  mean is not read with rms.  workspace:
+ *   fl_layer_norm_workspace_bytes.
+ *
+ * Limits (FL_ERR_INVALID beyond): tokens and rows <= 2^20, vocab <= 2^21, width <=
+ * 2^15, strides <= 2^40.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t tokens; /* T >= 0                                                  */
+  int64_t vocab;  /* V >= 1                                                  */
+  int64_t width;  /* D >= 1                                                  */
+  int64_t stride; /* between rows of weight (fl_embed) or dout (its gradient) */
+  int dtype;      /* FL_BF16 or FL_F32                                       */
+} fl_embed_shape;
+
+typedef struct {
+  int64_t rows;      /* R >= 0                    */
+  int64_t width;     /* D >= 1                    */
+  int64_t x_stride;  /* between rows of x         */
+  int64_t dy_stride; /* between rows of dy        */
+  int dtype;         /* FL_BF16 or FL_F32         */
+  int rms;           /* nonzero: no mean is taken */
+} fl_norm_shape;
+
+int fl_embed(const fl_embed_shape* shape, const int64_t* ids, const void* weight, float scale,
+             void* out, void* stream);
+size_t fl_embed_workspace_bytes(const fl_embed_shape* shape);
+int fl_embed_grad(const fl_embed_shape* shape, const int64_t* ids, const void* dout, float scale,
+                  int add, void* dweight, void* workspace, size_t workspace_bytes, void* stream);
+int fl_layer_norm(const fl_norm_shape* shape, const void* x, const void* weight, const void* bias,
+                  float eps, void* y, float* mean, float* rstd, void* stream);
+size_t fl_layer_norm_workspace_bytes(const fl_norm_shape* shape);
+int fl_layer_norm_grad(const fl_norm_shape* shape, const void* x, const void* weight,
+                       const float* mean, const float* rstd, const void* dy, void* dx,
+                       void* dweight, void* dbias, void* workspace, size_t workspace_bytes,
+                       void* stream);
 
 /* ------------------------------------------------------------------------
  * Launch-shape control, for tuning sweeps and for tests that check that

@@ -19,7 +19,10 @@ SOURCES = [os.path.join(HERE, "csrc", "flround_api.cpp"),
            os.path.join(HERE, "csrc", "flround_kernels.hip"),
            os.path.join(HERE, "csrc", "flround_head_api.cpp"),
            os.path.join(HERE, "csrc", "flround_head.hip"),
-           os.path.join(HERE, "csrc", "flround_top.hip")]
+           os.path.join(HERE, "csrc", "flround_top.hip"),
+           os.path.join(HERE, "csrc", "flround_layers_api.cpp"),
+           os.path.join(HERE, "csrc", "flround_embed.hip"),
+           os.path.join(HERE, "csrc", "flround_norm.hip")]
 
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "flr_launch.h"
+
 namespace flr {
 
 constexpr int kRowPad = 256;      // compacted rows are padded to this many
@@ -118,19 +120,6 @@ inline int tile_fit(int s) {   // tiles that the chip holds at a time, by LDS
 __host__ __device__ inline int splits_of(int fit, int tiles, int max_splits) {
   const int s = tiles > 0 ? fit / tiles : 1;
   return s < 1 ? 1 : s < max_splits ? s : max_splits;
-}
-
-// Enqueues a kernel.  The status is this launch's own: an error that an earlier call
-// of the runtime left behind is not this one's, and stays for who asks for it.
-template <typename T>
-struct Same {
-  using type = T;
-};
-template <typename... P>
-hipError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t lds, hipStream_t st,
-                  typename Same<P>::type... args) {
-  void* at[] = {static_cast<void*>(&args)...};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, lds, st);
 }
 
 hipError_t launch_head_teacher(const HeadArgs& a, hipStream_t st);

@@ -1,0 +1,65 @@
+// flr_layers.h -- types shared by the C-ABI layer of the embedding and the layer
+// norm (flround_layers_api.cpp) and their gfx950 kernels (flround_embed.hip,
+// flround_norm.hip).  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace flr {
+
+// The embedding and its gradient.
+struct EmbedArgs {
+  int64_t T, V, D, ld;     // ld: elements between rows of the input
+  bool bf16;               // elements of all rows: bf16, or fp32
+  const int64_t* ids;
+  const void* in;          // the weight (V rows), or the gradient of the output (T rows)
+  float scale;
+  void* out;               // T x D, or the weight's gradient (V x D)
+  int add;                 // gradient: added to what stands there
+  // gradient's plan and workspace
+  int words;               // words whose tokens one workgroup of the sort finds
+  int sort_waves;
+  int tile;                // sorted tokens that one wave sums
+  int32_t* start;          // V + 1: word v's tokens are order[start[v] .. start[v + 1])
+  int32_t* order;          // tokens by word, those of a word in ascending order
+  float* slab;             // two rows of D per tile: sums of words that go on beyond it
+};
+
+constexpr int kEmbedMaxWords = 1024;
+constexpr int kEmbedMaxWaves = 16;
+
+// The layer norm and its gradient.
+struct NormArgs {
+  int64_t T, D, ldx, ldy;  // ldy: elements between rows of dy
+  bool bf16, rms;
+  const void* x;
+  const void* weight;      // null: ones
+  const void* bias;        // null: zeros
+  float eps;
+  const float* mean_in;    // gradient
+  const float* rstd_in;
+  const void* dy;
+  void* y;                 // or dx
+  float* mean;             // may be null
+  float* rstd;
+  void* dweight;           // either may be null
+  void* dbias;
+  float* parts;            // n_parts rows of D for dweight, then as many for dbias
+  int64_t n_parts;         // workgroups of the gradient
+};
+
+// How a row lies in a workgroup: waves to a row, and 16-byte chunks to a lane.
+struct NormShape {
+  int waves, chunks;
+  int rows() const { return waves < 4 ? 4 / waves : 1; }   // rows that a workgroup takes at once
+};
+NormShape norm_shape(int64_t rows, int64_t width, bool bf16, bool grad);
+
+hipError_t launch_norm(const NormArgs& a, hipStream_t st);
+hipError_t launch_norm_grad(const NormArgs& a, hipStream_t st);
+
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t st);
+hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st);
+
+}  // namespace flr

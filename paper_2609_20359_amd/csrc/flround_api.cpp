@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "flr_internal.h"
+#include "flr_scalars.h"
 #include "flround.h"
 
 using flr::kTile;
@@ -41,6 +42,53 @@ struct fl_layout {
   // failed; fl_round_noalloc then reports FL_ERR_HIP when it needs it).
   void* noalloc = nullptr;
 };
+
+namespace {
+
+bool finite(float x) { return std::isfinite(x); }
+
+}  // namespace
+
+namespace flr {
+
+bool hparams_ok(const fl_adamw_hparams* h) {
+  if (!h) return false;
+  if (!finite(h->lr) || !finite(h->beta1) || !finite(h->beta2) || !finite(h->eps) ||
+      !finite(h->weight_decay))
+    return false;
+  if (!(h->lr >= 0.f)) return false;
+  if (!(h->beta1 >= 0.f && h->beta1 < 1.f)) return false;
+  if (!(h->beta2 >= 0.f && h->beta2 < 1.f)) return false;
+  if (!(h->eps > 0.f)) return false;
+  if (!(h->weight_decay >= 0.f)) return false;
+  return true;
+}
+
+// Per-step scalars: double on the host, each rounded once to float.
+AdamScalars adam_scalars(const fl_adamw_hparams& h, int64_t step) {
+  const double lr = (double)h.lr;
+  const double t = (double)step;
+  AdamScalars s;
+  s.b1 = h.beta1;
+  s.b2 = h.beta2;
+  s.omb1 = (float)(1.0 - (double)h.beta1);
+  s.omb2 = (float)(1.0 - (double)h.beta2);
+  s.step_size = (float)(lr / (1.0 - std::pow((double)h.beta1, t)));
+  s.bc2_sqrt = (float)std::sqrt(1.0 - std::pow((double)h.beta2, t));
+  s.eps = h.eps;
+  s.decay = (float)(1.0 - lr * (double)h.weight_decay);
+  // With these bounds, and the kernel's on the moments, no operand or result
+  // of the short forms leaves the normal range (the root is at most 2^30, the
+  // denominator between 2^-60 and 2^44, the quotient within 2^-104 to 2^90).
+  const bool short_forms = s.eps >= 0x1p-60f && s.eps <= 0x1p40f && s.bc2_sqrt >= 0x1p-13f;
+  s.rbc2 = short_forms ? (float)(1.0 / (double)s.bc2_sqrt) : 0.f;
+  return s;
+}
+
+}  // namespace flr
+
+using flr::adam_scalars;
+using flr::hparams_ok;
 
 namespace {
 
@@ -79,42 +127,6 @@ uint64_t fingerprint_of(int64_t n, int64_t n_seg, const int64_t* off, const uint
     h = fnv_bytes(h, &f, 1);
   }
   return h;
-}
-
-bool finite(float x) { return std::isfinite(x); }
-
-bool hparams_ok(const fl_adamw_hparams* h) {
-  if (!h) return false;
-  if (!finite(h->lr) || !finite(h->beta1) || !finite(h->beta2) || !finite(h->eps) ||
-      !finite(h->weight_decay))
-    return false;
-  if (!(h->lr >= 0.f)) return false;
-  if (!(h->beta1 >= 0.f && h->beta1 < 1.f)) return false;
-  if (!(h->beta2 >= 0.f && h->beta2 < 1.f)) return false;
-  if (!(h->eps > 0.f)) return false;
-  if (!(h->weight_decay >= 0.f)) return false;
-  return true;
-}
-
-// Per-step scalars: double on the host, each rounded once to float.
-flr::AdamScalars adam_scalars(const fl_adamw_hparams& h, int64_t step) {
-  const double lr = (double)h.lr;
-  const double t = (double)step;
-  flr::AdamScalars s;
-  s.b1 = h.beta1;
-  s.b2 = h.beta2;
-  s.omb1 = (float)(1.0 - (double)h.beta1);
-  s.omb2 = (float)(1.0 - (double)h.beta2);
-  s.step_size = (float)(lr / (1.0 - std::pow((double)h.beta1, t)));
-  s.bc2_sqrt = (float)std::sqrt(1.0 - std::pow((double)h.beta2, t));
-  s.eps = h.eps;
-  s.decay = (float)(1.0 - lr * (double)h.weight_decay);
-  // With these bounds, and the kernel's on the moments, no operand or result
-  // of the short forms leaves the normal range (the root is at most 2^30, the
-  // denominator between 2^-60 and 2^44, the quotient within 2^-104 to 2^90).
-  const bool short_forms = s.eps >= 0x1p-60f && s.eps <= 0x1p40f && s.bc2_sqrt >= 0x1p-13f;
-  s.rbc2 = short_forms ? (float)(1.0 / (double)s.bc2_sqrt) : 0.f;
-  return s;
 }
 
 // FedAvg weights w / sum(w): sum in double in index order.
@@ -563,7 +575,7 @@ const char* fl_status_string(int status) {
   }
 }
 
-int fl_version(void) { return (1 << 16) | 8; }
+int fl_version(void) { return (1 << 16) | 9; }
 
 float fl_lr_cosine(int64_t t, int64_t total_steps, int64_t warmup_steps, float lr_max,
                    float lr_min) {

@@ -40,7 +40,9 @@ EXPORTS = ("fl_status_string", "fl_version", "fl_layout_create", "fl_layout_dest
            "fl_lr_cosine", "fl_grad_sumsq", "fl_local_step_clipped", "fl_round_noalloc",
            "fl_noalloc_workspace_bytes", "fl_head_workspace_bytes", "fl_head_loss",
            "fl_head_loss_grad", "fl_head_distill", "fl_head_distill_grad",
-           "fl_top_workspace_bytes", "fl_top_logits")
+           "fl_top_workspace_bytes", "fl_top_logits", "fl_embed", "fl_embed_workspace_bytes",
+           "fl_embed_grad", "fl_layer_norm", "fl_layer_norm_workspace_bytes",
+           "fl_layer_norm_grad")
 
 _P = ctypes.c_void_p
 
@@ -86,6 +88,16 @@ class HsdpCfg(ctypes.Structure):
 class HeadShape(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_int64), ("vocab", ctypes.c_int64), ("width", ctypes.c_int64),
                 ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64)]
+
+
+class EmbedShape(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("vocab", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("stride", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("x_stride", ctypes.c_int64),
+                ("dy_stride", ctypes.c_int64), ("dtype", ctypes.c_int), ("rms", ctypes.c_int)]
 
 
 _lib = None
@@ -154,6 +166,17 @@ def lib():
         L.fl_top_logits.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int,
                                     _P, ctypes.c_int, ctypes.c_float, _P, _P, _P, _P,
                                     ctypes.c_size_t, _P]
+        shape = ctypes.POINTER(EmbedShape)
+        L.fl_embed.argtypes = [shape, _P, _P, ctypes.c_float, _P, _P]
+        L.fl_embed_workspace_bytes.argtypes = [shape]
+        L.fl_embed_workspace_bytes.restype = ctypes.c_size_t
+        L.fl_embed_grad.argtypes = [shape, _P, _P, ctypes.c_float, ctypes.c_int, _P, _P,
+                                    ctypes.c_size_t, _P]
+        shape = ctypes.POINTER(NormShape)
+        L.fl_layer_norm.argtypes = [shape, _P, _P, _P, ctypes.c_float, _P, _P, _P, _P]
+        L.fl_layer_norm_workspace_bytes.argtypes = [shape]
+        L.fl_layer_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.fl_layer_norm_grad.argtypes = [shape] + [_P] * 9 + [ctypes.c_size_t, _P]
         L.fl_set_blocks_per_cu.argtypes = [ctypes.c_int]
         L.fl_set_blocks_per_cu.restype = ctypes.c_int
         _lib = L
@@ -738,6 +761,127 @@ def fl_top_logits(logits, k, tau, values, ids, lse=None, workspace=None, stream=
     rc = lib().fl_top_logits(n, v, stride, dtype, p, k, float(tau), *args, ws, ws_bytes,
                              _stream(stream))
     _check(rc, "fl_top_logits")
+
+
+# ---- the embedding and the layer norm ----------------------------------------
+
+
+def _row_dtypes():
+    torch = _T or _torch()
+    return torch.bfloat16, torch.float32
+
+
+def _fl_dtype(t):
+    return FL_BF16 if t.dtype is _T.bfloat16 else FL_F32
+
+
+@functools.lru_cache(maxsize=256)
+def _embed_shape(T, V, D, stride, dtype):
+    """The shape as the library takes it, and the bytes of workspace for its gradient."""
+    s = EmbedShape(T, V, D, stride, dtype)
+    return ctypes.byref(s), lib().fl_embed_workspace_bytes(ctypes.byref(s))
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_shape(R, D, ldx, ldy, dtype, rms):
+    s = NormShape(R, D, ldx, ldy, dtype, rms)
+    return ctypes.byref(s), lib().fl_layer_norm_workspace_bytes(ctypes.byref(s))
+
+
+def embed_workspace_bytes(tokens, vocab, width, dtype=FL_BF16):
+    """Bytes of workspace that fl_embed_grad needs."""
+    return int(_embed_shape(tokens, vocab, width, 0, dtype)[1])
+
+
+def layer_norm_workspace_bytes(rows, width, dtype=FL_BF16):
+    """Bytes of workspace that fl_layer_norm_grad needs."""
+    return int(_norm_shape(rows, width, 0, 0, dtype, 0)[1])
+
+
+def _count(ids):
+    """The number of ids, a 1-D tensor."""
+    if ids.dim() != 1:
+        raise ValueError("ids must be a 1-D tensor")
+    return ids.shape[0]
+
+
+def fl_embed(ids, weight, out, scale=1.0, stream=None):
+    """out[t] = scale * weight[ids[t]]: ids (T int64, negative: the row is 0), weight
+    (V x D bf16 or float32, rows may be longer), out (T x D of its dtype)."""
+    dtypes = _row_dtypes()
+    dev = _device_of(weight, "weight")
+    w, ldw = _rows(weight, dtypes, dev, "weight")
+    V, D = weight.shape
+    T = _count(ids)
+    shape, _ = _embed_shape(T, V, D, ldw, _fl_dtype(weight))
+    rc = lib().fl_embed(shape, _array(ids, (T,), _T.int64, dev, "ids"), w, float(scale),
+                        _array(out, (T, D), weight.dtype, dev, "out"), _stream(stream))
+    _check(rc, "fl_embed")
+
+
+def fl_embed_grad(ids, dout, dweight, scale=1.0, add=False, workspace=None, stream=None):
+    """Gradient of sum(dout * out) by the weight: writes dweight (V x D, of dout's
+    dtype), or with add adds to the rows of the words that occur.  dout: T x D, rows
+    may be longer."""
+    dtypes = _row_dtypes()
+    dev = _device_of(dout, "dout")
+    d, ldd = _rows(dout, dtypes, dev, "dout")
+    T = _count(ids)
+    if dout.shape[0] != T:
+        raise ValueError("dout has %d rows, ids %d" % (dout.shape[0], T))
+    if dweight.dim() != 2:
+        raise ValueError("dweight must be a 2-D tensor")
+    V, D = dweight.shape[0], dout.shape[1]
+    shape, need = _embed_shape(T, V, D, ldd, _fl_dtype(dout))
+    keep, nbytes = _workspace(workspace, need, dev, stream)
+    rc = lib().fl_embed_grad(shape, _array(ids, (T,), _T.int64, dev, "ids"), d, float(scale),
+                             1 if add else 0, _array(dweight, (V, D), dout.dtype, dev, "dweight"),
+                             keep.data_ptr(), nbytes, _stream(stream))
+    _check(rc, "fl_embed_grad")
+
+
+def fl_layer_norm(x, weight, bias, eps, y, mean, rstd, rms=False, stream=None):
+    """Layer norm of the rows of x (R x D bf16 or float32, rows may be longer) into y;
+    weight and bias (D, or None) and y have x's dtype.  Writes mean (or None) and rstd
+    (R float32), which the gradient takes.  rms: root mean square norm, without a mean."""
+    dtypes = _row_dtypes()
+    dev = _device_of(x, "x")
+    p, ldx = _rows(x, dtypes, dev, "x")
+    R, D = x.shape
+    dt, f32 = x.dtype, dtypes[1]
+    shape, _ = _norm_shape(R, D, ldx, 0, _fl_dtype(x), 1 if rms else 0)
+    rc = lib().fl_layer_norm(shape, p,
+                             None if weight is None else _array(weight, (D,), dt, dev, "weight"),
+                             None if bias is None else _array(bias, (D,), dt, dev, "bias"),
+                             float(eps), _array(y, (R, D), dt, dev, "y"),
+                             None if mean is None else _array(mean, (R,), f32, dev, "mean"),
+                             _array(rstd, (R,), f32, dev, "rstd"), _stream(stream))
+    _check(rc, "fl_layer_norm")
+
+
+def fl_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight, dbias, rms=False, workspace=None,
+                       stream=None):
+    """Gradient of sum(dy * y) of fl_layer_norm: writes dx (R x D), dweight and dbias (D
+    each, or None), all of x's dtype.  mean (None with rms) and rstd as fl_layer_norm
+    wrote them; rows of x and dy may be longer."""
+    dtypes = _row_dtypes()
+    dev = _device_of(x, "x")
+    p, ldx = _rows(x, dtypes, dev, "x")
+    R, D = x.shape
+    dt, f32 = x.dtype, dtypes[1]
+    g, ldy = _rows(dy, (dt,), dev, "dy")
+    if dy.shape != x.shape:
+        raise ValueError("dy has shape %s, x %s" % (tuple(dy.shape), tuple(x.shape)))
+    shape, need = _norm_shape(R, D, ldx, ldy, _fl_dtype(x), 1 if rms else 0)
+    keep, nbytes = _workspace(workspace, need, dev, stream)
+    rc = lib().fl_layer_norm_grad(
+        shape, p, None if weight is None else _array(weight, (D,), dt, dev, "weight"),
+        None if mean is None else _array(mean, (R,), f32, dev, "mean"),
+        _array(rstd, (R,), f32, dev, "rstd"), g, _array(dx, (R, D), dt, dev, "dx"),
+        None if dweight is None else _array(dweight, (D,), dt, dev, "dweight"),
+        None if dbias is None else _array(dbias, (D,), dt, dev, "dbias"), keep.data_ptr(), nbytes,
+        _stream(stream))
+    _check(rc, "fl_layer_norm_grad")
 
 
 # ---- HIP events (for fl_round's per-phase timing) -------------------------
