@@ -77,7 +77,8 @@ const char* fl_status_string(int status);
  * 4: fl_round_cfg.max_grad_norm and the clipping entry points;
  * 5: fl_round_cfg.grad_scratch; 8: the output head (fl_head_*,
  * fl_top_logits); 9: the embedding and the layer norm (fl_embed*,
- * fl_layer_norm*). */
+ * fl_layer_norm*) and AdamW over many tensors (fl_adamw_tensors,
+ * fl_tensors_*, fl_state_convert). */
 int fl_version(void);
 
 /* ------------------------------------------------------------------------
@@ -623,6 +624,62 @@ int fl_layer_norm_grad(const fl_norm_shape* shape, const void* x, const void* we
                        const float* mean, const float* rstd, const void* dy, void* dx,
                        void* dweight, void* dbias, void* workspace, size_t workspace_bytes,
                        void* stream);
+
+/* ------------------------------------------------------------------------
+ * AdamW over many tensors, with moments in 32 or in 8 bits: for parameters that are not
+ * one flat shard (a model that one GPU holds whole, its embedding, norms and head), and
+ * where 8 bytes of moments for a parameter are too many.
+ *
+ * fl_adamw_tensors -- fl_adamw_step of each tensor, with g[i] = f32(grads[k][i]) *
+ *   grad_scale, in one launch for up to 96 tensors; a parameter's arithmetic is that of
+ *   fl_adamw_step, bit for bit.  tensors: host array, read during the call; grads: host
+ *   array of `count` device pointers to values of grad_dtype (FL_BF16 or FL_F32).  A
+ *   tensor whose gradient is NULL is left alone, its moments too; an empty tensor's
+ *   pointers are not looked at.  master, working and gradients are aligned to their
+ *   elements; masters and working copies overlap neither each other nor a gradient (a
+ *   tensor is listed once).  step, h: as for fl_adamw_step; grad_scale finite.  There is
+ *   no layout handle; the device is the current one; nothing is allocated, and calls may
+ *   be captured into a HIP graph (which keeps the step's scalars as they are).
+ *
+ *   state: device, 16-byte aligned, fl_tensors_state_bytes bytes, all zero before the
+ *   first step.  With S = fl_tensors_state_numel (each tensor's elements rounded up to a
+ *   multiple of 512, one after the other; those behind a tensor's last stay 0), it holds
+ *     32 bits: S floats m, S floats v;
+ *      8 bits: S codes of m, S of v, S / 64 exponent bytes of m, S / 64 of v.
+ *   A block of 64 elements shares an exponent byte b: the exponent field of its largest
+ *   finite magnitude as a float, one more where that one's mantissa is over 1.75, 12 at
+ *   least.  A code of m is a sign, 4 bits of exponent E and 3 of mantissa M, of v 5 and 3;
+ *   with T = 15 or 31 it stands for 2^(b - 127 + E - T) (1 + M / 8), or, where E = 0, for
+ *   2^(b - 126 - T) M / 8; E = T with M = 7 stands for NaN, and an infinite moment is held
+ *   as NaN.  A moment in 32 bits (as AdamW defines it; the update itself takes it so)
+ *   becomes a code
+ *     seed == 0: by rounding to nearest, ties to even;
+ *     else: up with the probability of its place between the two codes (to 2^-20),
+ *     with random bits that depend on seed, step and the element's place in state alone.
+ *   A v above 0 is at least the smallest code.  seed must be 0 with 32 bits.
+ *   Rounding to nearest is what holds a moment that moves by less than half a code's
+ *   step (3 to 6 %) where it is; a seed lets it move on average.
+ *
+ * fl_state_convert -- a state from 8 bits to 32 (exact), or from 32 to 8 (to nearest):
+ *   from_bits 8 or 32; `to` has the other form.  state_numel: S.  Both 16-byte aligned.
+ *
+ * fl_tensors_state_numel returns -1, fl_tensors_state_bytes 0 for invalid arguments.
+ * Limit: S <= 2^41.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t numel;     /* >= 0                                  */
+  float* master;     /* device, numel floats, updated         */
+  uint16_t* working; /* device, numel bf16, written; or NULL  */
+  int decay;         /* nonzero: takes weight decay           */
+} fl_tensor;
+
+int64_t fl_tensors_state_numel(int64_t count, const fl_tensor* tensors);
+size_t fl_tensors_state_bytes(int64_t state_numel, int state_bits);
+int fl_adamw_tensors(int64_t count, const fl_tensor* tensors, const void* const* grads,
+                     int grad_dtype, float grad_scale, const fl_adamw_hparams* h, int64_t step,
+                     int state_bits, void* state, uint64_t seed, void* stream);
+int fl_state_convert(int64_t state_numel, int from_bits, const void* from, void* to,
+                     void* stream);
 
 /* ------------------------------------------------------------------------
  * Launch-shape control, for tuning sweeps and for tests that check that

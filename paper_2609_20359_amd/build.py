@@ -22,7 +22,9 @@ SOURCES = [os.path.join(HERE, "csrc", "flround_api.cpp"),
            os.path.join(HERE, "csrc", "flround_top.hip"),
            os.path.join(HERE, "csrc", "flround_layers_api.cpp"),
            os.path.join(HERE, "csrc", "flround_embed.hip"),
-           os.path.join(HERE, "csrc", "flround_norm.hip")]
+           os.path.join(HERE, "csrc", "flround_norm.hip"),
+           os.path.join(HERE, "csrc", "flround_tensors_api.cpp"),
+           os.path.join(HERE, "csrc", "flround_tensors.hip")]
 
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -42,7 +42,8 @@ EXPORTS = ("fl_status_string", "fl_version", "fl_layout_create", "fl_layout_dest
            "fl_head_loss_grad", "fl_head_distill", "fl_head_distill_grad",
            "fl_top_workspace_bytes", "fl_top_logits", "fl_embed", "fl_embed_workspace_bytes",
            "fl_embed_grad", "fl_layer_norm", "fl_layer_norm_workspace_bytes",
-           "fl_layer_norm_grad")
+           "fl_layer_norm_grad", "fl_tensors_state_numel", "fl_tensors_state_bytes",
+           "fl_adamw_tensors", "fl_state_convert")
 
 _P = ctypes.c_void_p
 
@@ -98,6 +99,11 @@ class EmbedShape(ctypes.Structure):
 class NormShape(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("x_stride", ctypes.c_int64),
                 ("dy_stride", ctypes.c_int64), ("dtype", ctypes.c_int), ("rms", ctypes.c_int)]
+
+
+class FlTensor(ctypes.Structure):
+    _fields_ = [("numel", ctypes.c_int64), ("master", ctypes.c_void_p),
+                ("working", ctypes.c_void_p), ("decay", ctypes.c_int)]
 
 
 _lib = None
@@ -177,6 +183,14 @@ def lib():
         L.fl_layer_norm_workspace_bytes.argtypes = [shape]
         L.fl_layer_norm_workspace_bytes.restype = ctypes.c_size_t
         L.fl_layer_norm_grad.argtypes = [shape] + [_P] * 9 + [ctypes.c_size_t, _P]
+        L.fl_tensors_state_numel.argtypes = [ctypes.c_int64, _P]
+        L.fl_tensors_state_numel.restype = ctypes.c_int64
+        L.fl_tensors_state_bytes.argtypes = [ctypes.c_int64, ctypes.c_int]
+        L.fl_tensors_state_bytes.restype = ctypes.c_size_t
+        L.fl_adamw_tensors.argtypes = [ctypes.c_int64, _P, _P, ctypes.c_int, ctypes.c_float,
+                                       ctypes.POINTER(AdamwHparams), ctypes.c_int64,
+                                       ctypes.c_int, _P, ctypes.c_uint64, _P]
+        L.fl_state_convert.argtypes = [ctypes.c_int64, ctypes.c_int, _P, _P, _P]
         L.fl_set_blocks_per_cu.argtypes = [ctypes.c_int]
         L.fl_set_blocks_per_cu.restype = ctypes.c_int
         _lib = L
@@ -882,6 +896,138 @@ def fl_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight, dbias, rms=False,
         None if dbias is None else _array(dbias, (D,), dt, dev, "dbias"), keep.data_ptr(), nbytes,
         _stream(stream))
     _check(rc, "fl_layer_norm_grad")
+
+
+# ---- AdamW over many tensors --------------------------------------------------
+
+
+def _whole(t, dtype, what):
+    """Checks a contiguous CUDA tensor of this dtype."""
+    if not getattr(t, "is_cuda", False):
+        raise ValueError("%s must be a CUDA tensor" % what)
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor" % (what, dtype))
+
+
+class Tensors:
+    """Parameters that fl_adamw_tensors steps together: float32 masters and their bf16
+    working copies (None, or None for some: not written), all of one device, and which of
+    them decay (default: all).  It keeps the tensors and their addresses: make another one
+    when a parameter moves to other memory.
+
+    n_state: elements of each moment; state(bits) gives a state before the first step."""
+
+    def __init__(self, masters, workings=None, decays=None):
+        torch = _T or _torch()
+        self.masters = list(masters)
+        count = len(self.masters)
+        self.workings = [None] * count if workings is None else list(workings)
+        decays = [True] * count if decays is None else list(decays)
+        for name, xs in (("workings", self.workings), ("decays", decays)):
+            if len(xs) != count:
+                raise ValueError("%s has %d entries; expected %d" % (name, len(xs), count))
+        self.array = (FlTensor * max(count, 1))()
+        self.device = None
+        places = []
+        for i, (m, w) in enumerate(zip(self.masters, self.workings)):
+            for t, dtype, what in ((m, torch.float32, "masters"), (w, torch.bfloat16, "workings")):
+                if t is None and what == "workings":
+                    continue
+                _whole(t, dtype, "%s[%d]" % (what, i))
+                if self.device is None:
+                    self.device = t.get_device()
+                _on_device(t, self.device, "%s[%d]" % (what, i))
+                if t.numel() != m.numel():
+                    raise ValueError("workings[%d] has %d elements; expected %d"
+                                     % (i, t.numel(), m.numel()))
+                places.append((t.data_ptr(), t.numel() * t.element_size(), "%s[%d]" % (what, i)))
+            self.array[i] = FlTensor(m.numel(), m.data_ptr(), None if w is None else w.data_ptr(),
+                                     1 if decays[i] else 0)
+        places = sorted(p for p in places if p[1])
+        for a, b in zip(places, places[1:]):
+            if a[0] + a[1] > b[0]:
+                raise ValueError("%s and %s overlap" % (a[2], b[2]))
+        self.count = count
+        self.sizes = [m.numel() for m in self.masters]
+        self.n_state = int(lib().fl_tensors_state_numel(count, self.array))
+
+    def state(self, bits=8):
+        """Moments of zero: a uint8 tensor for 8 bits, a float32 one (m, then v) for 32."""
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        nbytes = int(lib().fl_tensors_state_bytes(self.n_state, bits))
+        dtype = _T.uint8 if bits == 8 else _T.float32
+        device = "cuda" if self.device is None else "cuda:%d" % self.device
+        return _T.zeros(nbytes if bits == 8 else nbytes // 4, dtype=dtype, device=device)
+
+
+def _state(t, n, dev, what):
+    """(address, bits) of the moments of n elements."""
+    torch = _T
+    if t.dtype is torch.uint8:
+        bits = 8
+    elif t.dtype is torch.float32:
+        bits = 32
+    else:
+        raise ValueError("%s must be a uint8 or a float32 tensor" % what)
+    size = lib().fl_tensors_state_bytes(n, bits) // t.element_size()
+    return _array(t, (size,), t.dtype, dev, what), bits
+
+
+def fl_adamw_tensors(tensors, hp, step, grads, state, grad_scale=1.0, seed=0, stream=None):
+    """One AdamW step of all `tensors` (a Tensors): grads holds a contiguous bf16 or
+    float32 gradient (all of one dtype) for each, or None for one that is left alone;
+    state as Tensors.state gives it, updated.  seed: nonzero rounds 8-bit moments by
+    random bits, whose expected value is the moment; 0 to nearest."""
+    torch = _T or _torch()
+    count, sizes = tensors.count, tensors.sizes
+    dev = _dev() if tensors.device is not None else None
+    if tensors.device != dev:
+        raise ValueError("the tensors are on device %s; the current device is %s"
+                         % (tensors.device, dev))
+    grads = list(grads)
+    if len(grads) != count:
+        raise ValueError("grads has %d entries; expected %d" % (len(grads), count))
+    ptrs, dtype = [], None
+    for i, g in enumerate(grads):
+        if g is None:
+            ptrs.append(None)
+            continue
+        if dtype is None:
+            dtype = g.dtype
+            if dtype is not torch.bfloat16 and dtype is not torch.float32:
+                raise ValueError("grads[%d] must be a bf16 or float32 tensor" % i)
+        if (g.dtype is dtype and g.numel() == sizes[i] and g.get_device() == dev
+                and g.is_contiguous()):
+            ptrs.append(g.data_ptr())
+            continue
+        # something is wrong with it: say what
+        _whole(g, dtype, "grads[%d]" % i)
+        _on_device(g, dev, "grads[%d]" % i)
+        raise ValueError("grads[%d] has %d elements; expected %d" % (i, g.numel(), sizes[i]))
+    if count == 0:
+        return
+    h = hparams(hp)
+    p, bits = _state(state, tensors.n_state, dev, "state")
+    rc = lib().fl_adamw_tensors(count, tensors.array, (ctypes.c_void_p * count)(*ptrs),
+                                FL_F32 if dtype is torch.float32 else FL_BF16, float(grad_scale),
+                                ctypes.byref(h), int(step), bits, p, int(seed), _stream(stream))
+    _check(rc, "fl_adamw_tensors")
+
+
+def fl_state_convert(src, dst, stream=None):
+    """The moments of an AdamW state in the other form: from 8 bits (uint8) to 32
+    (float32: m, then v), exactly, or from 32 to 8, to nearest."""
+    torch = _T or _torch()
+    dev = _device_of(src, "src")
+    if dst.dtype is not (torch.float32 if src.dtype is torch.uint8 else torch.uint8):
+        raise ValueError("one of src and dst must be a uint8, the other a float32 tensor")
+    wide = dst if src.dtype is torch.uint8 else src
+    n = wide.numel() // 2
+    p, bits = _state(src, n, dev, "src")
+    q, _ = _state(dst, n, dev, "dst")
+    rc = lib().fl_state_convert(n, bits, p, q, _stream(stream))
+    _check(rc, "fl_state_convert")
 
 
 # ---- HIP events (for fl_round's per-phase timing) -------------------------
