@@ -20,14 +20,17 @@ struct EmbedArgs {
   // gradient's plan and workspace
   int words;               // words whose tokens one workgroup of the sort finds
   int sort_waves;
+  int list;                // found tokens that a wave of the sort can list
   int tile;                // sorted tokens that one wave sums
   int32_t* start;          // V + 1: word v's tokens are order[start[v] .. start[v + 1])
-  int32_t* order;          // tokens by word, those of a word in ascending order
-  float* slab;             // two rows of D per tile: sums of words that go on beyond it
+  int2* order;             // (token, word), by word, a word's tokens in ascending order
+  float* slab;             // two rows per tile: sums of words that go on beyond it
+  int64_t ld_slab;
 };
 
-constexpr int kEmbedMaxWords = 1024;
+constexpr int kEmbedMaxWords = 512;
 constexpr int kEmbedMaxWaves = 16;
+constexpr int kEmbedMaxList = 1024;
 
 // The layer norm and its gradient.
 struct NormArgs {
@@ -49,12 +52,8 @@ struct NormArgs {
   int64_t n_parts;         // workgroups of the gradient
 };
 
-// How a row lies in a workgroup: waves to a row, and 16-byte chunks to a lane.
-struct NormShape {
-  int waves, chunks;
-  int rows() const { return waves < 4 ? 4 / waves : 1; }   // rows that a workgroup takes at once
-};
-NormShape norm_shape(int64_t rows, int64_t width, bool bf16, bool grad);
+// Rows that a workgroup of the gradient takes at once.
+int norm_rows(int64_t width, bool bf16);
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_grad(const NormArgs& a, hipStream_t st);

@@ -23,6 +23,10 @@ struct Rows<uint16_t> {
   static __device__ __forceinline__ void store(uint16_t* p, u32x4 w) {
     *reinterpret_cast<u32x4_at2*>(p) = w;
   }
+  // past the caches
+  static __device__ __forceinline__ void store_past(uint16_t* p, u32x4 w) {
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_at2*>(p));
+  }
   static __device__ __forceinline__ void floats(u32x4 w, float x[8]) {
     x[0] = bf16_lo(w.x), x[1] = bf16_hi(w.x), x[2] = bf16_lo(w.y), x[3] = bf16_hi(w.y);
     x[4] = bf16_lo(w.z), x[5] = bf16_hi(w.z), x[6] = bf16_lo(w.w), x[7] = bf16_hi(w.w);
@@ -50,6 +54,9 @@ struct Rows<float> {
   }
   static __device__ __forceinline__ void store(float* p, u32x4 w) {
     *reinterpret_cast<u32x4_at4*>(p) = w;
+  }
+  static __device__ __forceinline__ void store_past(float* p, u32x4 w) {
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_at4*>(p));
   }
   static __device__ __forceinline__ void floats(u32x4 w, float x[4]) {
     x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y);

@@ -17,68 +17,141 @@ __device__ __forceinline__ T uniform(const T* p) {
   return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
 }
 
-constexpr int kPiece = 4;   // chunks of a row that a lane holds at a time
-
-// out[t] = scale * weight[ids[t]].  A wave takes a piece of a row, all of its loads
-// first.
+// out[t] = scale * weight[ids[t]], one chunk to a lane, so that all that is read and
+// written at a time lies together.  Outputs larger than the L2s go past them (16384 rows
+// of 8 KiB, half of them of words that occur twice and more: 31.6 us, 46 through the
+// caches, 43 with four chunks to a lane).
 template <typename T>
-__global__ void __launch_bounds__(256) k_embed(const EmbedArgs a, int pieces) {
+__global__ void __launch_bounds__(256) k_embed(const EmbedArgs a, int pieces, bool past) {
   constexpr int E = Rows<T>::kE;
   const int lane = threadIdx.x & 63;
   const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int64_t t = w / pieces;
   if (t >= a.T) return;
-  const int64_t at = ((w - t * pieces) * kPiece * 64 + lane) * E;
+  const int64_t at = ((w - t * pieces) * 64 + lane) * E;
   const int64_t id = uniform(a.ids + t);
   T* out = static_cast<T*>(a.out) + t * a.D;
-  u32x4 x[kPiece];
-  if (id >= 0 && id < a.V) {
-    const T* row = static_cast<const T*>(a.in) + id * a.ld;
+  u32x4 x{0, 0, 0, 0};
+  if (id >= 0 && id < a.V) x = load_chunk(static_cast<const T*>(a.in) + id * a.ld, at, a.D);
+  float f[E];
+  Rows<T>::floats(x, f);
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) x[i] = load_chunk(row, at + i * 64 * E, a.D);
-  }
-#pragma unroll
-  for (int i = 0; i < kPiece; ++i) {
-    float f[E];
-    Rows<T>::floats(x[i], f);
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      f[e] = id < 0 ? 0.f : id >= a.V ? __builtin_nanf("") : f[e] * a.scale;
-    store_chunk(out, at + i * 64 * E, a.D, f);
-  }
+  for (int e = 0; e < E; ++e)
+    f[e] = id < 0 ? 0.f : id >= a.V ? __builtin_nanf("") : f[e] * a.scale;
+  if (past && at + E <= a.D) Rows<T>::store_past(out + at, Rows<T>::pack(f));
+  else store_chunk(out, at, a.D, f);
 }
 
 // The tokens by word.  A workgroup finds those of a.words words, and where they begin
-// among all, by reading every id twice: first each wave counts its share of the tokens
-// (a section of them, in order) for each word, and the tokens of all lower words; then,
-// from the sums of these counts, it knows where its next token of each word goes.  So
-// one launch sorts, stably, and nothing depends on which wave comes first.
-__global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedArgs a) {
-  extern __shared__ int32_t next[];   // [wave][word]
-  __shared__ int32_t sums[kEmbedMaxWaves];
-  __shared__ int32_t below_all;
+// among all, by reading every id: each wave counts its share of the tokens (a section of
+// them, in order) for each word, and the tokens of all lower words; from the sums of
+// these counts it knows where its next token of each word goes.  So one launch sorts,
+// stably, and nothing depends on which wave comes first.  A wave lists the tokens that it
+// finds (few, as all workgroups read all tokens) and handles 64 of its list at a time;
+// one that finds more than the list holds reads the ids of its share again instead.
+//
+// The workgroups behind those that sort fill the gradient with zeros meanwhile; the rows
+// of the words that occur are written by the next launch.
+
+constexpr int kIds = 16;   // ids that a lane holds at a time
+
+// Ids that are no words (< 0, or past 32 bits) as -1; those from V to 2^32 are no
+// workgroup's.
+__device__ __forceinline__ int word_of(int2 id) { return id.y != 0 ? -1 : id.x; }
+
+// One chunk to a thread, so that all that is written at a time lies together (131 k rows of
+// 8 KiB beside the sort: 165 us; 2 chunks 180, 4 chunks 184), and past the caches.
+template <typename T>
+__device__ __forceinline__ void fill_zero(const EmbedArgs& a, int64_t block) {
+  constexpr int E = Rows<T>::kE;
+  const int64_t at = (block * blockDim.x + threadIdx.x) * E, n = a.V * a.D;
+  T* out = static_cast<T*>(a.out);
+  const float zero[E] = {};
+  if (at + E <= n) Rows<T>::store_past(out + at, Rows<T>::pack(zero));
+  else store_chunk(out, at, n, zero);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedArgs a,
+                                                                    int sort_blocks) {
+  extern __shared__ int32_t lds[];   // next place [wave][word], then the waves' lists
+  __shared__ int32_t sums[kEmbedMaxWaves], belows[kEmbedMaxWaves];
+  if ((int)blockIdx.x >= sort_blocks) {
+    fill_zero<T>(a, (int)blockIdx.x - sort_blocks);
+    return;
+  }
   const int waves = blockDim.x / 64, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int64_t v0 = (int64_t)blockIdx.x * a.words;
-  const int nv = (int)(a.V - v0 < a.words ? a.V - v0 : a.words);
-  for (int i = threadIdx.x; i < waves * a.words; i += blockDim.x) next[i] = 0;
-  if (threadIdx.x == 0) below_all = 0;
-  __syncthreads();
-  const int64_t share = ((a.T + waves * 64 - 1) / (waves * 64)) * 64;
-  const int64_t t0 = wave * share, t1 = t0 + share < a.T ? t0 + share : a.T;
+  const int v0 = blockIdx.x * a.words;
+  const unsigned nv = (unsigned)(a.V - v0 < a.words ? a.V - v0 : a.words);
+  const int share = (int)((a.T + waves * 64 - 1) / (waves * 64)) * 64;
+  const int t0 = wave * share, t1 = t0 + share < (int)a.T ? t0 + share : (int)a.T;
+  int32_t* next = lds;
   volatile int32_t* mine = next + wave * a.words;   // (its lanes write for each other)
-  int below = 0;
-#pragma unroll 4
-  for (int64_t t = t0 + lane; t < t1; t += 64) {
-    const int64_t id = a.ids[t];
-    if (id >= 0 && id < v0) ++below;
-    if (id >= v0 && id < v0 + nv) atomicAdd(next + wave * a.words + (id - v0), 1);
-  }
-  if (below) atomicAdd(&below_all, below);
+  volatile uint32_t* list = reinterpret_cast<uint32_t*>(next + waves * a.words) + wave * a.list;
+  for (int i = lane; i < a.words; i += 64) mine[i] = 0;
+  const uint64_t lower = (1ull << lane) - 1;
+  const int2* ids = reinterpret_cast<const int2*>(a.ids);
+  // f(token, its word or -1) for 64 tokens of the share at a time
+  auto every = [&](auto f) {
+    for (int t = t0; t < t1; t += 64 * kIds) {
+      int2 id[kIds];
+#pragma unroll
+      for (int k = 0; k < kIds; ++k) {
+        const int at = t + 64 * k + lane;
+        id[k] = at < t1 ? ids[at] : make_int2(-1, -1);
+      }
+#pragma unroll
+      for (int k = 0; k < kIds; ++k) f(t + 64 * k + lane, word_of(id[k]));
+    }
+  };
+  // f(token, its word less v0 or -1) for 64 tokens that are this workgroup's, or fewer
+  int below = 0, found = 0;
+  auto own = [&](auto f) {
+    if (found <= a.list) {
+      for (int i = 0; i < found; i += 64) {
+        const uint32_t x = i + lane < found ? list[i + lane] : 0;
+        f(t0 + (int)(x & 0xFFFF), i + lane < found ? (int)(x >> 16) : -1);
+      }
+    } else {
+      every([&](int token, int word) {
+        const bool here = (unsigned)(word - v0) < nv;
+        if (__ballot(here)) f(token, here ? word - v0 : -1);
+      });
+    }
+  };
+  // How many of the lanes below this one have its word, and how many lanes in all.
+  auto alike = [&](int w, int& rank, int& count) {
+    uint64_t left = __ballot(w >= 0);
+    rank = count = 0;
+    while (left) {
+      const int x = __builtin_amdgcn_readlane(w, __builtin_ctzll(left));
+      const uint64_t same = __ballot(w == x);
+      if (w == x) rank = __popcll(same & lower), count = __popcll(same);
+      left &= ~same;
+    }
+  };
+  every([&](int token, int word) {
+    below += (unsigned)word < (unsigned)v0 ? 1 : 0;
+    const bool here = (unsigned)(word - v0) < nv;
+    const uint64_t at = __ballot(here);
+    if (at) {
+      const int place = found + __popcll(at & lower);
+      if (here && place < a.list) list[place] = (uint32_t)(word - v0) << 16 | (uint32_t)(token - t0);
+      found += __popcll(at);
+    }
+  });
+  own([&](int, int w) {
+    int rank, count;
+    alike(w, rank, count);
+    if (w >= 0 && rank == 0) mine[w] = mine[w] + count;
+  });
+  for (int d = 32; d > 0; d /= 2) below += __shfl_xor(below, d);
+  if (lane == 0) belows[wave] = below;
   __syncthreads();
   // where each word begins: thread j sums words j * per .. + per - 1
   const int per = (nv + blockDim.x - 1) / blockDim.x;
-  const int w0 = threadIdx.x * per, w1 = w0 + per < nv ? w0 + per : nv;
+  const int w0 = threadIdx.x * per, w1 = w0 + per < (int)nv ? w0 + per : (int)nv;
   int total = 0;
   for (int w = w0; w < w1; ++w)
     for (int k = 0; k < waves; ++k) total += next[k * a.words + w];
@@ -89,8 +162,12 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
   }
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
-  int at = below_all + upto - total;
-  for (int k = 0; k < wave; ++k) at += sums[k];
+  int at = upto - total, all = 0;
+  for (int k = 0; k < waves; ++k) {
+    if (k < wave) at += sums[k];
+    at += belows[k];
+    all += sums[k] + belows[k];
+  }
   for (int w = w0; w < w1; ++w) {
     a.start[v0 + w] = at;
     for (int k = 0; k < waves; ++k) {
@@ -99,171 +176,182 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
       at += c;
     }
   }
-  if (v0 + nv == a.V && threadIdx.x == 0) {
-    int n = below_all;
-    for (int k = 0; k < waves; ++k) n += sums[k];
-    a.start[a.V] = n;
-  }
+  if (v0 + (int64_t)nv == a.V && threadIdx.x == 0) a.start[a.V] = all;
   __syncthreads();
-  for (int64_t t = t0; t < t1; t += 64) {
-    const int64_t id = t + lane < t1 ? a.ids[t + lane] : -1;
-    const bool here = id >= v0 && id < v0 + nv;
-    uint64_t left = __ballot(here);
-    const int word = here ? (int)(id - v0) : -1;
-    while (left) {   // one word of these 64 tokens at a time
-      const int w = __builtin_amdgcn_readlane(word, __builtin_ctzll(left));
-      const uint64_t same = __ballot(word == w);
-      const int first = mine[w];
-      if (word == w)
-        a.order[first + __popcll(same & ((1ull << lane) - 1))] = (int32_t)(t + lane);
-      if (lane == 0) mine[w] = first + __popcll(same);
-      left &= ~same;
-    }
-  }
+  own([&](int token, int w) {
+    const int first = w >= 0 ? mine[w] : 0;
+    int rank, count;
+    alike(w, rank, count);
+    if (w >= 0) a.order[first + rank] = make_int2(token, v0 + w);
+    if (w >= 0 && rank == 0) mine[w] = first + count;
+  });
 }
 
 // scale * sum, beside what stands there, into the gradient's row (from column `at` on).
-template <typename T>
+template <typename T, bool kAdd>
 __device__ __forceinline__ void write_row(const EmbedArgs& a, int64_t word, int64_t at,
-                                          const float acc[Rows<T>::kE]) {
+                                          const float acc[Rows<T>::kE], u32x4 there) {
   constexpr int E = Rows<T>::kE;
-  T* row = static_cast<T*>(a.out) + word * a.D;
-  float f[E];
+  float f[E], old[E];
+  Rows<T>::floats(there, old);
 #pragma unroll
-  for (int e = 0; e < E; ++e) f[e] = acc[e] * a.scale;
-  if (a.add) {
-    float old[E];
-    Rows<T>::floats(load_chunk(row, at, a.D), old);
-#pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = old[e] + f[e];
-  }
-  store_chunk(row, at, a.D, f);
+  for (int e = 0; e < E; ++e) f[e] = kAdd ? old[e] + acc[e] * a.scale : acc[e] * a.scale;
+  store_chunk(static_cast<T*>(a.out) + word * a.D, at, a.D, f);
 }
 
-// Sums of the sorted tokens' rows (the first sum_blocks workgroups) and zeros for the
-// words without a token (the others).  A wave sums a tile of tokens, one chunk per lane:
+constexpr int kJoinWaves = 8;
+
+// Sums of the sorted tokens' rows.  A wave sums a tile of tokens, one chunk per lane:
 // words that lie in the tile are done, those that begin before it or go on beyond it
-// leave their part in the slab (rows 0 and 1 of the tile's).
-template <typename T>
-__global__ void __launch_bounds__(256) k_embed_sum(const EmbedArgs a, int pieces,
-                                                   int64_t sum_blocks) {
-  constexpr int E = Rows<T>::kE;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  if (blockIdx.x >= sum_blocks) {
-    const int64_t v = (blockIdx.x - sum_blocks) * 4 + wave;
-    if (v >= a.V || uniform(a.start + v) != uniform(a.start + v + 1)) return;
-    const float zero[E] = {};
-    T* row = static_cast<T*>(a.out) + v * a.D;
-    for (int64_t at = lane * E; at < a.D; at += 64 * E) store_chunk(row, at, a.D, zero);
-    return;
-  }
-  const int64_t w = (int64_t)blockIdx.x * 4 + wave;
-  const int64_t tile = w / pieces;
-  const int64_t at = ((w - tile * pieces) * 64 + lane) * E;
-  const int n = uniform(a.start + a.V);
-  const int64_t p0 = tile * a.tile;
-  if (p0 >= n) return;
-  const int count = (int)(n - p0 < a.tile ? n - p0 : a.tile);
-  // lane i: token i of the tile, and its word
-  const int token = lane < count ? a.order[p0 + lane] : 0;
-  const int word = (int)a.ids[token];
-  const T* in = static_cast<const T*>(a.in);
-  float acc[E] = {};
-  int now = __builtin_amdgcn_readlane(word, 0);
-  bool whole = uniform(a.start + now) >= p0;   // it begins in this tile
-  float* slab = a.slab + 2 * tile * a.D;
-  auto park = [&](int slot) {
-    if (at < a.D) {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (at + e < a.D) slab[slot * a.D + at + e] = acc[e];
-    }
-  };
-  constexpr int kAhead = 8;
-  for (int i0 = 0; i0 < count; i0 += kAhead) {
-    u32x4 x[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int t = __builtin_amdgcn_readlane(token, (i0 + i) & 63);
-      if (i0 + i < count) x[i] = load_chunk(in + t * a.ld, at, a.D);
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (i0 + i >= count) break;
-      const int next = __builtin_amdgcn_readlane(word, i0 + i);
-      if (next != now) {
-        if (whole) {
-          if (at < a.D) write_row<T>(a, now, at, acc);
-        } else {
-          park(0);
-        }
-        now = next, whole = true;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = 0.f;
-      }
-      float f[E];
-      Rows<T>::floats(x[i], f);
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = acc[e] + f[e];
-    }
-  }
-  if (uniform(a.start + now + 1) > p0 + count) park(whole ? 1 : 0);
-  else if (!whole) park(0);
-  else if (at < a.D) write_row<T>(a, now, at, acc);
-}
-
-// A word that begins in a tile and goes on beyond it: its parts in ascending order.
-template <typename T>
-__global__ void __launch_bounds__(256) k_embed_join(const EmbedArgs a, int pieces) {
-  constexpr int E = Rows<T>::kE;
+// leave their part in the slab (rows 0 and 1 of the tile's).  What it reads of dout, and
+// of the gradient where it adds to it, is asked for kAhead tokens at a time.
+template <typename T, bool kAdd>
+__global__ void __launch_bounds__(256) k_embed_sum(const EmbedArgs a, int pieces) {
+  constexpr int E = Rows<T>::kE, kAhead = 4;
   const int lane = threadIdx.x & 63;
   const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int64_t tile = w / pieces;
   const int64_t at = ((w - tile * pieces) * 64 + lane) * E;
+  const int64_t p0 = tile * a.tile, p1 = p0 + a.tile;
+  if (p0 >= a.T) return;
+  // the tile's tokens with their words, one to a lane, and the words beside it
+  const int2 mine = a.order[p0 + lane < a.T ? p0 + lane : a.T - 1];
+  const int before = p0 > 0 ? uniform(&a.order[p0 - 1].y) : -1;
+  const int behind = p1 < a.T ? uniform(&a.order[p1].y) : -1;
   const int n = uniform(a.start + a.V);
-  const int64_t p1 = (tile + 1) * a.tile;
-  if (p1 >= n) return;
-  const int word = (int)uniform(a.ids + uniform(a.order + p1 - 1));
-  const int end = uniform(a.start + word + 1);
-  if (end <= p1 || uniform(a.start + word) < p1 - a.tile) return;
-  if (at >= a.D) return;
-  const int64_t last = (end - 1) / a.tile;
-  float acc[E];
-  const float* part = a.slab + (2 * tile + 1) * a.D + at;
+  if (p0 >= n) return;
+  const int count = (int)(n < p1 ? n - p0 : a.tile);
+  const int after = p1 < n ? behind : -1;   // the word that follows the tile's last
+  const T* in = static_cast<const T*>(a.in);
+  const T* out = static_cast<const T*>(a.out);
+  float* slab = a.slab + 2 * tile * a.ld_slab + at;
+  float acc[E] = {};
+  bool whole = __builtin_amdgcn_readlane(mine.y, 0) != before;   // it begins in this tile
+  u32x4 x[kAhead], old[kAhead];
+  auto ask = [&](int i0) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = at + e < a.D ? part[e] : 0.f;
-  part += a.D;   // row 0 of the next tile
-#pragma unroll 4
-  for (int64_t t = tile + 1; t <= last; ++t, part += 2 * a.D) {
+    for (int i = 0; i < kAhead; ++i) {
+      if (i0 + i >= count) continue;
+      const int t = __builtin_amdgcn_readlane(mine.x, i0 + i);
+      x[i] = load_chunk(in + t * a.ld, at, a.D);
+      if constexpr (kAdd) {
+        const int64_t word = __builtin_amdgcn_readlane(mine.y, i0 + i);
+        const int next = i0 + i + 1 < count ? __builtin_amdgcn_readlane(mine.y, i0 + i + 1) : after;
+        if (word != next) old[i] = load_chunk(out + word * a.D, at, a.D);
+      }
+    }
+  };
+  ask(0);
+#pragma unroll 1
+  for (int i0 = 0; i0 < count; i0 += kAhead) {
+    u32x4 now[kAhead], there[kAhead];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = acc[e] + (at + e < a.D ? part[e] : 0.f);
+    for (int i = 0; i < kAhead; ++i) {
+      now[i] = x[i];
+      there[i] = kAdd ? old[i] : u32x4{0, 0, 0, 0};
+    }
+    ask(i0 + kAhead);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (i0 + i >= count) continue;
+      float f[E];
+      Rows<T>::floats(now[i], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = acc[e] + f[e];
+      const bool last = i0 + i + 1 == count;
+      const int word = __builtin_amdgcn_readlane(mine.y, i0 + i);
+      const int next = last ? after : __builtin_amdgcn_readlane(mine.y, i0 + i + 1);
+      if (word == next && !last) continue;
+      if (at < a.D) {
+        if (whole && word != next) {
+          write_row<T, kAdd>(a, word, at, acc, there[i]);
+        } else {
+          f32x4* p = reinterpret_cast<f32x4*>(slab + (whole ? a.ld_slab : 0));
+#pragma unroll
+          for (int e = 0; e < E; e += 4)
+            p[e / 4] = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+        }
+      }
+      whole = true;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    }
   }
-  write_row<T>(a, word, at, acc);
+}
+
+// A word that begins in a tile and goes on beyond it: every eighth of its parts in
+// ascending order by each wave, then the waves' sums.
+template <typename T, bool kAdd>
+__global__ void __launch_bounds__(64 * kJoinWaves) k_embed_join(const EmbedArgs a, int pieces) {
+  constexpr int E = Rows<T>::kE;
+  __shared__ float red[kJoinWaves][E][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t tile = blockIdx.x / pieces;
+  const int64_t at = ((blockIdx.x - tile * pieces) * 64 + lane) * E;
+  const int64_t p0 = tile * a.tile, p1 = p0 + a.tile;
+  if (p1 >= a.T) return;
+  const int word = uniform(&a.order[p1 - 1].y), behind = uniform(&a.order[p1].y);
+  const int before = p0 > 0 ? uniform(&a.order[p0 - 1].y) : -1;
+  const int n = uniform(a.start + a.V);
+  if (p1 >= n || behind != word || before == word) return;
+  const int end = uniform(a.start + word + 1);
+  u32x4 old{0, 0, 0, 0};
+  if (kAdd && wave == 0) old = load_chunk(static_cast<const T*>(a.out) + word * a.D, at, a.D);
+  const int parts = (int)((end - 1) / a.tile - tile) + 1;
+  // part 0: row 1 of this tile's; part i: row 0 of tile + i
+  const float* slab = a.slab + 2 * tile * a.ld_slab + at;
+  float acc[E] = {};
+  if (at < a.D) {
+#pragma unroll 8
+    for (int i = wave; i < parts; i += kJoinWaves) {
+      const f32x4* p = reinterpret_cast<const f32x4*>(slab + (i == 0 ? 1 : 2 * (int64_t)i) * a.ld_slab);
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const f32x4 x = p[e / 4];
+        acc[e] = acc[e] + x.x, acc[e + 1] = acc[e + 1] + x.y;
+        acc[e + 2] = acc[e + 2] + x.z, acc[e + 3] = acc[e + 3] + x.w;
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) red[wave][e][lane] = acc[e];
+  __syncthreads();
+  if (wave > 0 || at >= a.D) return;
+#pragma unroll
+  for (int k = 1; k < kJoinWaves; ++k)
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = acc[e] + red[k][e][lane];
+  write_row<T, kAdd>(a, word, at, acc, old);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <typename T>
-hipError_t embed(const EmbedArgs& a, hipStream_t st) {
-  const int pieces = (int)ceil_div(a.D, kPiece * 64 * Rows<T>::kE);
-  return launch(k_embed<T>, dim3((unsigned)ceil_div(a.T * pieces, 4)), 256, 0, st, a, pieces);
-}
+constexpr int64_t kL2Bytes = (int64_t)32 << 20;   // of the eight L2s
 
 template <typename T>
+hipError_t embed(const EmbedArgs& a, hipStream_t st) {
+  const int pieces = (int)ceil_div(a.D, 64 * Rows<T>::kE);
+  const bool past = a.T * a.D * (int64_t)sizeof(T) > kL2Bytes;
+  return launch(k_embed<T>, dim3((unsigned)ceil_div(a.T * pieces, 4)), 256, 0, st, a, pieces, past);
+}
+
+template <typename T, bool kAdd>
 hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
   const int pieces = (int)ceil_div(a.D, 64 * Rows<T>::kE);
   const int64_t tiles = ceil_div(a.T, a.tile);
-  const size_t lds = (size_t)a.sort_waves * a.words * sizeof(int32_t);
-  if (const hipError_t e = launch(k_embed_sort, dim3((unsigned)ceil_div(a.V, a.words)),
-                                  64 * a.sort_waves, lds, st, a))
+  const unsigned threads = 64 * a.sort_waves;
+  const size_t lds = (size_t)a.sort_waves * (a.words + a.list) * sizeof(int32_t);
+  const int64_t sorts = ceil_div(a.V, a.words);
+  const int64_t fills = kAdd ? 0 : ceil_div(a.V * a.D, (int64_t)threads * Rows<T>::kE);
+  if (const hipError_t e = launch(k_embed_sort<T>, dim3((unsigned)(sorts + fills)), threads, lds, st,
+                                  a, (int)sorts))
     return e;
-  const int64_t sums = ceil_div(tiles * pieces, 4), zeros = a.add ? 0 : ceil_div(a.V, 4);
-  if (sums + zeros == 0) return hipSuccess;
-  if (const hipError_t e =
-          launch(k_embed_sum<T>, dim3((unsigned)(sums + zeros)), 256, 0, st, a, pieces, sums))
-    return e;
-  return tiles > 1 ? launch(k_embed_join<T>, dim3((unsigned)sums), 256, 0, st, a, pieces)
+  if (tiles == 0) return hipSuccess;
+  const dim3 grid((unsigned)ceil_div(tiles * pieces, 4));
+  if (const hipError_t e = launch(k_embed_sum<T, kAdd>, grid, 256, 0, st, a, pieces)) return e;
+  return tiles > 1 ? launch(k_embed_join<T, kAdd>, dim3((unsigned)(tiles * pieces)),
+                            64 * kJoinWaves, 0, st, a, pieces)
                    : hipSuccess;
 }
 
@@ -274,7 +362,8 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st) {
-  return a.bf16 ? embed_grad<uint16_t>(a, st) : embed_grad<float>(a, st);
+  if (a.add) return a.bf16 ? embed_grad<uint16_t, true>(a, st) : embed_grad<float, true>(a, st);
+  return a.bf16 ? embed_grad<uint16_t, false>(a, st) : embed_grad<float, false>(a, st);
 }
 
 }  // namespace flr

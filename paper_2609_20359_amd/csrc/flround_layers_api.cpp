@@ -61,15 +61,17 @@ bool norm_ok(const fl_norm_shape* s) {
 }
 
 struct EmbedPlan {
-  int words, waves, tile;
+  int words, waves, list, tile;
   size_t start, order, slab, bytes;
 };
 
 EmbedPlan embed_plan(const fl_embed_shape& s) {
   EmbedPlan p{};
   p.words = (int)std::min<int64_t>(ceil_div(s.vocab, kCus), kEmbedMaxWords);
-  p.waves = (int)std::clamp<int64_t>(ceil_div(s.tokens, 256), 1, kEmbedMaxWaves);
-  p.tile = s.tokens <= 8192 ? 16 : 64;
+  p.waves = (int)std::clamp<int64_t>(ceil_div(s.tokens, 64), 1, kEmbedMaxWaves);
+  // (the list's entries hold a token's place in the wave's share in 16 bits)
+  p.list = (int)std::min<int64_t>(round_up(ceil_div(s.tokens, p.waves), 64), kEmbedMaxList);
+  p.tile = s.tokens <= 1024 ? 4 : s.tokens <= 8192 ? 16 : 64;
   const int64_t tiles = ceil_div(s.tokens, p.tile);
   size_t at = 0;
   auto take = [&at](int64_t bytes) {
@@ -78,8 +80,8 @@ EmbedPlan embed_plan(const fl_embed_shape& s) {
     return here;
   };
   p.start = take(4 * (s.vocab + 1));
-  p.order = take(4 * s.tokens);
-  p.slab = take(tiles > 1 ? 8 * tiles * s.width : 0);
+  p.order = take(8 * s.tokens);
+  p.slab = take(tiles > 1 ? 8 * tiles * round_up(s.width, 8) : 0);
   p.bytes = at + 256;   // for a workspace that does not start on 256 bytes
   return p;
 }
@@ -96,8 +98,7 @@ EmbedArgs embed_args(const fl_embed_shape& s, const int64_t* ids, const void* in
 
 // Workgroups of the norm's gradient, each of which leaves a part of the weight's.
 int64_t norm_parts(const fl_norm_shape& s) {
-  const NormShape n = norm_shape(s.rows, s.width, s.dtype == FL_BF16, true);
-  return std::min<int64_t>(ceil_div(s.rows, n.rows()), 2 * kCus);
+  return std::min<int64_t>(ceil_div(s.rows, norm_rows(s.width, s.dtype == FL_BF16)), kCus);
 }
 
 size_t norm_bytes(const fl_norm_shape& s) {
@@ -150,10 +151,11 @@ int fl_embed_grad(const fl_embed_shape* shape, const int64_t* ids, const void* d
   EmbedArgs a = embed_args(*shape, ids, dout, scale, dweight);
   char* ws = aligned(workspace);
   a.add = add != 0;
-  a.words = p.words, a.sort_waves = p.waves, a.tile = p.tile;
+  a.words = p.words, a.sort_waves = p.waves, a.list = p.list, a.tile = p.tile;
   a.start = reinterpret_cast<int32_t*>(ws + p.start);
-  a.order = reinterpret_cast<int32_t*>(ws + p.order);
+  a.order = reinterpret_cast<int2*>(ws + p.order);
   a.slab = reinterpret_cast<float*>(ws + p.slab);
+  a.ld_slab = round_up(shape->width, 8);
   return status_of(launch_embed_grad(a, static_cast<hipStream_t>(stream)));
 }
 

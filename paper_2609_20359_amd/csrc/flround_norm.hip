@@ -33,7 +33,7 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N], int wav
 
 // y = (x - mean) rstd w + b.  W waves to a row, K chunks to a lane.
 template <typename T, int W, int K, bool kRms>
-__global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a) {
+__global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a, bool past) {
   constexpr int E = Rows<T>::kE, kAt = W < 4 ? 4 / W : 1;
   __shared__ float red[2][W][1];
   const int lane = threadIdx.x & 63;
@@ -102,40 +102,57 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a)
       if (bs) y = y + h[e];
       f[e] = y;
     }
-    store_chunk(out, at + k * kNext, a.D, f);
+    if (past && at + k * kNext + E <= a.D) Rows<T>::store_past(out + at + k * kNext, Rows<T>::pack(f));
+    else store_chunk(out, at + k * kNext, a.D, f);
   }
 }
 
 // dx = rstd (c - mean(c) - xh mean(c xh)), c = dy w, xh = (x - mean) rstd (the second
 // term not for a root mean square), and the workgroup's sums of dy xh and of dy, which it
-// holds in registers over all of its rows.
-template <typename T, int W, int K, bool kRms>
-__global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm_grad(const NormArgs a) {
-  constexpr int E = Rows<T>::kE, kAt = W < 4 ? 4 / W : 1;
-  __shared__ float red[2][W][2];
+// holds in registers over all of its rows, R at a time.  kNext: the next rows are asked
+// for while these are summed.
+template <typename T, int W, int K, int R, bool kRms, bool kNext>
+__global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a, bool past) {
+  constexpr int E = Rows<T>::kE;
+  __shared__ float red[2][R][W][2];
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int64_t at = ((W == 1 ? 0 : wave * 64) + lane) * E;
-  constexpr int64_t kNext = W * 64 * E;
+  const int all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int wave = all_waves % W, group = all_waves / W;
+  const int64_t at = (wave * 64 + lane) * E;
+  constexpr int64_t kStep = W * 64 * E;
   const T* wt = static_cast<const T*>(a.weight);
   float dw[K][E] = {}, db[K][E] = {};
   u32x4 w[K] = {};
   if (wt) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) w[k] = load_chunk(wt, at + k * kNext, a.D);
+    for (int k = 0; k < K; ++k) w[k] = load_chunk(wt, at + k * kStep, a.D);
   }
   const float per = 1.0f / (float)a.D;
+  const int64_t step = (int64_t)gridDim.x * R;
+  const T* xs = static_cast<const T*>(a.x);
+  const T* ds = static_cast<const T*>(a.dy);
+  u32x4 xn[K], dn[K];
+  float mean_n, rstd_n;
+  // (rows behind the last are zeros, with statistics of zero: they add nothing)
+  auto ask = [&](int64_t row) {
+    const bool some = row < a.T;
+#pragma unroll
+    for (int k = 0; k < K; ++k) xn[k] = load_chunk(xs + row * a.ldx, at + k * kStep, some ? a.D : 0);
+#pragma unroll
+    for (int k = 0; k < K; ++k) dn[k] = load_chunk(ds + row * a.ldy, at + k * kStep, some ? a.D : 0);
+    mean_n = !kRms && some ? a.mean_in[row] : 0.f;
+    rstd_n = some ? a.rstd_in[row] : 0.f;
+  };
+  int64_t r = (int64_t)blockIdx.x * R + group;
+  if (kNext) ask(r);
   int turn = 0;
-  for (int64_t r = (int64_t)blockIdx.x * kAt + (W == 1 ? wave : 0); r < a.T;
-       r += (int64_t)gridDim.x * kAt, turn ^= 1) {
-    const T* xr = static_cast<const T*>(a.x) + r * a.ldx;
-    const T* dr = static_cast<const T*>(a.dy) + r * a.ldy;
+  for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.T; r0 += step, r += step, turn ^= 1) {
+    if (!kNext) ask(r);
     u32x4 x[K], d[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = load_chunk(xr, at + k * kNext, a.D);
-#pragma unroll
-    for (int k = 0; k < K; ++k) d[k] = load_chunk(dr, at + k * kNext, a.D);
-    const float mean = kRms ? 0.f : a.mean_in[r], rstd = a.rstd_in[r];
+    for (int k = 0; k < K; ++k) x[k] = xn[k], d[k] = dn[k];
+    const float mean = mean_n, rstd = rstd_n;
+    if (kNext && r0 + step < a.T) ask(r + step);
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -153,7 +170,8 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm_grad(const NormAr
         db[k][e] = db[k][e] + g[e];
       }
     }
-    row_sums<W>(s, red[turn], wave);
+    row_sums<W>(s, red[turn][group], wave);
+    if (r >= a.T) continue;
     const float m0 = s[0] * per, m1 = s[1] * per;
     T* out = static_cast<T*>(a.y) + r * a.D;
 #pragma unroll
@@ -169,34 +187,41 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm_grad(const NormAr
         if constexpr (!kRms) c = c - m1;
         f[e] = rstd * __builtin_fmaf(-xh, m0, c);
       }
-      store_chunk(out, at + k * kNext, a.D, f);
+      if (past && at + k * kStep + E <= a.D)
+        Rows<T>::store_past(out + at + k * kStep, Rows<T>::pack(f));
+      else store_chunk(out, at + k * kStep, a.D, f);
     }
   }
-  // the sums of the waves that hold the same columns, then the workgroup's row of parts
-  __shared__ float all[W == 1 ? 3 : 1][W == 1 ? 64 * K * E : 1];
+  // the sums of the waves that hold the same columns, halving the groups, then the
+  // workgroup's row of parts
+  constexpr int kHalf = R > 1 ? R / 2 : 1;
+  __shared__ float half[kHalf][R > 1 ? W * 64 * K * E : 1];
   auto leave = [&](float (&sum)[K][E], float* part) {
-    if constexpr (W == 1) {
+    const int mine = wave * 64 + lane;
+#pragma unroll
+    for (int n = R / 2; n > 0; n /= 2) {
       __syncthreads();
-      if (wave > 0) {
+      if (group >= n && group < 2 * n) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-          for (int e = 0; e < E; ++e) all[wave - 1][(k * E + e) * 64 + lane] = sum[k][e];
+          for (int e = 0; e < E; ++e) half[group - n][(k * E + e) * W * 64 + mine] = sum[k][e];
       }
       __syncthreads();
-      if (wave > 0) return;
+      if (group < n) {
 #pragma unroll
-      for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-#pragma unroll
-          for (int v = 0; v < 3; ++v) sum[k][e] = sum[k][e] + all[v][(k * E + e) * 64 + lane];
+          for (int e = 0; e < E; ++e)
+            sum[k][e] = sum[k][e] + half[group][(k * E + e) * W * 64 + mine];
+      }
     }
+    if (group > 0) return;
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (at + k * kNext + e < a.D) part[at + k * kNext + e] = sum[k][e];
+        if (at + k * kStep + e < a.D) part[at + k * kStep + e] = sum[k][e];
   };
   float* part = a.parts + blockIdx.x * a.D;
   if (a.dweight) leave(dw, part);
@@ -229,76 +254,69 @@ __global__ void __launch_bounds__(64 * kSumWaves) k_norm_sum(const NormArgs a) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// f.run<W, K>() for the shape.
-template <typename F>
-hipError_t with_shape(NormShape s, F f) {
-  if (s.waves == 1) {
-    if (s.chunks == 1) return f.template run<1, 1>();
-    if (s.chunks == 2) return f.template run<1, 2>();
-    return f.template run<1, 4>();
-  }
-  if (s.waves == 4) {
-    if (s.chunks == 1) return f.template run<4, 1>();
-    if (s.chunks == 2) return f.template run<4, 2>();
-    return f.template run<4, 4>();
-  }
-  if (s.chunks == 2) return f.template run<16, 2>();
-  if (s.chunks == 4) return f.template run<16, 4>();
-  return f.template run<16, 8>();
+constexpr int64_t kL2Bytes = (int64_t)32 << 20;   // of the eight L2s
+
+// Whether an output goes past the caches: one that they do not hold.
+bool past(const NormArgs& a) { return a.T * a.D * (a.bf16 ? 2 : 4) > kL2Bytes; }
+
+template <typename T, int W, int K, bool kRms>
+hipError_t forward(const NormArgs& a, hipStream_t st) {
+  const int rows = W < 4 ? 4 / W : 1;
+  return launch(k_norm<T, W, K, kRms>, dim3((unsigned)ceil_div(a.T, rows)), W < 4 ? 256 : 64 * W, 0,
+                st, a, past(a));
 }
 
 template <typename T, bool kRms>
-struct Forward {
-  const NormArgs& a;
-  hipStream_t st;
-  template <int W, int K>
-  hipError_t run() {
-    const int rows = W < 4 ? 4 / W : 1;
-    return launch(k_norm<T, W, K, kRms>, dim3((unsigned)ceil_div(a.T, rows)),
-                  W < 4 ? 256 : 64 * W, 0, st, a);
-  }
-};
+hipError_t forward(const NormArgs& a, hipStream_t st) {
+  const int64_t c = ceil_div(a.D, Rows<T>::kE);
+  if (c <= 64) return forward<T, 1, 1, kRms>(a, st);
+  if (c <= 128) return forward<T, 1, 2, kRms>(a, st);
+  if (c <= 256) return forward<T, 4, 1, kRms>(a, st);
+  if (c <= 512) return forward<T, 4, 2, kRms>(a, st);
+  if (c <= 1024) return forward<T, 8, 2, kRms>(a, st);
+  if (c <= 2048) return forward<T, 16, 2, kRms>(a, st);
+  if (c <= 4096) return forward<T, 16, 4, kRms>(a, st);
+  return forward<T, 16, 8, kRms>(a, st);
+}
+
+template <typename T, int W, int K, int R, bool kNext, bool kRms>
+hipError_t backward(const NormArgs& a, hipStream_t st) {
+  return launch(k_norm_grad<T, W, K, R, kRms, kNext>, dim3((unsigned)a.n_parts), 64 * W * R, 0, st,
+                a, past(a));
+}
 
 template <typename T, bool kRms>
-struct Backward {
-  const NormArgs& a;
-  hipStream_t st;
-  template <int W, int K>
-  hipError_t run() {
-    return launch(k_norm_grad<T, W, K, kRms>, dim3((unsigned)a.n_parts), W < 4 ? 256 : 64 * W, 0,
-                  st, a);
-  }
-};
-
-template <template <typename, bool> class Pass>
-hipError_t pass(const NormArgs& a, bool grad, hipStream_t st) {
-  const NormShape s = norm_shape(a.T, a.D, a.bf16, grad);
-  if (a.bf16)
-    return a.rms ? with_shape(s, Pass<uint16_t, true>{a, st})
-                 : with_shape(s, Pass<uint16_t, false>{a, st});
-  return a.rms ? with_shape(s, Pass<float, true>{a, st}) : with_shape(s, Pass<float, false>{a, st});
+hipError_t backward(const NormArgs& a, hipStream_t st) {
+  const int64_t c = ceil_div(a.D, Rows<T>::kE);
+  if (c <= 64) return backward<T, 1, 1, 16, true, kRms>(a, st);
+  if (c <= 128) return backward<T, 2, 1, 8, true, kRms>(a, st);
+  if (c <= 256) return backward<T, 4, 1, 4, true, kRms>(a, st);
+  if (c <= 512) return backward<T, 8, 1, 2, true, kRms>(a, st);
+  if (c <= 1024) return backward<T, 16, 1, 1, true, kRms>(a, st);
+  if (c <= 2048) return backward<T, 16, 2, 1, false, kRms>(a, st);
+  if (c <= 4096) return backward<T, 16, 4, 1, false, kRms>(a, st);
+  return backward<T, 16, 8, 1, false, kRms>(a, st);
 }
 
 }  // namespace
 
-NormShape norm_shape(int64_t rows, int64_t width, bool bf16, bool grad) {
-  (void)rows, (void)grad;
+int norm_rows(int64_t width, bool bf16) {
   const int64_t c = ceil_div(width, bf16 ? 8 : 4);
-  if (c <= 64) return {1, 1};
-  if (c <= 128) return {1, 2};
-  if (c <= 256) return {1, 4};
-  if (c <= 512) return {4, 2};
-  if (c <= 1024) return {4, 4};
-  if (c <= 2048) return {16, 2};
-  if (c <= 4096) return {16, 4};
-  return {16, 8};
+  return c <= 64 ? 16 : c <= 128 ? 8 : c <= 256 ? 4 : c <= 512 ? 2 : 1;
 }
 
-hipError_t launch_norm(const NormArgs& a, hipStream_t st) { return pass<Forward>(a, false, st); }
+hipError_t launch_norm(const NormArgs& a, hipStream_t st) {
+  if (a.bf16) return a.rms ? forward<uint16_t, true>(a, st) : forward<uint16_t, false>(a, st);
+  return a.rms ? forward<float, true>(a, st) : forward<float, false>(a, st);
+}
 
 hipError_t launch_norm_grad(const NormArgs& a, hipStream_t st) {
-  if (a.n_parts > 0)
-    if (const hipError_t e = pass<Backward>(a, true, st)) return e;
+  if (a.n_parts > 0) {
+    const hipError_t e =
+        a.bf16 ? (a.rms ? backward<uint16_t, true>(a, st) : backward<uint16_t, false>(a, st))
+               : (a.rms ? backward<float, true>(a, st) : backward<float, false>(a, st));
+    if (e != hipSuccess) return e;
+  }
   if (!a.dweight && !a.dbias) return hipSuccess;
   const dim3 grid((unsigned)ceil_div(a.D, 64), a.dweight && a.dbias ? 2 : 1);
   return a.bf16 ? launch(k_norm_sum<uint16_t>, grid, 64 * kSumWaves, 0, st, a)
