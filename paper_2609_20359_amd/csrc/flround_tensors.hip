@@ -2,7 +2,7 @@
 // or in 8 bits.
 //
 // A stream, bound by memory: a wave takes a unit of 512 elements of one tensor, 4 of
-// each half of it to a lane, all of its loads first.  The tensors' addresses are in the
+// each half of it to a lane, all of its loads first and past the caches.  The tensors' addresses are in the
 // launch's arguments; a wave finds its tensor by comparing its number with all of their
 // first units at once.
 //
@@ -31,14 +31,25 @@ constexpr int kLowExp = 12;             // so that a code's step is above fp32's
 typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
 typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
 
-// Random bits of element i: two rounds of shifts and products, with constants of a
-// published search for little bias.
-__device__ __forceinline__ uint32_t random_bits(const TensorsArgs& a, int64_t i) {
-  uint32_t x = (uint32_t)i ^ a.key_lo;
-  x = (x ^ (x >> 16)) * 0x7FEB352Du;
-  x ^= (uint32_t)(i >> 32) + a.key_hi;
-  x = (x ^ (x >> 15)) * 0x846CA68Bu;
-  return x ^ (x >> 16);
+constexpr uint32_t kInf = 0x7F800000u;
+
+// Random bits of elements i .. i + 3 (i a multiple of 4): two rounds of shifts and
+// products, with constants of a published search for little bias.  The four differ in two
+// bits until the first product, so one product gives the others' by additions.
+__device__ __forceinline__ void random_bits(const TensorsArgs& a, int64_t i, uint32_t x[4]) {
+  constexpr uint32_t kFirst = 0x7FEB352Du;
+  uint32_t y = (uint32_t)i ^ a.key_lo;
+  y ^= y >> 16;
+  const uint32_t one = y & 1 ? 0u - kFirst : kFirst, two = y & 2 ? 0u - 2 * kFirst : 2 * kFirst;
+  x[0] = y * kFirst;
+  x[1] = x[0] + one, x[2] = x[0] + two, x[3] = x[1] + two;
+  const uint32_t high = (uint32_t)(i >> 32) + a.key_hi;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    uint32_t z = x[e] ^ high;
+    z = (z ^ (z >> 15)) * 0x846CA68Bu;
+    x[e] = z ^ (z >> 16);
+  }
 }
 
 template <int kCtrl>
@@ -47,100 +58,164 @@ __device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
   return x > o ? x : o;
 }
 
-// The exponent byte of a block whose lanes hold four elements each.
-__device__ __forceinline__ uint32_t block_exp(const float* x) {
-  uint32_t most = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t b = __float_as_uint(x[e]) & 0x7FFFFFFFu;
-    if (b < 0x7F800000u && b > most) most = b;
-  }
-  most = max_dpp<0xB1>(most);    // lane ^ 1
-  most = max_dpp<0x4E>(most);    // lane ^ 2
-  most = max_dpp<0x141>(most);   // the other half of 8
-  most = max_dpp<0x140>(most);   // the other half of 16
-  // (a mantissa over 1.75 would be rounded to a code that stands for no number)
-  const uint32_t b = (most >> 23) + ((most & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+// The largest of a block's 16 lanes' values, in all of them.
+__device__ __forceinline__ uint32_t block_max(uint32_t most) {
+  most = max_dpp<0xB1>(most);      // lane ^ 1
+  most = max_dpp<0x4E>(most);      // lane ^ 2
+  most = max_dpp<0x141>(most);     // the other half of 8
+  return max_dpp<0x140>(most);     // the other half of 16
+}
+
+// The exponent byte of a block whose largest finite magnitude has this pattern.  (A
+// mantissa over 1.75 would be rounded to a code that stands for no number: (0x7FFFFF -
+// 0x600000) more carries into the exponent for these.)
+__device__ __forceinline__ uint32_t block_exp(uint32_t most) {
+  const uint32_t b = (most + 0x1FFFFFu) >> 23;
   return b < kLowExp ? kLowExp : b;
 }
 
-// The code of x in a block of exponent b; `bits`: 20 random ones.
-template <int kTop, bool kDrawn>
-__device__ __forceinline__ uint32_t code_of(float x, int b, uint32_t bits) {
-  const uint32_t w = __float_as_uint(x), abs = w & 0x7FFFFFFFu;
-  const uint32_t y = __float_as_uint(__builtin_amdgcn_ldexpf(__uint_as_float(abs), kTop - b));
-  uint32_t c = (y + (kDrawn ? bits : 0x7FFFFu + ((y >> 20) & 1))) >> 20;
-  if (kTop == kTopV && c == 0 && abs != 0) c = 1;
-  if (abs >= 0x7F800000u) c = 8 * kTop + 7;
-  return kTop == kTopM ? c | (w >> 31) << 7 : c;
+// What is added to a scaled value's pattern before its low 20 bits are dropped.
+template <bool kDrawn>
+__device__ __forceinline__ uint32_t rounded(uint32_t y, uint32_t bits) {
+  return y + (kDrawn ? bits : 0x7FFFFu + ((y >> 20) & 1));
 }
 
-template <int kTop>
-__device__ __forceinline__ float value_of(uint32_t c, int b) {
-  const uint32_t k = kTop == kTopM ? c & 127 : c;
-  uint32_t w = k == 8 * kTop + 7 ? 0x7FC00000u : k << 20;
-  if (kTop == kTopM) w |= (c & 128) << 24;
-  return __builtin_amdgcn_ldexpf(__uint_as_float(w), b - kTop);
-}
-
-// Four codes of each half, whose exponents the lanes of a block share.
-template <int kTop>
-__device__ __forceinline__ void load_codes(const uint8_t* codes, const uint8_t* exps, int64_t unit,
-                                           int lane, uint32_t w[2], uint32_t b[2]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    w[h] = *reinterpret_cast<const uint32_t*>(codes + unit * kUnit + h * kHalf + lane * 4);
-    b[h] = exps[unit * (kUnit / kStateBlock) + h * 4 + lane / 16];
-  }
-}
-
-template <int kTop>
-__device__ __forceinline__ void values(const uint32_t w[2], const uint32_t b[2], float x[8]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      x[4 * h + e] = value_of<kTop>((w[h] >> (8 * e)) & 255, (int)b[h]);
-}
-
+// The codes of 4 elements of each half, and their blocks' exponents; bits: 20 random ones
+// for each element.
 template <int kTop, bool kDrawn>
 __device__ __forceinline__ void store_codes(uint8_t* codes, uint8_t* exps, int64_t unit, int lane,
                                             const float x[8], const uint32_t bits[8]) {
+  uint32_t most[2], b[2], c[8];
+  float z[8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint32_t b = block_exp(x + 4 * h);
-    uint32_t w = 0;
+    most[h] = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      w |= code_of<kTop, kDrawn>(x[4 * h + e], (int)b, bits[4 * h + e]) << (8 * e);
-    *reinterpret_cast<uint32_t*>(codes + unit * kUnit + h * kHalf + lane * 4) = w;
-    if ((lane & 15) == 0) exps[unit * (kUnit / kStateBlock) + h * 4 + lane / 16] = (uint8_t)b;
+    for (int e = 0; e < 4; ++e) {
+      z[4 * h + e] = x[4 * h + e];
+      const uint32_t w = __float_as_uint(x[4 * h + e]) & (kTop == kTopM ? 0x7FFFFFFFu : 0xFFFFFFFFu);
+      if (w > most[h]) most[h] = w;
+    }
+  }
+  // (a second moment with a sign, -0 say, is more than any, too: it loses the sign)
+  const bool odd = most[0] >= kInf || most[1] >= kInf;
+  if (__builtin_expect(__any(odd), 0)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      most[h] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t w = __float_as_uint(x[4 * h + e]) & 0x7FFFFFFFu;
+        if (w < kInf && w > most[h]) most[h] = w;
+        if (kTop == kTopV) z[4 * h + e] = __builtin_fabsf(x[4 * h + e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    b[h] = block_exp(block_max(most[h]));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * h + e;
+      const uint32_t y =
+          __float_as_uint(__builtin_amdgcn_ldexpf(z[i], kTop - (int)b[h]));
+      c[i] = rounded<kDrawn>(y, bits[i]) >> 20;
+      if constexpr (kTop == kTopM) {
+        c[i] = (c[i] & 0x7F) | ((y >> 24) & 0x80);   // the sign is y's
+      } else {
+        const uint32_t w = __float_as_uint(z[i]), least = w < 1 ? w : 1;   // not 0 for v > 0
+        c[i] = c[i] > least ? c[i] : least;
+      }
+    }
+  }
+  if (__builtin_expect(__any(odd), 0)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = __float_as_uint(x[i]);
+      if ((w & 0x7FFFFFFFu) >= kInf) c[i] = (8 * kTop + 7) | (kTop == kTopM ? (w >> 24) & 0x80 : 0);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t* k = c + 4 * h;
+    const uint32_t w = (k[0] | k[1] << 8) | (k[2] << 16 | k[3] << 24);
+    __builtin_nontemporal_store(
+        w, reinterpret_cast<uint32_t*>(codes + unit * kUnit + h * kHalf + lane * 4));
+    if ((lane & 15) == 0) exps[unit * (kUnit / kStateBlock) + h * 4 + lane / 16] = (uint8_t)b[h];
   }
 }
 
-// Elements lane * 4 .. + 3 of each half of a unit of which n (from the unit's start) are
-// the tensor's; `rest` behind them.
-__device__ __forceinline__ void load_f32(const float* p, int64_t n, int lane, float x[8],
-                                         float rest = 0.f) {
+// Four codes of each half, whose exponents the lanes of a block share.
+struct Codes {
+  uint32_t w[2], b[2];
+};
+
+__device__ __forceinline__ Codes load_codes(const uint8_t* codes, const uint8_t* exps, int64_t unit,
+                                            int lane) {
+  Codes c;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int at = h * kHalf + lane * 4;
-    if (at + 4 <= n) {
-      const f32x4 w = *reinterpret_cast<const f32x4_at4*>(p + at);
-      x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
+    c.w[h] = __builtin_nontemporal_load(
+        reinterpret_cast<const uint32_t*>(codes + unit * kUnit + h * kHalf + lane * 4));
+    c.b[h] = exps[unit * (kUnit / kStateBlock) + h * 4 + lane / 16];
+  }
+  return c;
+}
+
+// A first moment's code is an fp8 value of 4 and 3 bits, which the chip converts; a second
+// moment's the top of an fp32 pattern.
+template <int kTop>
+__device__ __forceinline__ void values(const Codes& c, float x[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (kTop == kTopM) {
+      const float scale = __uint_as_float((c.b[h] - 8) << 23);   // 2^(b - 135)
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[h], false);
+      const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[h], true);
+      x[4 * h] = lo[0] * scale, x[4 * h + 1] = lo[1] * scale;
+      x[4 * h + 2] = hi[0] * scale, x[4 * h + 3] = hi[1] * scale;
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * h + e] = at + e < n ? p[at + e] : rest;
+      for (int e = 0; e < 4; ++e)
+        x[4 * h + e] = __builtin_amdgcn_ldexpf(
+            __uint_as_float(((c.w[h] >> (8 * e)) & 255) << 20), (int)c.b[h] - kTopV);
+    }
+  }
+  if constexpr (kTop == kTopV) {
+    // a byte of ones somewhere (or so it may seem)
+    auto ones = [](uint32_t w) { return (~w - 0x01010101u) & w & 0x80808080u; };
+    if (__builtin_expect(__any((ones(c.w[0]) | ones(c.w[1])) != 0), 0)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (((c.w[i / 4] >> (8 * (i % 4))) & 255) == 255) x[i] = __builtin_nanf("");
     }
   }
 }
 
-__device__ __forceinline__ void load_bf16(const uint16_t* p, int64_t n, int lane, float x[8]) {
+// Elements lane * 4 .. + 3 of each half of a unit of which n (from the unit's start) are
+// the tensor's, zeros behind them.  kFull: all of them are.
+template <bool kFull>
+__device__ __forceinline__ void load_f32(const float* p, int n, int lane, float x[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int at = h * kHalf + lane * 4;
-    if (at + 4 <= n) {
-      const u32x2 w = *reinterpret_cast<const u32x2_at2*>(p + at);
+    if (kFull || at + 4 <= n) {
+      const f32x4 w = __builtin_nontemporal_load(reinterpret_cast<const f32x4_at4*>(p + at));
+      x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * h + e] = at + e < n ? p[at + e] : 0.f;
+    }
+  }
+}
+
+template <bool kFull>
+__device__ __forceinline__ void load_bf16(const uint16_t* p, int n, int lane, float x[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int at = h * kHalf + lane * 4;
+    if (kFull || at + 4 <= n) {
+      const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_at2*>(p + at));
       x[4 * h] = bf16_lo(w.x), x[4 * h + 1] = bf16_hi(w.x);
       x[4 * h + 2] = bf16_lo(w.y), x[4 * h + 3] = bf16_hi(w.y);
     } else {
@@ -151,13 +226,15 @@ __device__ __forceinline__ void load_bf16(const uint16_t* p, int64_t n, int lane
   }
 }
 
-__device__ __forceinline__ void store_f32(float* p, int64_t n, int lane, const float x[8]) {
+template <bool kFull, bool kPast = true>
+__device__ __forceinline__ void store_f32(float* p, int n, int lane, const float x[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int at = h * kHalf + lane * 4;
-    if (at + 4 <= n) {
-      *reinterpret_cast<f32x4_at4*>(p + at) =
-          f32x4{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+    if (kFull || at + 4 <= n) {
+      const f32x4 w{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+      if constexpr (kPast) __builtin_nontemporal_store(w, reinterpret_cast<f32x4_at4*>(p + at));
+      else *reinterpret_cast<f32x4_at4*>(p + at) = w;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -166,13 +243,14 @@ __device__ __forceinline__ void store_f32(float* p, int64_t n, int lane, const f
   }
 }
 
-__device__ __forceinline__ void store_bf16(uint16_t* p, int64_t n, int lane, const float x[8]) {
+template <bool kFull>
+__device__ __forceinline__ void store_bf16(uint16_t* p, int n, int lane, const float x[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int at = h * kHalf + lane * 4;
-    if (at + 4 <= n) {
-      *reinterpret_cast<u32x2_at2*>(p + at) =
-          u32x2{pack_bf16x2(x[4 * h], x[4 * h + 1]), pack_bf16x2(x[4 * h + 2], x[4 * h + 3])};
+    if (kFull || at + 4 <= n) {
+      const u32x2 w{pack_bf16x2(x[4 * h], x[4 * h + 1]), pack_bf16x2(x[4 * h + 2], x[4 * h + 3])};
+      __builtin_nontemporal_store(w, reinterpret_cast<u32x2_at2*>(p + at));
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -181,38 +259,45 @@ __device__ __forceinline__ void store_bf16(uint16_t* p, int64_t n, int lane, con
   }
 }
 
-template <bool kGradF32, int kBits, bool kDrawn>
-__global__ void __launch_bounds__(256) k_tensors(const TensorsArgs a, int64_t units) {
-  const int lane = threadIdx.x & 63;
-  const int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  if (u >= units) return;
-  // tensors that begin behind the first one, up to this unit
-  static_assert(kMaxTensors > 64 && kMaxTensors <= 128);
-  const int more = lane < kMaxTensors - 64 ? a.first[lane + 65] : INT32_MAX;
-  const int k = __popcll(__ballot(a.first[lane + 1] <= u)) + __popcll(__ballot(more <= u));
-  const int64_t from = (u - a.first[k]) * kUnit;
-  const int64_t n = a.numel[k] - from;
-  const int64_t unit = a.unit0 + u;
+// One unit: elements `from` on of tensor k, n of them the tensor's.
+template <bool kGradF32, int kBits, bool kDrawn, bool kFull>
+__device__ __forceinline__ void step_unit(const TensorsArgs& a, int k, int64_t from, int n,
+                                          int64_t unit, int lane) {
   float* master = a.master[k] + from;
   float p[8], g[8], m[8], v[8];
-  load_f32(master, n, lane, p);
-  if constexpr (kGradF32)
-    load_f32(static_cast<const float*>(a.grad[k]) + from, n, lane, g);
-  else
-    load_bf16(static_cast<const uint16_t*>(a.grad[k]) + from, n, lane, g);
   float* mf = static_cast<float*>(a.state.m) + unit * kUnit;
   float* vf = static_cast<float*>(a.state.v) + unit * kUnit;
   uint8_t* mc = static_cast<uint8_t*>(a.state.m);
   uint8_t* vc = static_cast<uint8_t*>(a.state.v);
-  uint32_t wm[2], bm[2], wv[2], bv[2];
+  Codes cm, cv;
+  load_f32<kFull>(master, n, lane, p);
+  if constexpr (kGradF32)
+    load_f32<kFull>(static_cast<const float*>(a.grad[k]) + from, n, lane, g);
+  else
+    load_bf16<kFull>(static_cast<const uint16_t*>(a.grad[k]) + from, n, lane, g);
   if constexpr (kBits == 32) {
-    load_f32(mf, kUnit, lane, m);
-    load_f32(vf, kUnit, lane, v);
+    load_f32<true>(mf, kUnit, lane, m);
+    load_f32<true>(vf, kUnit, lane, v);
   } else {
-    load_codes<kTopM>(mc, a.state.m_exp, unit, lane, wm, bm);
-    load_codes<kTopV>(vc, a.state.v_exp, unit, lane, wv, bv);
-    values<kTopM>(wm, bm, m);
-    values<kTopV>(wv, bv, v);
+    cm = load_codes(mc, a.state.m_exp, unit, lane);
+    cv = load_codes(vc, a.state.v_exp, unit, lane);
+  }
+  __builtin_amdgcn_sched_barrier(0);   // all of them before the arithmetic
+  uint32_t rm[8], rv[8];
+  if constexpr (kDrawn) {   // while the loads are under way
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      random_bits(a, unit * kUnit + h * kHalf + lane * 4, rm + 4 * h);
+#pragma unroll
+      for (int e = 4 * h; e < 4 * h + 4; ++e) {
+        rv[e] = (rm[e] * 0x9E3779B1u) >> 12;
+        rm[e] = rm[e] >> 12;
+      }
+    }
+  }
+  if constexpr (kBits == 8) {
+    values<kTopM>(cm, m);
+    values<kTopV>(cv, v);
   }
   const float decay = (a.decay[k / 32] >> (k % 32)) & 1 ? a.s.decay : 1.0f;
 #pragma unroll
@@ -221,31 +306,57 @@ __global__ void __launch_bounds__(256) k_tensors(const TensorsArgs a, int64_t un
     g[e] = g[e] * a.grad_scale;
   }
   adam8(a.s, g, p, m, v);
-  store_f32(master, n, lane, p);
-  if (a.working[k]) store_bf16(a.working[k] + from, n, lane, p);
+  store_f32<kFull>(master, n, lane, p);
+  if (a.working[k]) store_bf16<kFull>(a.working[k] + from, n, lane, p);
   if constexpr (kBits == 32) {
-    store_f32(mf, kUnit, lane, m);
-    store_f32(vf, kUnit, lane, v);
+    store_f32<true>(mf, kUnit, lane, m);
+    store_f32<true>(vf, kUnit, lane, v);
   } else {
-    uint32_t rm[8], rv[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (kDrawn) {
-        const uint32_t x = random_bits(a, unit * kUnit + (e / 4) * kHalf + lane * 4 + e % 4);
-        rm[e] = x >> 12;
-        rv[e] = (x * 0x9E3779B1u) >> 12;
-      }
-    }
     store_codes<kTopM, kDrawn>(mc, a.state.m_exp, unit, lane, m, rm);
     store_codes<kTopV, kDrawn>(vc, a.state.v_exp, unit, lane, v, rv);
   }
 }
 
-template <bool kTo8>
-__global__ void __launch_bounds__(256) k_state_convert(const StateDev narrow, const StateDev wide,
-                                                       int64_t units) {
+// Workgroups of one wave, twelve of which a CU holds at once (by the LDS that they ask for
+// and do not use), or of four with seven.  More waves than it takes to keep the memory
+// busy only spread what they read and write: 92 M elements with states in 32 bits take 422
+// us with 12 waves, 438 with 20, 445 with all 32; the states in 8 bits take more
+// arithmetic (about 580 instructions a unit beside 300), and with it 28 waves: 218 M
+// elements 568 us, with 16 797.
+template <int kBits>
+constexpr int kThreads = kBits == 8 ? 256 : 64;
+template <int kBits>
+constexpr unsigned kLds = kBits == 8 ? 23200 : 13632;
+
+template <bool kGradF32, int kBits, bool kDrawn>
+__global__ void __launch_bounds__(kThreads<kBits>) k_tensors(const TensorsArgs a, int64_t units) {
   const int lane = threadIdx.x & 63;
-  const int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t u = (int64_t)blockIdx.x * (kThreads<kBits> / 64) +
+                    __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  if (u >= units) return;
+  // tensors that begin behind the first one, up to this unit
+  static_assert(kMaxTensors > 64 && kMaxTensors <= 128);
+  const int more = lane < kMaxTensors - 64 ? a.first[lane + 65] : INT32_MAX;
+  const int k = __popcll(__ballot(a.first[lane + 1] <= u)) + __popcll(__ballot(more <= u));
+  const int64_t from = (u - a.first[k]) * kUnit;
+  const int64_t n = a.numel[k] - from;
+  if (__builtin_expect(n >= kUnit, 1))
+    step_unit<kGradF32, kBits, kDrawn, true>(a, k, from, kUnit, a.unit0 + u, lane);
+  else
+    step_unit<kGradF32, kBits, kDrawn, false>(a, k, from, (int)n, a.unit0 + u, lane);
+}
+
+// Two waves to a workgroup, eight of which a CU holds at once (218 M elements: 355 us;
+// with all that fit 398).
+constexpr int kConvertThreads = 128;
+constexpr unsigned kConvertLds = 20480;
+
+template <bool kTo8>
+__global__ void __launch_bounds__(kConvertThreads)
+    k_state_convert(const StateDev narrow, const StateDev wide, int64_t units) {
+  const int lane = threadIdx.x & 63;
+  const int64_t u = (int64_t)blockIdx.x * (kConvertThreads / 64) +
+                    __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   if (u >= units) return;
   float* mf = static_cast<float*>(wide.m) + u * kUnit;
   float* vf = static_cast<float*>(wide.v) + u * kUnit;
@@ -253,19 +364,18 @@ __global__ void __launch_bounds__(256) k_state_convert(const StateDev narrow, co
   uint8_t* vc = static_cast<uint8_t*>(narrow.v);
   float m[8], v[8];
   if constexpr (kTo8) {
-    load_f32(mf, kUnit, lane, m);
-    load_f32(vf, kUnit, lane, v);
+    load_f32<true>(mf, kUnit, lane, m);
+    load_f32<true>(vf, kUnit, lane, v);
     const uint32_t none[8] = {};
     store_codes<kTopM, false>(mc, narrow.m_exp, u, lane, m, none);
     store_codes<kTopV, false>(vc, narrow.v_exp, u, lane, v, none);
   } else {
-    uint32_t wm[2], bm[2], wv[2], bv[2];
-    load_codes<kTopM>(mc, narrow.m_exp, u, lane, wm, bm);
-    load_codes<kTopV>(vc, narrow.v_exp, u, lane, wv, bv);
-    values<kTopM>(wm, bm, m);
-    values<kTopV>(wv, bv, v);
-    store_f32(mf, kUnit, lane, m);
-    store_f32(vf, kUnit, lane, v);
+    const Codes cm = load_codes(mc, narrow.m_exp, u, lane);
+    const Codes cv = load_codes(vc, narrow.v_exp, u, lane);
+    values<kTopM>(cm, m);
+    values<kTopV>(cv, v);
+    store_f32<true, false>(mf, kUnit, lane, m);
+    store_f32<true, false>(vf, kUnit, lane, v);
   }
 }
 
@@ -278,14 +388,17 @@ hipError_t launch_tensors(const TensorsArgs& a, int64_t units, hipStream_t st) {
                            : (a.state.bits == 32 ? k_tensors<false, 32, false>
                               : a.drawn          ? k_tensors<false, 8, true>
                                                  : k_tensors<false, 8, false>);
-  return launch(kernel, dim3((unsigned)((units + 3) / 4)), 256, 0, st, a, units);
+  const int threads = a.state.bits == 8 ? kThreads<8> : kThreads<32>, waves = threads / 64;
+  return launch(kernel, dim3((unsigned)((units + waves - 1) / waves)), threads,
+                a.state.bits == 8 ? kLds<8> : kLds<32>, st, a, units);
 }
 
 hipError_t launch_state_convert(const StateDev& from, const StateDev& to, int64_t units,
                                 hipStream_t st) {
-  const dim3 grid((unsigned)((units + 3) / 4));
-  return to.bits == 8 ? launch(k_state_convert<true>, grid, 256, 0, st, to, from, units)
-                      : launch(k_state_convert<false>, grid, 256, 0, st, from, to, units);
+  const dim3 grid((unsigned)((units + kConvertThreads / 64 - 1) / (kConvertThreads / 64)));
+  return to.bits == 8 ? launch(k_state_convert<true>, grid, kConvertThreads, kConvertLds, st, to, from, units)
+                      : launch(k_state_convert<false>, grid, kConvertThreads, kConvertLds, st, from, to,
+                               units);
 }
 
 }  // namespace flr

@@ -177,7 +177,9 @@ def specials():
     sub = np.concatenate([np.array([448.0] + [(k + 0.5) * 2.0 ** -9 for k in range(63)])]).astype(f)
     none = np.zeros(64, f)
     only = np.full(64, np.inf, f)
-    x = np.concatenate([tiny, huge, one, near, mixed, odd, rand, ties, sub, none, only, -one, -mixed])
+    zeros = one * np.float32(1e-3)
+    zeros[::3] = -0.0
+    x = np.concatenate([zeros, tiny, huge, one, near, mixed, odd, rand, ties, sub, none, only, -one, -mixed])
     return np.pad(x, (0, -len(x) % 512))
 
 
@@ -185,12 +187,14 @@ def test_convert_special_values(env):
     torch, P = env["torch"], env["P"]
     x = specials()
     n = len(x)
-    wide = torch.from_numpy(np.concatenate([x, np.abs(x)])).cuda()
+    v = np.abs(x)
+    v[0] = -0.0                                # (held as 0)
+    wide = torch.from_numpy(np.concatenate([x, v])).cuda()
     narrow = torch.full((2 * n + n // 32,), 99, dtype=torch.uint8, device="cuda")
     P.fl_state_convert(wide, narrow)
     mc, vc, me, ve = S8.split(narrow.cpu().numpy(), n)
     for got, want in ((mc, S8.encode(x, 15)[0]), (me, S8.encode(x, 15)[1]),
-                      (vc, S8.encode(np.abs(x), 31)[0]), (ve, S8.encode(np.abs(x), 31)[1])):
+                      (vc, S8.encode(v, 31)[0]), (ve, S8.encode(v, 31)[1])):
         assert np.array_equal(got, want)
     back = torch.empty_like(wide)
     P.fl_state_convert(narrow, back)
