@@ -9,6 +9,7 @@ there is no fallback.
 """
 import ctypes
 import functools
+import operator
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -901,6 +902,9 @@ def fl_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight, dbias, rms=False,
 # ---- AdamW over many tensors --------------------------------------------------
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 def _whole(t, dtype, what):
     """Checks a contiguous CUDA tensor of this dtype."""
     if not getattr(t, "is_cuda", False):
@@ -974,6 +978,40 @@ def _state(t, n, dev, what):
     return _array(t, (size,), t.dtype, dev, what), bits
 
 
+def _grad_ptrs(grads, sizes, dev):
+    """Addresses of the gradients (None for one that is left out), checked, and their
+    dtype."""
+    torch = _T
+    T = torch.Tensor
+    dtype = None
+    try:   # all at once: a list of some hundred costs 0.2 us each
+        if list(map(T.numel, grads)) == sizes:
+            dtypes, devs = set(map(_dtype_of, grads)), set(map(T.get_device, grads))
+            if len(dtypes) == 1 and devs == {dev} and all(map(T.is_contiguous, grads)):
+                dtype = dtypes.pop()
+                if dtype is torch.bfloat16 or dtype is torch.float32:
+                    return list(map(T.data_ptr, grads)), dtype
+    except (TypeError, AttributeError):
+        pass
+    # one is left out, or something is wrong: one by one
+    ptrs, dtype = [], None
+    for i, g in enumerate(grads):
+        if g is None:
+            ptrs.append(None)
+            continue
+        what = "grads[%d]" % i
+        if dtype is None:
+            dtype = getattr(g, "dtype", None)
+            if dtype is not torch.bfloat16 and dtype is not torch.float32:
+                raise ValueError("%s must be a bf16 or float32 tensor" % what)
+        _whole(g, dtype, what)
+        _on_device(g, dev, what)
+        if g.numel() != sizes[i]:
+            raise ValueError("%s has %d elements; expected %d" % (what, g.numel(), sizes[i]))
+        ptrs.append(g.data_ptr())
+    return ptrs, dtype
+
+
 def fl_adamw_tensors(tensors, hp, step, grads, state, grad_scale=1.0, seed=0, stream=None):
     """One AdamW step of all `tensors` (a Tensors): grads holds a contiguous bf16 or
     float32 gradient (all of one dtype) for each, or None for one that is left alone;
@@ -988,23 +1026,7 @@ def fl_adamw_tensors(tensors, hp, step, grads, state, grad_scale=1.0, seed=0, st
     grads = list(grads)
     if len(grads) != count:
         raise ValueError("grads has %d entries; expected %d" % (len(grads), count))
-    ptrs, dtype = [], None
-    for i, g in enumerate(grads):
-        if g is None:
-            ptrs.append(None)
-            continue
-        if dtype is None:
-            dtype = g.dtype
-            if dtype is not torch.bfloat16 and dtype is not torch.float32:
-                raise ValueError("grads[%d] must be a bf16 or float32 tensor" % i)
-        if (g.dtype is dtype and g.numel() == sizes[i] and g.get_device() == dev
-                and g.is_contiguous()):
-            ptrs.append(g.data_ptr())
-            continue
-        # something is wrong with it: say what
-        _whole(g, dtype, "grads[%d]" % i)
-        _on_device(g, dev, "grads[%d]" % i)
-        raise ValueError("grads[%d] has %d elements; expected %d" % (i, g.numel(), sizes[i]))
+    ptrs, dtype = _grad_ptrs(grads, sizes, dev)
     if count == 0:
         return
     h = hparams(hp)
