@@ -648,7 +648,7 @@ int fl_layer_norm_grad(const fl_norm_shape* shape, const void* x, const void* we
  *      8 bits: S codes of m, S of v, S / 64 exponent bytes of m, S / 64 of v.
  *   A block of 64 elements shares an exponent byte b: the exponent field of its largest
  *   finite magnitude as a float, one more where that one's mantissa is over 1.75, 12 at
- *   least.  A code of m is a sign, 4 bits of exponent E and 3 of mantissa M, of v 5 and 3;
+ *   least (a lower byte, as before the first step, stands for 12).  A code of m is a sign, 4 bits of exponent E and 3 of mantissa M, of v 5 and 3;
  *   with T = 15 or 31 it stands for 2^(b - 127 + E - T) (1 + M / 8), or, where E = 0, for
  *   2^(b - 126 - T) M / 8; E = T with M = 7 stands for NaN, and an infinite moment is held
  *   as NaN.  A moment in 32 bits (as AdamW defines it; the update itself takes it so)

@@ -157,7 +157,8 @@ __device__ __forceinline__ Codes load_codes(const uint8_t* codes, const uint8_t*
   for (int h = 0; h < 2; ++h) {
     c.w[h] = __builtin_nontemporal_load(
         reinterpret_cast<const uint32_t*>(codes + unit * kUnit + h * kHalf + lane * 4));
-    c.b[h] = exps[unit * (kUnit / kStateBlock) + h * 4 + lane / 16];
+    const uint32_t b = exps[unit * (kUnit / kStateBlock) + h * 4 + lane / 16];
+    c.b[h] = b < kLowExp ? kLowExp : b;   // (0 before the first step)
   }
   return c;
 }

@@ -1029,6 +1029,8 @@ def fl_adamw_tensors(tensors, hp, step, grads, state, grad_scale=1.0, seed=0, st
     ptrs, dtype = _grad_ptrs(grads, sizes, dev)
     if count == 0:
         return
+    if not 0 <= seed < 1 << 64:
+        raise ValueError("seed must be between 0 and 2^64 - 1")
     h = hparams(hp)
     p, bits = _state(state, tensors.n_state, dev, "state")
     rc = lib().fl_adamw_tensors(count, tensors.array, (ctypes.c_void_p * count)(*ptrs),

@@ -102,10 +102,14 @@ def check_grad(env, ids, d, V, scale, add=False, off=3, **kw):
         empty[at] = False
         dw[empty] = math.nan                 # left as they are
         old = torch.where(empty[:, None], 0.0, dw.double())
-    total = torch.zeros(V, D, device="cuda", dtype=torch.float64).index_add_(0, at, x)
-    size = torch.zeros(V, D, device="cuda", dtype=torch.float64).index_add_(0, at, x.abs())
-    n = torch.zeros(V, device="cuda", dtype=torch.float64).index_add_(
-        0, at, torch.ones_like(at, dtype=torch.float64))[:, None]
+    # (summed on the CPU: many additions to one row at once take a GPU minutes)
+    at_c, x_c = at.cpu(), x.cpu()
+
+    def by_word(rows):
+        return torch.zeros(V, rows.shape[1], dtype=torch.float64).index_add_(0, at_c, rows).cuda()
+
+    total, size = by_word(x_c), by_word(x_c.abs())
+    n = by_word(torch.ones(len(at_c), 1, dtype=torch.float64))
     P.fl_embed_grad(ids, d, dw, scale=scale, add=add, **kw)
     want = old + scale * total
     off64 = abs(scale) * (n * U * size + U * total.abs()) * (1 + 1e-6) + U * want.abs()
@@ -135,6 +139,32 @@ def test_runs_of_one_word(env, T, kind):
     """A word of many tokens ends inside a wave's tokens, at their end, or beyond."""
     ids, _, d = make(env["torch"], T, 600, 96, "bf16", kind)
     check_grad(env, ids, d, 600, 0.25)
+
+
+@pytest.mark.parametrize("T,V,kind", [(20000, 150001, "all"), (20000, 1 << 18, "mixed"),
+                                      (1 << 20, 3000, "mixed"), (1 << 20, 700, "same")])
+def test_many_tokens_and_words(env, T, V, kind):
+    """Workgroups of as many words as they take, and words of more tokens than a wave of
+    the sort lists."""
+    ids, _, d = make(env["torch"], T, V, 8, "fp32", kind)
+    check_grad(env, ids, d, V, 1.0)
+
+
+def test_ids_past_32_bits(env):
+    """Ids from V on are no words, whatever their low bits."""
+    torch, P = env["torch"], env["P"]
+    ids = torch.tensor([3, (1 << 32) + 3, -(1 << 32) + 3, 1 << 31, (1 << 32) - 1, 20, 19, 3,
+                        (1 << 63) - 1, -(1 << 63)], device="cuda")
+    d = torch.ones(10, 8, device="cuda")
+    dw = torch.empty(20, 8, device="cuda")
+    P.fl_embed_grad(ids, d, dw)
+    want = torch.zeros(20, 8, device="cuda")
+    want[3], want[19] = 2.0, 1.0
+    assert torch.equal(dw, want)
+    out = torch.empty(10, 8, device="cuda")
+    P.fl_embed(ids, want, out)
+    nan = [False, True, False, True, True, True, False, False, True, False]
+    assert out.isnan().all(1).tolist() == nan and not bool(out[[2, 9]].any())
 
 
 @pytest.mark.parametrize("first", [1, 14, 15, 16, 17, 31, 32, 33, 63, 64, 65])

@@ -229,6 +229,30 @@ def test_every_code_and_exponent(env):
         assert np.array_equal(x, y)
 
 
+def test_a_state_of_zeros_is_positive_zeros(env):
+    """Before the first step: no sign in either moment, and exponent bytes below 12, which
+    stand for 12."""
+    torch, P = env["torch"], env["P"]
+    n = 1024
+    narrow = torch.zeros(2 * n + n // 32, dtype=torch.uint8, device="cuda")
+    wide = torch.full((2 * n,), -7.0, device="cuda")
+    P.fl_state_convert(narrow, wide)
+    assert not bool(wide.view(torch.int32).any())
+    codes = np.tile(np.arange(256, dtype=np.uint8), 4)
+    exps = np.arange(16, dtype=np.uint8)
+    narrow = torch.from_numpy(np.concatenate([codes, codes, exps, exps])).cuda()
+    P.fl_state_convert(narrow, wide)
+    got = wide.cpu().numpy()
+    low = np.maximum(exps, 12)
+    assert np.array_equal(got[:n], S8.decode(codes, low, 15), equal_nan=True)
+    assert np.array_equal(got[n:], S8.decode(codes, low, 31), equal_nan=True)
+    master = torch.ones(600, device="cuda")
+    t = P.Tensors([master])
+    state = t.state(8)
+    P.fl_adamw_tensors(t, HP, 1, [torch.full((600,), -0.0, device="cuda")], state)
+    assert not bool(state[:2 * n].any())       # 0 * beta1 + -0 is 0
+
+
 def test_draws_are_even_and_the_held_value_is_right_on_average(env):
     """n equal moments between two codes, a quarter of the way up.  What is held is one of
     the two, up in a share of 1/4 that n independent draws miss by 6 sqrt(3/16/n) once in
@@ -412,6 +436,9 @@ def test_refusals(env):
         a = dict(dict(hp=HP, step=1, grads=good, state=state), **kw)
         with pytest.raises(P.FlError):
             P.fl_adamw_tensors(ts, a.pop("hp"), a.pop("step"), a.pop("grads"), a.pop("state"), **a)
+    for seed in (-1, 1 << 64):
+        with pytest.raises(ValueError):
+            P.fl_adamw_tensors(ts, HP, 1, good, state, seed=seed)
     wide = torch.zeros(2 * ts.n_state, device="cuda")
     for src, dst in ((state, state.clone()), (wide, wide.clone()), (state, wide[2:]),
                      (state[1:], wide), (state, wide.half())):
