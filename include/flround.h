@@ -569,7 +569,7 @@ int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const 
  *
  * fl_embed_grad -- gradient of sum_td dout[t][d] * out[t][d]:
  *     dweight[v][d] = scale * sum over t with ids[t] == v of dout[t][d]
- *   summed in ascending order of t (in parts of 16 or 64 tokens of the sorted ones).
+ *   summed in an order that the ids alone fix.
  *   add == 0: all V x D of it are written; else the sum is added to what stands in
  *   the rows of the words that occur, rounded once, and the other rows are left alone
  *   (tied weights, several batches).  A negative id, or one >= V, takes no part: its

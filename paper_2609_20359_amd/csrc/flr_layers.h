@@ -28,6 +28,10 @@ struct EmbedArgs {
   int64_t ld_slab;
 };
 
+// Tokens up to which the gradient is one launch, whose workgroups all read all ids (1000
+// tokens into 5000 x 1024: 12.5 us, 14.1 by the sort, but 22 and 18.6 where nine of ten are
+// one word).
+constexpr int kEmbedFew = 512;
 constexpr int kEmbedMaxWords = 512;
 constexpr int kEmbedMaxWaves = 16;
 constexpr int kEmbedMaxList = 1024;

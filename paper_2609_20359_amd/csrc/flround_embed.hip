@@ -325,6 +325,109 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embed_join(const EmbedArgs 
   write_row<T, kAdd>(a, word, at, acc, old);
 }
 
+// Few tokens need no sort: one launch does all of it.  A workgroup for a token and 64
+// chunks of its row looks for the tokens of the same word by reading all ids; that of the
+// word's first token sums their rows, every eighth of them in ascending order in each
+// wave, then the waves' sums.  The workgroups behind these write zeros to the rows of
+// some words each, but for those that occur.
+// (333 tokens into 5003 x 321 fp32: 7.9 us, 14.4 by the sort and its two launches.)
+constexpr int kFewIds = kEmbedFew / 64;   // ids that a lane holds
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
+constexpr int kFewRows = 4;               // rows that a wave has asked for at a time
+constexpr int kFewFill = 1024;            // words of a workgroup of zeros, at most
+
+template <typename T, bool kAdd>
+__global__ void __launch_bounds__(kFewThreads) k_embed_few(const EmbedArgs a, int pieces, int sum_blocks,
+                                                   int fill_words) {
+  constexpr int E = Rows<T>::kE;
+  __shared__ float red[kFewWaves][E][64];
+  __shared__ bool used[kFewFill];
+  __shared__ int tokens_of[kEmbedFew];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int tokens = (int)a.T;
+  if ((int)blockIdx.x >= sum_blocks) {
+    const int64_t v0 = (int64_t)((int)blockIdx.x - sum_blocks) * fill_words;
+    const int n = (int)(a.V - v0 < fill_words ? a.V - v0 : fill_words);
+    for (int i = threadIdx.x; i < n; i += kFewThreads) used[i] = false;
+    __syncthreads();
+    for (int t = threadIdx.x; t < tokens; t += kFewThreads) {
+      const int64_t id = a.ids[t];
+      if (id >= v0 && id < v0 + n) used[id - v0] = true;
+    }
+    __syncthreads();
+    const float zero[E] = {};
+    const unsigned chunks = (unsigned)((a.D + E - 1) / E);
+    for (unsigned c = threadIdx.x; c < n * chunks; c += kFewThreads) {
+      const unsigned row = c / chunks;
+      if (used[row]) continue;
+      T* to = static_cast<T*>(a.out) + (v0 + row) * a.D;
+      const int64_t k = (int64_t)(c - row * chunks) * E;
+      if (k + E <= a.D) Rows<T>::store_past(to + k, Rows<T>::pack(zero));
+      else store_chunk(to, k, a.D, zero);
+    }
+    return;
+  }
+  const int t = blockIdx.x / pieces;
+  const int64_t at = ((blockIdx.x - t * pieces) * 64 + lane) * E;
+  int64_t id[kFewIds];
+#pragma unroll
+  for (int k = 0; k < kFewIds; ++k) id[k] = 64 * k + lane < tokens ? a.ids[64 * k + lane] : -1;
+  const int64_t word = uniform(a.ids + t);
+  if (word < 0 || word >= a.V) return;
+  uint64_t same[kFewIds];
+  int count = 0, first = -1;
+#pragma unroll
+  for (int k = 0; k < kFewIds; ++k) {
+    same[k] = __ballot(id[k] == word);
+    if (first < 0 && same[k]) first = 64 * k + __builtin_ctzll(same[k]);
+    count += __popcll(same[k]);
+  }
+  if (first != t || (count == 1 && wave > 0)) return;
+  const T* in = static_cast<const T*>(a.in);
+  u32x4 old{0, 0, 0, 0};
+  if (kAdd && wave == 0) old = load_chunk(static_cast<const T*>(a.out) + word * a.D, at, a.D);
+  if (count > 1) {   // the word's tokens in ascending order: 64 ids to a wave at a time
+    int before = 0;
+#pragma unroll
+    for (int k = 0; k < kFewIds; ++k) {
+      if (k % kFewWaves == wave && id[k] == word)
+        tokens_of[before + __popcll(same[k] & ((1ull << lane) - 1))] = 64 * k + lane;
+      before += __popcll(same[k]);
+    }
+    __syncthreads();
+  }
+  float acc[E] = {};
+  for (int i0 = wave; i0 < count; i0 += kFewWaves * kFewRows) {
+    u32x4 x[kFewRows];
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i) {
+      const int rank = i0 + i * kFewWaves;
+      x[i] = u32x4{0, 0, 0, 0};
+      if (rank < count)
+        x[i] = load_chunk(in + (count > 1 ? tokens_of[rank] : t) * a.ld, at, a.D);
+    }
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i) {
+      float f[E];
+      Rows<T>::floats(x[i], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = acc[e] + f[e];
+    }
+  }
+  if (count > 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) red[wave][e][lane] = acc[e];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int k = 1; k < kFewWaves; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = acc[e] + red[k][e][lane];
+  }
+  if (at < a.D) write_row<T, kAdd>(a, word, at, acc, old);
+}
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int64_t kL2Bytes = (int64_t)32 << 20;   // of the eight L2s
@@ -339,6 +442,15 @@ hipError_t embed(const EmbedArgs& a, hipStream_t st) {
 template <typename T, bool kAdd>
 hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
   const int pieces = (int)ceil_div(a.D, 64 * Rows<T>::kE);
+  if (a.T <= kEmbedFew) {
+    // zeros of 16 KiB to a workgroup
+    const int64_t row = a.D * (int64_t)sizeof(T);
+    const int words = (int)(row < 16 ? kFewFill : row < 16384 ? 16384 / row : 1);
+    const int64_t sums = a.T * pieces, fills = kAdd ? 0 : ceil_div(a.V, words);
+    return sums + fills ? launch(k_embed_few<T, kAdd>, dim3((unsigned)(sums + fills)),
+                                 kFewThreads, 0, st, a, pieces, (int)sums, words)
+                        : hipSuccess;
+  }
   const int64_t tiles = ceil_div(a.T, a.tile);
   const unsigned threads = 64 * a.sort_waves;
   const size_t lds = (size_t)a.sort_waves * (a.words + a.list) * sizeof(int32_t);

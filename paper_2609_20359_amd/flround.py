@@ -299,6 +299,13 @@ def _stream(stream):
     return ctypes.c_void_p(_raw_stream())
 
 
+def _stream_number(stream):
+    """As _stream, as a number (a call of a few us takes it faster)."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream()
+    return _stream(stream)
+
+
 def hparams(hp):
     if isinstance(hp, AdamwHparams):
         return hp
@@ -781,13 +788,21 @@ def fl_top_logits(logits, k, tau, values, ids, lse=None, workspace=None, stream=
 # ---- the embedding and the layer norm ----------------------------------------
 
 
-def _row_dtypes():
-    torch = _T or _torch()
-    return torch.bfloat16, torch.float32
-
-
-def _fl_dtype(t):
+def _dtype_number(t):
+    """FL_BF16 or FL_F32 of a tensor that _rows has seen."""
     return FL_BF16 if t.dtype is _T.bfloat16 else FL_F32
+
+
+def _row_tensor(t, what):
+    """(device, address, elements between rows) of a bf16 or float32 tensor of rows on the
+    current device."""
+    torch = _T or _torch()
+    dev = _device_of(t, what)
+    return (dev, *_rows(t, (torch.bfloat16, torch.float32), dev, what))
+
+
+def _maybe(t, shape, dtype, dev, what):
+    return None if t is None else _array(t, shape, dtype, dev, what)
 
 
 @functools.lru_cache(maxsize=256)
@@ -813,65 +828,51 @@ def layer_norm_workspace_bytes(rows, width, dtype=FL_BF16):
     return int(_norm_shape(rows, width, 0, 0, dtype, 0)[1])
 
 
-def _count(ids):
-    """The number of ids, a 1-D tensor."""
-    if ids.dim() != 1:
-        raise ValueError("ids must be a 1-D tensor")
-    return ids.shape[0]
-
-
 def fl_embed(ids, weight, out, scale=1.0, stream=None):
     """out[t] = scale * weight[ids[t]]: ids (T int64, negative: the row is 0), weight
     (V x D bf16 or float32, rows may be longer), out (T x D of its dtype)."""
-    dtypes = _row_dtypes()
-    dev = _device_of(weight, "weight")
-    w, ldw = _rows(weight, dtypes, dev, "weight")
+    dev, w, ldw = _row_tensor(weight, "weight")
     V, D = weight.shape
-    T = _count(ids)
-    shape, _ = _embed_shape(T, V, D, ldw, _fl_dtype(weight))
-    rc = lib().fl_embed(shape, _array(ids, (T,), _T.int64, dev, "ids"), w, float(scale),
-                        _array(out, (T, D), weight.dtype, dev, "out"), _stream(stream))
-    _check(rc, "fl_embed")
+    T = ids.numel()
+    shape, _ = _embed_shape(T, V, D, ldw, _dtype_number(weight))
+    rc = lib().fl_embed(shape, _array(ids, (T,), _T.int64, dev, "ids"), w, scale,
+                        _array(out, (T, D), weight.dtype, dev, "out"), _stream_number(stream))
+    if rc:
+        _check(rc, "fl_embed")
 
 
 def fl_embed_grad(ids, dout, dweight, scale=1.0, add=False, workspace=None, stream=None):
     """Gradient of sum(dout * out) by the weight: writes dweight (V x D, of dout's
     dtype), or with add adds to the rows of the words that occur.  dout: T x D, rows
     may be longer."""
-    dtypes = _row_dtypes()
-    dev = _device_of(dout, "dout")
-    d, ldd = _rows(dout, dtypes, dev, "dout")
-    T = _count(ids)
-    if dout.shape[0] != T:
-        raise ValueError("dout has %d rows, ids %d" % (dout.shape[0], T))
+    dev, d, ldd = _row_tensor(dout, "dout")
+    T, D = dout.shape
     if dweight.dim() != 2:
         raise ValueError("dweight must be a 2-D tensor")
-    V, D = dweight.shape[0], dout.shape[1]
-    shape, need = _embed_shape(T, V, D, ldd, _fl_dtype(dout))
+    V = dweight.shape[0]
+    shape, need = _embed_shape(T, V, D, ldd, _dtype_number(dout))
     keep, nbytes = _workspace(workspace, need, dev, stream)
-    rc = lib().fl_embed_grad(shape, _array(ids, (T,), _T.int64, dev, "ids"), d, float(scale),
+    rc = lib().fl_embed_grad(shape, _array(ids, (T,), _T.int64, dev, "ids"), d, scale,
                              1 if add else 0, _array(dweight, (V, D), dout.dtype, dev, "dweight"),
-                             keep.data_ptr(), nbytes, _stream(stream))
-    _check(rc, "fl_embed_grad")
+                             keep.data_ptr(), nbytes, _stream_number(stream))
+    if rc:
+        _check(rc, "fl_embed_grad")
 
 
 def fl_layer_norm(x, weight, bias, eps, y, mean, rstd, rms=False, stream=None):
     """Layer norm of the rows of x (R x D bf16 or float32, rows may be longer) into y;
     weight and bias (D, or None) and y have x's dtype.  Writes mean (or None) and rstd
     (R float32), which the gradient takes.  rms: root mean square norm, without a mean."""
-    dtypes = _row_dtypes()
-    dev = _device_of(x, "x")
-    p, ldx = _rows(x, dtypes, dev, "x")
+    dev, p, ldx = _row_tensor(x, "x")
     R, D = x.shape
-    dt, f32 = x.dtype, dtypes[1]
-    shape, _ = _norm_shape(R, D, ldx, 0, _fl_dtype(x), 1 if rms else 0)
-    rc = lib().fl_layer_norm(shape, p,
-                             None if weight is None else _array(weight, (D,), dt, dev, "weight"),
-                             None if bias is None else _array(bias, (D,), dt, dev, "bias"),
-                             float(eps), _array(y, (R, D), dt, dev, "y"),
-                             None if mean is None else _array(mean, (R,), f32, dev, "mean"),
-                             _array(rstd, (R,), f32, dev, "rstd"), _stream(stream))
-    _check(rc, "fl_layer_norm")
+    dt, f32 = x.dtype, _T.float32
+    shape, _ = _norm_shape(R, D, ldx, 0, _dtype_number(x), 1 if rms else 0)
+    rc = lib().fl_layer_norm(shape, p, _maybe(weight, (D,), dt, dev, "weight"),
+                             _maybe(bias, (D,), dt, dev, "bias"), eps,
+                             _array(y, (R, D), dt, dev, "y"), _maybe(mean, (R,), f32, dev, "mean"),
+                             _array(rstd, (R,), f32, dev, "rstd"), _stream_number(stream))
+    if rc:
+        _check(rc, "fl_layer_norm")
 
 
 def fl_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight, dbias, rms=False, workspace=None,
@@ -879,24 +880,21 @@ def fl_layer_norm_grad(x, weight, mean, rstd, dy, dx, dweight, dbias, rms=False,
     """Gradient of sum(dy * y) of fl_layer_norm: writes dx (R x D), dweight and dbias (D
     each, or None), all of x's dtype.  mean (None with rms) and rstd as fl_layer_norm
     wrote them; rows of x and dy may be longer."""
-    dtypes = _row_dtypes()
-    dev = _device_of(x, "x")
-    p, ldx = _rows(x, dtypes, dev, "x")
+    dev, p, ldx = _row_tensor(x, "x")
     R, D = x.shape
-    dt, f32 = x.dtype, dtypes[1]
+    dt, f32 = x.dtype, _T.float32
     g, ldy = _rows(dy, (dt,), dev, "dy")
     if dy.shape != x.shape:
         raise ValueError("dy has shape %s, x %s" % (tuple(dy.shape), tuple(x.shape)))
-    shape, need = _norm_shape(R, D, ldx, ldy, _fl_dtype(x), 1 if rms else 0)
+    shape, need = _norm_shape(R, D, ldx, ldy, _dtype_number(x), 1 if rms else 0)
     keep, nbytes = _workspace(workspace, need, dev, stream)
     rc = lib().fl_layer_norm_grad(
-        shape, p, None if weight is None else _array(weight, (D,), dt, dev, "weight"),
-        None if mean is None else _array(mean, (R,), f32, dev, "mean"),
+        shape, p, _maybe(weight, (D,), dt, dev, "weight"), _maybe(mean, (R,), f32, dev, "mean"),
         _array(rstd, (R,), f32, dev, "rstd"), g, _array(dx, (R, D), dt, dev, "dx"),
-        None if dweight is None else _array(dweight, (D,), dt, dev, "dweight"),
-        None if dbias is None else _array(dbias, (D,), dt, dev, "dbias"), keep.data_ptr(), nbytes,
-        _stream(stream))
-    _check(rc, "fl_layer_norm_grad")
+        _maybe(dweight, (D,), dt, dev, "dweight"), _maybe(dbias, (D,), dt, dev, "dbias"),
+        keep.data_ptr(), nbytes, _stream_number(stream))
+    if rc:
+        _check(rc, "fl_layer_norm_grad")
 
 
 # ---- AdamW over many tensors --------------------------------------------------

@@ -134,7 +134,7 @@ def test_embed_grad(env, T, V, D, dtype, add):
 
 
 @pytest.mark.parametrize("kind", ["same", "none", "all"])
-@pytest.mark.parametrize("T", [15, 16, 17, 48, 257, 8192, 8193, 8256, 30000])
+@pytest.mark.parametrize("T", [15, 16, 17, 48, 257, 511, 512, 513, 1024, 1025, 8192, 8193, 8256, 30000])
 def test_runs_of_one_word(env, T, kind):
     """A word of many tokens ends inside a wave's tokens, at their end, or beyond."""
     ids, _, d = make(env["torch"], T, 600, 96, "bf16", kind)
