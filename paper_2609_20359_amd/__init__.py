@@ -6,7 +6,8 @@ gradient reduce-scatter, the AdamW step on the fp32 master shard, and the
 FedAvg of the federation groups' replicas, as a C-ABI library (libflround.so,
 include/flround.h) of hand-written gfx950 kernels; and the output head, where a
 step's gradients begin: cross entropy, distillation from top logits, and their
-gradients.  The Python face below is a thin ctypes binding with the same names.
+gradients; the embedding and the layer norm with theirs; and AdamW over many
+tensors, with moments in 32 or in 8 bits.  The Python face below is a thin ctypes binding with the same names.
 """
 from .flround import (FL_BF16, FL_F32, FL_MAX_GROUPS, FL_MAX_PEERS, FL_MAX_TARGETS,
                       FL_NOALLOC_SCRATCH_BYTES, HIP_EVENT_DISABLE_SYSTEM_FENCE, FlError,
