@@ -580,7 +580,7 @@ int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const 
  * fl_layer_norm -- with E(.) the mean over a row's D elements:
  *     mean[r] = E(x[r]);  rstd[r] = 1 / sqrt(E((x[r] - mean[r])^2) + eps)
  *     y[r][d] = (x[r][d] - mean[r]) * rstd[r] * weight[d] + bias[d]
- *   rms nonzero: the mean is taken as 0 (root mean square norm).  weight, bias: D
+ *   rms nonzero: the mean is taken as 0 (root mean square norm), and written as 0.  weight, bias: D
  *   values of dtype, or NULL (1 and 0).  x: R rows (x_stride); y: R x D; mean, rstd: R
  *   floats (mean may be NULL), which the gradient needs.  eps finite, >= 0.
  *
@@ -684,7 +684,7 @@ int fl_state_convert(int64_t state_numel, int from_bits, const void* from, void*
 /* ------------------------------------------------------------------------
  * Launch-shape control, for tuning sweeps and for tests that check that
  * results do not depend on the launch shape.  blocks_per_cu > 0 caps the
- * grid of every streaming kernel at blocks_per_cu * (number of CUs)
+ * grid of every streaming kernel of a layout's calls at blocks_per_cu * (number of CUs)
  * workgroups of 256 threads (four times as many of one wave); 0 restores the
  * defaults (a wave for every 512 elements, started in order, with a limit per
  * pass on how many a CU holds at once).  Process-wide; returns the previous

@@ -11,6 +11,12 @@ namespace {
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
 
+// A value that a whole wave reads at one address and no kernel writes meanwhile.
+template <typename T>
+__device__ __forceinline__ T uniform(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
 template <typename T>
 struct Rows;
 

@@ -11,12 +11,6 @@
 namespace flr {
 namespace {
 
-// A value that a whole wave reads at one address.
-template <typename T>
-__device__ __forceinline__ T uniform(const T* p) {
-  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
-}
-
 // out[t] = scale * weight[ids[t]], one chunk to a lane, so that all that is read and
 // written at a time lies together.  Outputs larger than the L2s go past them (16384 rows
 // of 8 KiB, half of them of words that occur twice and more: 31.6 us, 46 through the

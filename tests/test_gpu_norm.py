@@ -118,7 +118,7 @@ WIDTHS = [1, 2, 7, 8, 9, 63, 64, 255, 321, 512, 513, 1024, 1601, 2048, 2049, 409
 @pytest.mark.parametrize("rms", [False, True])
 @pytest.mark.parametrize("D", WIDTHS)
 def test_widths(env, D, rms, dtype):  # noqa: F811
-    for R, pad, off in ((1, 0, 0), (5, 3, 1), (130, 8, 0)):
+    for R, pad, off in ((1, 0, 0), (5, 3, 1), (130, 8, 0), (530, 0, 2)):
         c = Case(env["torch"], R, D, dtype, rms, pad=pad, off=off)
         c.check_forward(env["P"])
         c.check_backward(env["P"])
@@ -126,7 +126,8 @@ def test_widths(env, D, rms, dtype):  # noqa: F811
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("R,D", [(2, 100), (700, 64), (1029, 768), (3000, 1000), (5000, 24),
-                                 (2050, 2560)])
+                                 (2050, 2560), (512, 500), (513, 500), (512, 4096),
+                                 (1500, 40), (1300, 9000), (1100, 1), (16, 63), (17, 65)])
 def test_rows(env, R, D, dtype):  # noqa: F811
     c = Case(env["torch"], R, D, dtype)
     c.check_forward(env["P"])
