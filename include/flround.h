@@ -580,9 +580,9 @@ int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const 
  * fl_layer_norm -- with E(.) the mean over a row's D elements:
  *     mean[r] = E(x[r]);  rstd[r] = 1 / sqrt(E((x[r] - mean[r])^2) + eps)
  *     y[r][d] = (x[r][d] - mean[r]) * rstd[r] * weight[d] + bias[d]
- *   rms nonzero: the mean is taken as 0 (root mean square norm), and written as 0.  weight, bias: D
- *   values of dtype, or NULL (1 and 0).  x: R rows (x_stride); y: R x D; mean, rstd: R
- *   floats (mean may be NULL), which the gradient needs.  eps finite, >= 0.
+ *   rms nonzero: the mean is taken as 0 (root mean square norm), and written as 0.
+ *   weight, bias: D values of dtype, or NULL (1 and 0).  x: R rows (x_stride); y: R x D;
+ *   mean, rstd: R floats (mean may be NULL), which the gradient needs.  eps finite, >= 0.
  *
  * fl_layer_norm_grad -- gradient of sum_rd dy[r][d] * y[r][d], at mean and rstd as
  *   fl_layer_norm wrote them; with xh = (x[r] - mean[r]) * rstd[r], c = dy[r] * weight:

@@ -34,6 +34,8 @@ struct EmbedArgs {
 constexpr int kEmbedFew = 512;
 constexpr int kEmbedMaxWords = 512;
 constexpr int kEmbedMaxWaves = 16;
+// Found tokens that a wave of the sort lists: half of its share of 32768 tokens (30 % of
+// them one word: 92 us for the gradient, 110 with a list of 512, which is read again).
 constexpr int kEmbedMaxList = 1024;
 
 // The layer norm and its gradient.

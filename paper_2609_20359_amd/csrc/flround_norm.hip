@@ -31,7 +31,9 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N], int wav
   }
 }
 
-// y = (x - mean) rstd w + b.  W waves to a row, K chunks to a lane.
+// y = (x - mean) rstd w + b.  W waves to a row, K chunks to a lane; outputs larger than the
+// L2s go past them.  (16384 x 4096 bf16, four waves of two chunks: 45 us, 5.9 TB/s; 46
+// through the caches, 45.4 with eight waves of a chunk.)
 template <typename T, int W, int K, bool kRms>
 __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a, bool past) {
   constexpr int E = Rows<T>::kE, kAt = W < 4 ? 4 / W : 1;
@@ -110,7 +112,9 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a,
 // dx = rstd (c - mean(c) - xh mean(c xh)), c = dy w, xh = (x - mean) rstd (the second
 // term not for a root mean square), and the workgroup's sums of dy xh and of dy, which it
 // holds in registers over all of its rows, R at a time.  kNext: the next rows are asked
-// for while these are summed.
+// for while these are summed.  (16384 x 4096 bf16, two rows of eight waves: 70.6 us, 5.7
+// TB/s, and 4.6 for the parts; four waves of two chunks 76.7 in all, without the next rows
+// 78.6.)
 template <typename T, int W, int K, int R, bool kRms, bool kNext>
 __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a, bool past) {
   constexpr int E = Rows<T>::kE;
