@@ -2,9 +2,9 @@
 // or in 8 bits.
 //
 // A stream, bound by memory: a wave takes a unit of 512 elements of one tensor, 4 of
-// each half of it to a lane, all of its loads first and past the caches.  The tensors' addresses are in the
-// launch's arguments; a wave finds its tensor by comparing its number with all of their
-// first units at once.
+// each half of it to a lane, all of its loads first and past the caches.  The tensors'
+// addresses are in the launch's arguments; a wave finds its tensor by comparing its
+// number with all of their first units at once.
 //
 // States in 8 bits.  A block of 64 elements (16 lanes) shares an exponent byte b, that of
 // its largest magnitude.  A code is the top of the element's fp32 pattern after scaling
@@ -397,7 +397,8 @@ hipError_t launch_tensors(const TensorsArgs& a, int64_t units, hipStream_t st) {
 hipError_t launch_state_convert(const StateDev& from, const StateDev& to, int64_t units,
                                 hipStream_t st) {
   const dim3 grid((unsigned)((units + kConvertThreads / 64 - 1) / (kConvertThreads / 64)));
-  return to.bits == 8 ? launch(k_state_convert<true>, grid, kConvertThreads, kConvertLds, st, to, from, units)
+  return to.bits == 8 ? launch(k_state_convert<true>, grid, kConvertThreads, kConvertLds, st, to,
+                               from, units)
                       : launch(k_state_convert<false>, grid, kConvertThreads, kConvertLds, st, from, to,
                                units);
 }
