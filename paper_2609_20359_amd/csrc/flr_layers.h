@@ -8,6 +8,10 @@
 
 namespace flr {
 
+// Whether an array is more than the eight L2s hold: what is read or written of it once goes
+// past them.
+inline bool past_l2(int64_t bytes) { return bytes > (int64_t)32 << 20; }
+
 // The embedding and its gradient.
 struct EmbedArgs {
   int64_t T, V, D, ld;     // ld: elements between rows of the input

@@ -23,6 +23,9 @@ struct Rows;
 template <>
 struct Rows<uint16_t> {
   static constexpr int kE = 8;   // elements of a chunk
+  static __device__ __forceinline__ u32x4 load_past(const uint16_t* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_at2*>(p));
+  }
   static __device__ __forceinline__ u32x4 load(const uint16_t* p) {
     return *reinterpret_cast<const u32x4_at2*>(p);
   }
@@ -55,6 +58,9 @@ struct Rows<uint16_t> {
 template <>
 struct Rows<float> {
   static constexpr int kE = 4;
+  static __device__ __forceinline__ u32x4 load_past(const float* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_at4*>(p));
+  }
   static __device__ __forceinline__ u32x4 load(const float* p) {
     return *reinterpret_cast<const u32x4_at4*>(p);
   }
@@ -84,17 +90,20 @@ struct Rows<float> {
 };
 
 // Elements [at, at + kE) of a row of n elements; zeros from n on (none where at >= n).
-template <typename T>
+// kPast: what is read once, and more of it than the caches hold.  (A template's argument,
+// as the compiler makes one plain access of two that a condition chooses between.)
+template <bool kPast = false, typename T>
 __device__ __forceinline__ u32x4 load_chunk(const T* row, int64_t at, int64_t n) {
-  if (at + Rows<T>::kE <= n) return Rows<T>::load(row + at);
+  if (at + Rows<T>::kE <= n) return kPast ? Rows<T>::load_past(row + at) : Rows<T>::load(row + at);
   if (at < n) return Rows<T>::load_part(row + at, (int)(n - at));
   return u32x4{0, 0, 0, 0};
 }
 
-template <typename T>
+template <bool kPast = false, typename T>
 __device__ __forceinline__ void store_chunk(T* row, int64_t at, int64_t n, const float* x) {
   if (at + Rows<T>::kE <= n) {
-    Rows<T>::store(row + at, Rows<T>::pack(x));
+    if constexpr (kPast) Rows<T>::store_past(row + at, Rows<T>::pack(x));
+    else Rows<T>::store(row + at, Rows<T>::pack(x));
   } else {
 #pragma unroll
     for (int e = 0; e < Rows<T>::kE - 1; ++e)

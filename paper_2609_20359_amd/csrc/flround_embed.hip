@@ -15,8 +15,8 @@ namespace {
 // written at a time lies together.  Outputs larger than the L2s go past them (16384 rows
 // of 8 KiB, of 7 k words: 31.4 us, 6.1 TB/s; 46 through the caches, 43 with four chunks to
 // a lane).
-template <typename T>
-__global__ void __launch_bounds__(256) k_embed(const EmbedArgs a, int pieces, bool past) {
+template <typename T, bool kPast>
+__global__ void __launch_bounds__(256) k_embed(const EmbedArgs a, int pieces) {
   constexpr int E = Rows<T>::kE;
   const int lane = threadIdx.x & 63;
   const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -32,8 +32,7 @@ __global__ void __launch_bounds__(256) k_embed(const EmbedArgs a, int pieces, bo
 #pragma unroll
   for (int e = 0; e < E; ++e)
     f[e] = id < 0 ? 0.f : id >= a.V ? __builtin_nanf("") : f[e] * a.scale;
-  if (past && at + E <= a.D) Rows<T>::store_past(out + at, Rows<T>::pack(f));
-  else store_chunk(out, at, a.D, f);
+  store_chunk<kPast>(out, at, a.D, f);
 }
 
 // The tokens by word.  A workgroup finds those of a.words words, and where they begin
@@ -64,8 +63,7 @@ __device__ __forceinline__ void fill_zero(const EmbedArgs& a, int64_t block) {
   const int64_t at = (block * blockDim.x + threadIdx.x) * E, n = a.V * a.D;
   T* out = static_cast<T*>(a.out);
   const float zero[E] = {};
-  if (at + E <= n) Rows<T>::store_past(out + at, Rows<T>::pack(zero));
-  else store_chunk(out, at, n, zero);
+  store_chunk<true>(out, at, n, zero);
 }
 
 template <typename T>
@@ -185,7 +183,7 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
 }
 
 // scale * sum, beside what stands there, into the gradient's row (from column `at` on).
-template <typename T, bool kAdd>
+template <typename T, bool kAdd, bool kPast = false>
 __device__ __forceinline__ void write_row(const EmbedArgs& a, int64_t word, int64_t at,
                                           const float acc[Rows<T>::kE], u32x4 there) {
   constexpr int E = Rows<T>::kE;
@@ -193,7 +191,7 @@ __device__ __forceinline__ void write_row(const EmbedArgs& a, int64_t word, int6
   Rows<T>::floats(there, old);
 #pragma unroll
   for (int e = 0; e < E; ++e) f[e] = kAdd ? old[e] + acc[e] * a.scale : acc[e] * a.scale;
-  store_chunk(static_cast<T*>(a.out) + word * a.D, at, a.D, f);
+  store_chunk<kPast>(static_cast<T*>(a.out) + word * a.D, at, a.D, f);
 }
 
 constexpr int kJoinWaves = 8;
@@ -203,8 +201,9 @@ constexpr int kJoinWaves = 8;
 // leave their part in the slab (rows 0 and 1 of the tile's).  What it reads of dout, and
 // of the gradient where it adds to it, is asked for kAhead tokens ahead, in a loop: 16
 // tokens at a time without one are code that is slower to fetch than the rows (32768
-// tokens added to 32000 x 2048: 46 us, 4.4 TB/s; without the loop 52).
-template <typename T, bool kAdd>
+// tokens added to 32000 x 2048: 82 us for the gradient, 92 without the loop).  More rows
+// than the L2s hold are read past them: 73.
+template <typename T, bool kAdd, bool kPastIn, bool kPastOut>
 __global__ void __launch_bounds__(256) k_embed_sum(const EmbedArgs a, int pieces) {
   constexpr int E = Rows<T>::kE, kAhead = 4;
   const int lane = threadIdx.x & 63;
@@ -232,7 +231,7 @@ __global__ void __launch_bounds__(256) k_embed_sum(const EmbedArgs a, int pieces
     for (int i = 0; i < kAhead; ++i) {
       if (i0 + i >= count) continue;
       const int t = __builtin_amdgcn_readlane(mine.x, i0 + i);
-      x[i] = load_chunk(in + t * a.ld, at, a.D);
+      x[i] = load_chunk<kPastIn>(in + t * a.ld, at, a.D);
       if constexpr (kAdd) {
         const int64_t word = __builtin_amdgcn_readlane(mine.y, i0 + i);
         const int next = i0 + i + 1 < count ? __builtin_amdgcn_readlane(mine.y, i0 + i + 1) : after;
@@ -263,7 +262,7 @@ __global__ void __launch_bounds__(256) k_embed_sum(const EmbedArgs a, int pieces
       if (word == next && !last) continue;
       if (at < a.D) {
         if (whole && word != next) {
-          write_row<T, kAdd>(a, word, at, acc, there[i]);
+          write_row<T, kAdd, kPastOut>(a, word, at, acc, there[i]);
         } else {
           f32x4* p = reinterpret_cast<f32x4*>(slab + (whole ? a.ld_slab : 0));
 #pragma unroll
@@ -363,8 +362,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(const EmbedArgs a, in
       if (used[row]) continue;
       T* to = static_cast<T*>(a.out) + (v0 + row) * a.D;
       const int64_t k = (int64_t)(c - row * chunks) * E;
-      if (k + E <= a.D) Rows<T>::store_past(to + k, Rows<T>::pack(zero));
-      else store_chunk(to, k, a.D, zero);
+      store_chunk<true>(to, k, a.D, zero);
     }
     return;
   }
@@ -430,13 +428,11 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(const EmbedArgs a, in
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-constexpr int64_t kL2Bytes = (int64_t)32 << 20;   // of the eight L2s
-
 template <typename T>
 hipError_t embed(const EmbedArgs& a, hipStream_t st) {
   const int pieces = (int)ceil_div(a.D, 64 * Rows<T>::kE);
-  const bool past = a.T * a.D * (int64_t)sizeof(T) > kL2Bytes;
-  return launch(k_embed<T>, dim3((unsigned)ceil_div(a.T * pieces, 4)), 256, 0, st, a, pieces, past);
+  return launch(past_l2(a.T * a.D * (int64_t)sizeof(T)) ? k_embed<T, true> : k_embed<T, false>,
+                dim3((unsigned)ceil_div(a.T * pieces, 4)), 256, 0, st, a, pieces);
 }
 
 template <typename T, bool kAdd>
@@ -461,7 +457,13 @@ hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
     return e;
   if (tiles == 0) return hipSuccess;
   const dim3 grid((unsigned)ceil_div(tiles * pieces, 4));
-  if (const hipError_t e = launch(k_embed_sum<T, kAdd>, grid, 256, 0, st, a, pieces)) return e;
+  const bool in = past_l2(a.T * a.D * (int64_t)sizeof(T)), out = past_l2(a.V * a.D * (int64_t)sizeof(T));
+  if (const hipError_t e = launch(in ? (out ? k_embed_sum<T, kAdd, true, true>
+                                            : k_embed_sum<T, kAdd, true, false>)
+                                     : (out ? k_embed_sum<T, kAdd, false, true>
+                                            : k_embed_sum<T, kAdd, false, false>),
+                                  grid, 256, 0, st, a, pieces))
+    return e;
   return tiles > 1 ? launch(k_embed_join<T, kAdd>, dim3((unsigned)(tiles * pieces)),
                             64 * kJoinWaves, 0, st, a, pieces)
                    : hipSuccess;

@@ -32,10 +32,10 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N], int wav
 }
 
 // y = (x - mean) rstd w + b.  W waves to a row, K chunks to a lane; outputs larger than the
-// L2s go past them.  (16384 x 4096 bf16, four waves of two chunks: 45 us, 5.9 TB/s; 46
-// through the caches, 45.4 with eight waves of a chunk.)
-template <typename T, int W, int K, bool kRms>
-__global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a, bool past) {
+// L2s go past them, and so do inputs.  (16384 x 4096 bf16, four waves of two chunks: 44 us,
+// 6.1 TB/s; 46 through the caches, 45 only with outputs past them.)
+template <typename T, int W, int K, bool kRms, bool kPast>
+__global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a) {
   constexpr int E = Rows<T>::kE, kAt = W < 4 ? 4 / W : 1;
   __shared__ float red[2][W][1];
   const int lane = threadIdx.x & 63;
@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a,
   const T* row = static_cast<const T*>(a.x) + r * a.ldx;
   u32x4 x[K];
 #pragma unroll
-  for (int k = 0; k < K; ++k) x[k] = load_chunk(row, at + k * kNext, a.D);
+  for (int k = 0; k < K; ++k) x[k] = load_chunk<kPast>(row, at + k * kNext, a.D);
   const T* wt = static_cast<const T*>(a.weight);
   const T* bs = static_cast<const T*>(a.bias);
   u32x4 w[K] = {}, b[K] = {};
@@ -104,19 +104,18 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a,
       if (bs) y = y + h[e];
       f[e] = y;
     }
-    if (past && at + k * kNext + E <= a.D) Rows<T>::store_past(out + at + k * kNext, Rows<T>::pack(f));
-    else store_chunk(out, at + k * kNext, a.D, f);
+    store_chunk<kPast>(out, at + k * kNext, a.D, f);
   }
 }
 
 // dx = rstd (c - mean(c) - xh mean(c xh)), c = dy w, xh = (x - mean) rstd (the second
 // term not for a root mean square), and the workgroup's sums of dy xh and of dy, which it
 // holds in registers over all of its rows, R at a time.  kNext: the next rows are asked
-// for while these are summed.  (16384 x 4096 bf16, two rows of eight waves: 70.6 us, 5.7
-// TB/s, and 4.6 for the parts; four waves of two chunks 76.7 in all, without the next rows
-// 78.6.)
-template <typename T, int W, int K, int R, bool kRms, bool kNext>
-__global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a, bool past) {
+// for while these are summed.  (16384 x 4096 bf16, two rows of eight waves, inputs past the
+// caches: 71 us, 5.7 TB/s, 4.6 of them for the parts; through the caches 74, and so four
+// waves of two chunks 76.7, without the next rows 78.6.)
+template <typename T, int W, int K, int R, bool kRms, bool kNext, bool kPast>
+__global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a) {
   constexpr int E = Rows<T>::kE;
   __shared__ float red[2][R][W][2];
   const int lane = threadIdx.x & 63;
@@ -141,9 +140,11 @@ __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a, bool
   auto ask = [&](int64_t row) {
     const bool some = row < a.T;
 #pragma unroll
-    for (int k = 0; k < K; ++k) xn[k] = load_chunk(xs + row * a.ldx, at + k * kStep, some ? a.D : 0);
+    for (int k = 0; k < K; ++k)
+      xn[k] = load_chunk<kPast>(xs + row * a.ldx, at + k * kStep, some ? a.D : 0);
 #pragma unroll
-    for (int k = 0; k < K; ++k) dn[k] = load_chunk(ds + row * a.ldy, at + k * kStep, some ? a.D : 0);
+    for (int k = 0; k < K; ++k)
+      dn[k] = load_chunk<kPast>(ds + row * a.ldy, at + k * kStep, some ? a.D : 0);
     mean_n = !kRms && some ? a.mean_in[row] : 0.f;
     rstd_n = some ? a.rstd_in[row] : 0.f;
   };
@@ -191,9 +192,7 @@ __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a, bool
         if constexpr (!kRms) c = c - m1;
         f[e] = rstd * __builtin_fmaf(-xh, m0, c);
       }
-      if (past && at + k * kStep + E <= a.D)
-        Rows<T>::store_past(out + at + k * kStep, Rows<T>::pack(f));
-      else store_chunk(out, at + k * kStep, a.D, f);
+      store_chunk<kPast>(out, at + k * kStep, a.D, f);
     }
   }
   // the sums of the waves that hold the same columns, halving the groups, then the
@@ -322,16 +321,13 @@ __global__ void __launch_bounds__(64 * kSumWaves) k_norm_sum(const NormArgs a) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-constexpr int64_t kL2Bytes = (int64_t)32 << 20;   // of the eight L2s
-
-// Whether an output goes past the caches: one that they do not hold.
-bool past(const NormArgs& a) { return a.T * a.D * (a.bf16 ? 2 : 4) > kL2Bytes; }
+bool past(const NormArgs& a) { return past_l2(a.T * a.D * (a.bf16 ? 2 : 4)); }
 
 template <typename T, int W, int K, bool kRms>
 hipError_t forward(const NormArgs& a, hipStream_t st) {
   const int rows = W < 4 ? 4 / W : 1;
-  return launch(k_norm<T, W, K, kRms>, dim3((unsigned)ceil_div(a.T, rows)), W < 4 ? 256 : 64 * W, 0,
-                st, a, past(a));
+  return launch(past(a) ? k_norm<T, W, K, kRms, true> : k_norm<T, W, K, kRms, false>,
+                dim3((unsigned)ceil_div(a.T, rows)), W < 4 ? 256 : 64 * W, 0, st, a);
 }
 
 template <typename T, bool kRms>
@@ -349,8 +345,9 @@ hipError_t forward(const NormArgs& a, hipStream_t st) {
 
 template <typename T, int W, int K, int R, bool kNext, bool kRms>
 hipError_t backward(const NormArgs& a, hipStream_t st) {
-  return launch(k_norm_grad<T, W, K, R, kRms, kNext>, dim3((unsigned)a.n_parts), 64 * W * R, 0, st,
-                a, past(a));
+  return launch(past(a) ? k_norm_grad<T, W, K, R, kRms, kNext, true>
+                        : k_norm_grad<T, W, K, R, kRms, kNext, false>,
+                dim3((unsigned)a.n_parts), 64 * W * R, 0, st, a);
 }
 
 template <typename T, int W, bool kRms>
