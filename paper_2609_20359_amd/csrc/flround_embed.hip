@@ -455,7 +455,6 @@ hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
   if (const hipError_t e = launch(k_embed_sort<T>, dim3((unsigned)(sorts + fills)), threads, lds, st,
                                   a, (int)sorts))
     return e;
-  if (tiles == 0) return hipSuccess;
   const dim3 grid((unsigned)ceil_div(tiles * pieces, 4));
   const bool in = past_l2(a.T * a.D * (int64_t)sizeof(T)), out = past_l2(a.V * a.D * (int64_t)sizeof(T));
   if (const hipError_t e = launch(in ? (out ? k_embed_sum<T, kAdd, true, true>
@@ -464,9 +463,8 @@ hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
                                             : k_embed_sum<T, kAdd, false, false>),
                                   grid, 256, 0, st, a, pieces))
     return e;
-  return tiles > 1 ? launch(k_embed_join<T, kAdd>, dim3((unsigned)(tiles * pieces)),
-                            64 * kJoinWaves, 0, st, a, pieces)
-                   : hipSuccess;
+  return launch(k_embed_join<T, kAdd>, dim3((unsigned)(tiles * pieces)), 64 * kJoinWaves, 0, st, a,
+                pieces);
 }
 
 }  // namespace

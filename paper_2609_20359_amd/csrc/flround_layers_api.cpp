@@ -87,7 +87,7 @@ EmbedPlan embed_plan(const fl_embed_shape& s) {
   };
   p.start = take(4 * (s.vocab + 1));
   p.order = take(8 * s.tokens);
-  p.slab = take(tiles > 1 ? 8 * tiles * round_up(s.width, 8) : 0);
+  p.slab = take(8 * tiles * round_up(s.width, 8));
   p.bytes = at + 256;   // for a workspace that does not start on 256 bytes
   return p;
 }

@@ -339,8 +339,8 @@ hipError_t forward(const NormArgs& a, hipStream_t st) {
   if (c <= 512) return forward<T, 4, 2, kRms>(a, st);
   if (c <= 1024) return forward<T, 8, 2, kRms>(a, st);
   if (c <= 2048) return forward<T, 16, 2, kRms>(a, st);
-  if (c <= 4096) return forward<T, 16, 4, kRms>(a, st);
-  return forward<T, 16, 8, kRms>(a, st);
+  if constexpr (Rows<T>::kE == 8) return forward<T, 16, 4, kRms>(a, st);
+  else return c <= 4096 ? forward<T, 16, 4, kRms>(a, st) : forward<T, 16, 8, kRms>(a, st);
 }
 
 template <typename T, int W, int K, int R, bool kNext, bool kRms>
@@ -377,8 +377,10 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
   if (c <= 512) return backward<T, 8, 1, 2, true, kRms>(a, st);
   if (c <= 1024) return backward<T, 16, 1, 1, true, kRms>(a, st);
   if (c <= 2048) return backward<T, 16, 2, 1, false, kRms>(a, st);
-  if (c <= 4096) return backward<T, 16, 4, 1, false, kRms>(a, st);
-  return backward<T, 16, 8, 1, false, kRms>(a, st);
+  if constexpr (Rows<T>::kE == 8) return backward<T, 16, 4, 1, false, kRms>(a, st);
+  else
+    return c <= 4096 ? backward<T, 16, 4, 1, false, kRms>(a, st)
+                     : backward<T, 16, 8, 1, false, kRms>(a, st);
 }
 
 }  // namespace
