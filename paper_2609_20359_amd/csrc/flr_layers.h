@@ -12,6 +12,10 @@ namespace flr {
 // past them.
 inline bool past_l2(int64_t bytes) { return bytes > (int64_t)32 << 20; }
 
+// Threads of one launch, of which HIP takes less than 2^32: what needs more takes several
+// (each of them milliseconds long, so that another costs nothing).
+constexpr int64_t kMaxLaunchThreads = (int64_t)1 << 31;
+
 // The embedding and its gradient.
 struct EmbedArgs {
   int64_t T, V, D, ld;     // ld: elements between rows of the input
@@ -31,6 +35,12 @@ struct EmbedArgs {
   float* slab;             // two rows per tile: sums of words that go on beyond it
   int64_t ld_slab;
 };
+
+// Waves to a row of the input, which has a chunk of 16 bytes for each lane.
+inline int embed_pieces(const EmbedArgs& a) {
+  const int64_t wave = 64 * (a.bf16 ? 8 : 4);
+  return (int)((a.D + wave - 1) / wave);
+}
 
 // Tokens up to which the gradient is one launch, whose workgroups all read all ids (1000
 // tokens into 5000 x 1024: 12.5 us, 14.1 by the sort, but 22 and 18.6 where nine of ten are
@@ -68,6 +78,7 @@ int norm_rows(int64_t width, bool bf16);
 hipError_t launch_norm(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_grad(const NormArgs& a, hipStream_t st);
 
+// Up to kMaxLaunchThreads.
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t st);
 hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st);
 

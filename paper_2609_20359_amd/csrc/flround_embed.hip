@@ -430,14 +430,14 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 template <typename T>
 hipError_t embed(const EmbedArgs& a, hipStream_t st) {
-  const int pieces = (int)ceil_div(a.D, 64 * Rows<T>::kE);
+  const int pieces = embed_pieces(a);
   return launch(past_l2(a.T * a.D * (int64_t)sizeof(T)) ? k_embed<T, true> : k_embed<T, false>,
                 dim3((unsigned)ceil_div(a.T * pieces, 4)), 256, 0, st, a, pieces);
 }
 
 template <typename T, bool kAdd>
 hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
-  const int pieces = (int)ceil_div(a.D, 64 * Rows<T>::kE);
+  const int pieces = embed_pieces(a);
   if (a.T <= kEmbedFew) {
     // zeros of 16 KiB to a workgroup
     const int64_t row = a.D * (int64_t)sizeof(T);

@@ -135,9 +135,15 @@ int fl_embed(const fl_embed_shape* shape, const int64_t* ids, const void* weight
   if ((rc = elem_ptr(weight, 1, es)) != FL_OK) return rc;
   if ((rc = elem_ptr(out, shape->tokens, es)) != FL_OK) return rc;
   if (out == weight) return FL_ERR_INVALID;
-  if (shape->tokens == 0) return FL_OK;
-  return status_of(launch_embed(embed_args(*shape, ids, weight, scale, out),
-                                static_cast<hipStream_t>(stream)));
+  EmbedArgs a = embed_args(*shape, ids, weight, scale, out);
+  const int64_t most = kMaxLaunchThreads / (64 * embed_pieces(a));   // tokens of a launch
+  for (int64_t t = 0; t < shape->tokens; t += most) {
+    a.T = std::min(most, shape->tokens - t);
+    a.ids = ids + t;
+    a.out = static_cast<char*>(out) + t * a.D * (int64_t)es;
+    if ((rc = status_of(launch_embed(a, static_cast<hipStream_t>(stream)))) != FL_OK) return rc;
+  }
+  return FL_OK;
 }
 
 size_t fl_embed_workspace_bytes(const fl_embed_shape* shape) {

@@ -1,0 +1,73 @@
+// Calls the library's entry points at sizes that need many threads, with the kernels'
+// launches replaced by functions that note what each one covers: every launch is one that
+// HIP takes, and together they cover the call's work once (test code; no GPU; run by
+// tests/test_launches_cpu.py).
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+
+#include "flr_layers.h"
+#include "flround.h"
+
+namespace {
+
+constexpr int64_t kTooMany = (int64_t)1 << 32;   // threads that HIP does not take
+char* const kIn = reinterpret_cast<char*>((uintptr_t)1 << 40);    // never dereferenced
+char* const kOut = reinterpret_cast<char*>((uintptr_t)1 << 50);
+
+struct Span {
+  int64_t from, n;   // bytes of the output
+};
+std::vector<Span> spans;
+
+void check(bool ok, const char* what) {
+  if (ok) return;
+  std::printf("wrong: %s\n", what);
+  std::exit(1);
+}
+
+// The spans follow each other from 0 to n.
+void check_cover(int64_t n, const char* what) {
+  std::sort(spans.begin(), spans.end(), [](Span a, Span b) { return a.from < b.from; });
+  int64_t at = 0;
+  for (const Span& s : spans) {
+    check(s.from == at && s.n > 0, what);
+    at += s.n;
+  }
+  check(at == n, what);
+  std::printf("%s: %zu launches\n", what, spans.size());
+  spans.clear();
+}
+
+}  // namespace
+
+namespace flr {
+
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t) {
+  const int64_t es = a.bf16 ? 2 : 4, chunk = 16 / es;
+  check((a.D + 64 * chunk - 1) / (64 * chunk) * a.T * 64 + 256 < kTooMany, "threads of the embedding");
+  const int64_t from = static_cast<char*>(a.out) - kOut;
+  check(reinterpret_cast<const char*>(a.ids) - kIn == from / (a.D * es) * 8, "ids of a launch");
+  spans.push_back({from, a.T * a.D * es});
+  return hipSuccess;
+}
+
+hipError_t launch_embed_grad(const EmbedArgs&, hipStream_t) { return hipSuccess; }
+hipError_t launch_norm(const NormArgs&, hipStream_t) { return hipSuccess; }
+hipError_t launch_norm_grad(const NormArgs&, hipStream_t) { return hipSuccess; }
+int norm_rows(int64_t, bool) { return 1; }
+
+}  // namespace flr
+
+int main() {
+  const int64_t T = 1 << 20, D = 1 << 15;
+  for (int dtype : {FL_BF16, FL_F32})
+    for (int64_t tokens : {(int64_t)1, (int64_t)333, T / 8, T / 2 - 1, T - 1, T})
+      for (int64_t width : {(int64_t)1, (int64_t)4096, D - 511, D}) {
+        const fl_embed_shape s{tokens, 1000, width, 0, dtype};
+        check(fl_embed(&s, reinterpret_cast<int64_t*>(kIn), kIn, 1.f, kOut, nullptr) == FL_OK, "status");
+        check_cover(tokens * width * (dtype == FL_BF16 ? 2 : 4), "embedding");
+      }
+  return 0;
+}

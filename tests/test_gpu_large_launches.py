@@ -1,0 +1,33 @@
+"""Outputs, tables and states so large that one launch would take 2^32 threads or more,
+which HIP refuses: such a call takes several.  (The largest array of a test is 64 GiB.)"""
+import math
+
+import pytest
+
+from test_gpu_embed import env  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def give_back(env):  # noqa: F811
+    yield
+    env["torch"].cuda.synchronize()
+    env["torch"].cuda.empty_cache()
+
+
+def test_embed_of_64_gib(env):  # noqa: F811
+    """2^32 chunks of 16 bytes."""
+    torch, P = env["torch"], env["P"]
+    T, V, D = 1 << 20, 7, 1 << 15
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    w = torch.randn(V, D, generator=g, device="cuda").bfloat16()
+    ids = torch.randint(-1, V + 1, (T,), generator=g, device="cuda")
+    out = torch.full((T, D), -7.0, dtype=torch.bfloat16, device="cuda")
+    P.fl_embed(ids, w, out)
+    rows = torch.cat([w, torch.full((1, D), math.nan, dtype=w.dtype, device="cuda"),
+                      torch.zeros(1, D, dtype=w.dtype, device="cuda")])    # of V and of -1
+    for t in range(0, T, 1 << 15):
+        got, want = out[t:t + (1 << 15)], rows[ids[t:t + (1 << 15)]]
+        assert bool(((got == want) | (got.isnan() & want.isnan())).all()), t
