@@ -26,6 +26,7 @@ struct EmbedArgs {
   void* out;               // T x D, or the weight's gradient (V x D)
   int add;                 // gradient: added to what stands there
   // gradient's plan and workspace
+  int64_t zeros;           // elements of the table, from its first on, zeroed beside the sort
   int words;               // words whose tokens one workgroup of the sort finds
   int sort_waves;
   int list;                // found tokens that a wave of the sort can list
@@ -81,5 +82,7 @@ hipError_t launch_norm_grad(const NormArgs& a, hipStream_t st);
 // Up to kMaxLaunchThreads.
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t st);
 hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st);
+// Zeros to n elements, a thread to each chunk of 16 bytes.
+hipError_t launch_embed_zeros(void* out, int64_t n, bool bf16, hipStream_t st);
 
 }  // namespace flr

@@ -58,12 +58,16 @@ __device__ __forceinline__ int word_of(int2 id) { return id.y != 0 ? -1 : id.x; 
 // One chunk to a thread, so that all that is written at a time lies together (128 k rows of
 // 8 KiB beside the sort: 165 to 172 us; 2 chunks 180, 4 chunks 184), and past the caches.
 template <typename T>
-__device__ __forceinline__ void fill_zero(const EmbedArgs& a, int64_t block) {
+__device__ __forceinline__ void fill_zero(void* out, int64_t n, int64_t block) {
   constexpr int E = Rows<T>::kE;
-  const int64_t at = (block * blockDim.x + threadIdx.x) * E, n = a.V * a.D;
-  T* out = static_cast<T*>(a.out);
   const float zero[E] = {};
-  store_chunk<true>(out, at, n, zero);
+  store_chunk<true>(static_cast<T*>(out), (block * blockDim.x + threadIdx.x) * E, n, zero);
+}
+
+// What the sort's launch has no threads for.
+template <typename T>
+__global__ void __launch_bounds__(256) k_embed_zeros(void* out, int64_t n) {
+  fill_zero<T>(out, n, blockIdx.x);
 }
 
 template <typename T>
@@ -72,7 +76,7 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
   extern __shared__ int32_t lds[];   // next place [wave][word], then the waves' lists
   __shared__ int32_t sums[kEmbedMaxWaves], belows[kEmbedMaxWaves];
   if ((int)blockIdx.x >= sort_blocks) {
-    fill_zero<T>(a, (int)blockIdx.x - sort_blocks);
+    fill_zero<T>(a.out, a.zeros, (int)blockIdx.x - sort_blocks);
     return;
   }
   const int waves = blockDim.x / 64, lane = threadIdx.x & 63;
@@ -451,7 +455,7 @@ hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
   const unsigned threads = 64 * a.sort_waves;
   const size_t lds = (size_t)a.sort_waves * (a.words + a.list) * sizeof(int32_t);
   const int64_t sorts = ceil_div(a.V, a.words);
-  const int64_t fills = kAdd ? 0 : ceil_div(a.V * a.D, (int64_t)threads * Rows<T>::kE);
+  const int64_t fills = ceil_div(a.zeros, (int64_t)threads * Rows<T>::kE);
   if (const hipError_t e = launch(k_embed_sort<T>, dim3((unsigned)(sorts + fills)), threads, lds, st,
                                   a, (int)sorts))
     return e;
@@ -471,6 +475,11 @@ hipError_t embed_grad(const EmbedArgs& a, hipStream_t st) {
 
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
   return a.bf16 ? embed<uint16_t>(a, st) : embed<float>(a, st);
+}
+
+hipError_t launch_embed_zeros(void* out, int64_t n, bool bf16, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(n, 256 * (bf16 ? 8 : 4)));
+  return launch(bf16 ? k_embed_zeros<uint16_t> : k_embed_zeros<float>, grid, 256, 0, st, out, n);
 }
 
 hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st) {

@@ -169,7 +169,17 @@ int fl_embed_grad(const fl_embed_shape* shape, const int64_t* ids, const void* d
   a.order = reinterpret_cast<int2*>(ws + p.order);
   a.slab = reinterpret_cast<float*>(ws + p.slab);
   a.ld_slab = round_up(shape->width, 8);
-  return status_of(launch_embed_grad(a, static_cast<hipStream_t>(stream)));
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  // one launch writes the zeros of few tokens' gradient, row by row; else those that the
+  // sort's launch has no threads for are written before it
+  const int64_t table = a.V * a.D, most = kMaxLaunchThreads * (int64_t)(16 / es);
+  a.zeros = add || a.T <= kEmbedFew ? 0 : std::min(table, most);
+  for (int64_t from = a.zeros; a.zeros && from < table; from += most) {
+    char* at = static_cast<char*>(dweight) + from * (int64_t)es;
+    rc = status_of(launch_embed_zeros(at, std::min(most, table - from), a.bf16, st));
+    if (rc != FL_OK) return rc;
+  }
+  return status_of(launch_embed_grad(a, st));
 }
 
 int fl_layer_norm(const fl_norm_shape* shape, const void* x, const void* weight, const void* bias,

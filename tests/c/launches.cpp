@@ -53,7 +53,31 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t) {
   return hipSuccess;
 }
 
-hipError_t launch_embed_grad(const EmbedArgs&, hipStream_t) { return hipSuccess; }
+hipError_t launch_embed_zeros(void* out, int64_t n, bool bf16, hipStream_t) {
+  check((n * (bf16 ? 2 : 4) + 15) / 16 + 256 < kTooMany, "threads of the zeros");
+  spans.push_back({static_cast<char*>(out) - kOut, n * (bf16 ? 2 : 4)});
+  return hipSuccess;
+}
+
+hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t) {
+  const int64_t es = a.bf16 ? 2 : 4, table = a.V * a.D;
+  if (a.T <= kEmbedFew) {   // zeros by rows: 512 threads for 16 KiB, or for a row, or for 1024
+    const int64_t row = a.D * es, words = row < 16 ? 1024 : row < 16384 ? 16384 / row : 1;
+    check((a.V / words + 1 + a.T * embed_pieces(a)) * 512 < kTooMany, "threads of few tokens");
+    check(a.zeros == 0, "zeros of few tokens");
+    spans.push_back({0, table * es});
+    return hipSuccess;
+  }
+  const int64_t tiles = (a.T + a.tile - 1) / a.tile, threads = 64 * a.sort_waves;
+  const int64_t sorts = (a.V + a.words - 1) / a.words;
+  const int64_t fills = (a.zeros + threads * (16 / es) - 1) / (threads * (16 / es));
+  check((sorts + fills) * threads < kTooMany, "threads of the sort");
+  check(tiles * embed_pieces(a) * 512 < kTooMany, "threads of the sums and of the parts");
+  check(static_cast<char*>(a.out) == kOut, "the gradient");
+  if (a.zeros) spans.push_back({0, a.zeros * es});
+  return hipSuccess;
+}
+
 hipError_t launch_norm(const NormArgs&, hipStream_t) { return hipSuccess; }
 hipError_t launch_norm_grad(const NormArgs&, hipStream_t) { return hipSuccess; }
 int norm_rows(int64_t, bool) { return 1; }
@@ -69,5 +93,17 @@ int main() {
         check(fl_embed(&s, reinterpret_cast<int64_t*>(kIn), kIn, 1.f, kOut, nullptr) == FL_OK, "status");
         check_cover(tokens * width * (dtype == FL_BF16 ? 2 : 4), "embedding");
       }
+  for (int dtype : {FL_BF16, FL_F32})
+    for (int64_t tokens : {(int64_t)0, (int64_t)512, (int64_t)513, T})
+      for (int64_t vocab : {(int64_t)1, (int64_t)32000, T, 2 * T - 1, 2 * T})
+        for (int64_t width : {(int64_t)1, (int64_t)7, (int64_t)4096, D - 511, D})
+          for (int add : {0, 1}) {
+            const fl_embed_shape s{tokens, vocab, width, 0, dtype};
+            check(fl_embed_grad(&s, reinterpret_cast<int64_t*>(kIn), kIn, 1.f, add, kOut, kIn,
+                                fl_embed_workspace_bytes(&s), nullptr) == FL_OK, "status");
+            if (add) check(tokens <= 512 || spans.empty(), "no zeros where the sum is added");
+            if (add) spans.clear();
+            else check_cover(vocab * width * (dtype == FL_BF16 ? 2 : 4), "zeros");
+          }
   return 0;
 }

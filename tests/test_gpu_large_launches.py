@@ -31,3 +31,20 @@ def test_embed_of_64_gib(env):  # noqa: F811
     for t in range(0, T, 1 << 15):
         got, want = out[t:t + (1 << 15)], rows[ids[t:t + (1 << 15)]]
         assert bool(((got == want) | (got.isnan() & want.isnan())).all()), t
+
+
+@pytest.mark.parametrize("extra", [0, 5])
+def test_embed_grad_of_a_table_of_64_gib(env, extra):  # noqa: F811
+    """2^32 chunks of zeros, and some rows more; all values are whole and small."""
+    torch, P = env["torch"], env["P"]
+    V, D = (1 << 20) + extra, 1 << 15
+    half, last = 1 << 19, V - 1
+    ids = torch.tensor([0, half - 1, half, last] * 150 + [last, 77, -1, V], device="cuda")
+    d = torch.ones(ids.numel(), D, dtype=torch.bfloat16, device="cuda")
+    dw = torch.full((V, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    P.fl_embed_grad(ids, d, dw, scale=0.5)
+    for v, want in ((0, 75.0), (half - 1, 75.0), (half, 75.0), (last, 75.5), (77, 0.5)):
+        assert bool((dw[v] == want).all()), v
+        dw[v] = 0.0
+    for v in range(0, V, 1 << 15):
+        assert not bool(dw[v:v + (1 << 15)].any()), v

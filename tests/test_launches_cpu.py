@@ -21,3 +21,4 @@ def test_launches(tmp_path):
     r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, r.stdout
     assert "embedding: 1 launches" in r.stdout and "embedding: 4 launches" in r.stdout
+    assert "zeros: 1 launches" in r.stdout and "zeros: 8 launches" in r.stdout
