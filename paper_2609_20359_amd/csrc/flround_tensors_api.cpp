@@ -14,7 +14,9 @@ using namespace flr;
 namespace {
 
 constexpr int64_t kMaxUnits = (int64_t)1 << 32;        // of all tensors: 2^41 elements
-constexpr int64_t kMaxLaunchUnits = (int64_t)1 << 30;  // of one launch
+// Of one launch, whose threads, 64 to a unit, have to be fewer than 2^32: 2^32 elements,
+// whose step takes ten milliseconds, so that another launch costs nothing.
+constexpr int64_t kMaxLaunchUnits = (int64_t)1 << 23;
 
 int64_t units_of(int64_t numel) { return (numel + kUnit - 1) / kUnit; }
 

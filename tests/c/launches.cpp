@@ -8,12 +8,15 @@
 #include <vector>
 
 #include "flr_layers.h"
+#include "flr_scalars.h"
+#include "flr_tensors.h"
 #include "flround.h"
 
 namespace {
 
 constexpr int64_t kTooMany = (int64_t)1 << 32;   // threads that HIP does not take
 char* const kIn = reinterpret_cast<char*>((uintptr_t)1 << 40);    // never dereferenced
+char* const kWork = reinterpret_cast<char*>((uintptr_t)1 << 45);
 char* const kOut = reinterpret_cast<char*>((uintptr_t)1 << 50);
 
 struct Span {
@@ -82,7 +85,55 @@ hipError_t launch_norm(const NormArgs&, hipStream_t) { return hipSuccess; }
 hipError_t launch_norm_grad(const NormArgs&, hipStream_t) { return hipSuccess; }
 int norm_rows(int64_t, bool) { return 1; }
 
+bool hparams_ok(const fl_adamw_hparams*) { return true; }
+AdamScalars adam_scalars(const fl_adamw_hparams&, int64_t) { return {}; }
+
+// The tensors' masters stand in kOut as their moments do in the state; gradients and
+// working copies, of half the size, likewise in kIn and kWork.
+hipError_t launch_tensors(const TensorsArgs& a, int64_t units, hipStream_t) {
+  check(units * 64 + 256 < kTooMany, "threads of the step");
+  int n = 0;
+  while (n < kMaxTensors && a.first[n + 1] != INT32_MAX) ++n;
+  check(n > 0 && a.first[n] == units, "units of a launch");
+  for (int k = n + 1; k <= kMaxTensors; ++k) check(a.first[k] == INT32_MAX, "behind the last tensor");
+  for (int k = 0; k < n; ++k) {
+    const int64_t from = (a.unit0 + a.first[k]) * kUnit, its = a.first[k + 1] - a.first[k];
+    check(reinterpret_cast<char*>(a.master[k]) == kOut + 4 * from, "master");
+    check(static_cast<const char*>(a.grad[k]) == kIn + 2 * from, "gradient");
+    check(reinterpret_cast<char*>(a.working[k]) == kWork + 2 * from, "working copy");
+    check(a.numel[k] > (its - 1) * kUnit, "elements");
+    check(((a.decay[k / 32] >> (k % 32)) & 1) == (from / kUnit) % 2, "decay");
+    spans.push_back({from, its * kUnit});
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_state_convert(const StateDev&, const StateDev&, int64_t, hipStream_t) {
+  return hipSuccess;
+}
+
 }  // namespace flr
+
+namespace {
+
+// One step of tensors of these sizes.
+void tensors(const std::vector<int64_t>& sizes) {
+  std::vector<fl_tensor> t;
+  std::vector<const void*> grads;
+  int64_t at = 0;
+  for (int64_t n : sizes) {
+    t.push_back({n, reinterpret_cast<float*>(kOut + 4 * at),
+                 reinterpret_cast<uint16_t*>(kWork + 2 * at), (int)(at / 512 % 2)});
+    grads.push_back(kIn + 2 * at);
+    at += (n + 511) / 512 * 512;
+  }
+  const fl_adamw_hparams h{};
+  check(fl_adamw_tensors((int64_t)t.size(), t.data(), grads.data(), FL_BF16, 1.f, &h, 1, 8, kOut, 1,
+                         nullptr) == FL_OK, "status");
+  check_cover(at, "step");
+}
+
+}  // namespace
 
 int main() {
   const int64_t T = 1 << 20, D = 1 << 15;
@@ -105,5 +156,13 @@ int main() {
             if (add) spans.clear();
             else check_cover(vocab * width * (dtype == FL_BF16 ? 2 : 4), "zeros");
           }
+  const int64_t most = (int64_t)1 << 32;   // elements of a launch
+  tensors({1});
+  tensors({most});
+  tensors({most + 1});
+  tensors({most - 512, 512, 513, most, 7});
+  tensors({700, 3 * most + 5, 512, 1});
+  tensors({((int64_t)1 << 41) - 512, 1});
+  for (int64_t n : {95, 96, 97, 300}) tensors(std::vector<int64_t>(n, 777));
   return 0;
 }

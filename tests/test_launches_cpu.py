@@ -17,7 +17,8 @@ def test_launches(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-D__HIP_PLATFORM_AMD__",
                     "-I/opt/rocm/include", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", exe,
                     os.path.join(ROOT, "tests", "c", "launches.cpp"),
-                    os.path.join(CSRC, "flround_layers_api.cpp")], check=True)
+                    os.path.join(CSRC, "flround_layers_api.cpp"),
+                    os.path.join(CSRC, "flround_tensors_api.cpp")], check=True)
     r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, r.stdout
     assert "embedding: 1 launches" in r.stdout and "embedding: 4 launches" in r.stdout
