@@ -51,6 +51,15 @@ StateDev state_at(void* state, int64_t units, int bits) {
   return s;
 }
 
+// The state from a unit on.
+StateDev state_from(StateDev s, int64_t unit) {
+  const int64_t n = unit * kUnit, wide = s.bits / 8;
+  s.m = static_cast<char*>(s.m) + n * wide;
+  s.v = static_cast<char*>(s.v) + n * wide;
+  if (s.bits == 8) s.m_exp += n / kStateBlock, s.v_exp += n / kStateBlock;
+  return s;
+}
+
 int status_of(hipError_t e) {
   return e == hipSuccess ? FL_OK : e == hipErrorOutOfMemory ? FL_ERR_NOMEM : FL_ERR_HIP;
 }
@@ -150,9 +159,15 @@ int fl_state_convert(int64_t state_numel, int from_bits, const void* from, void*
   if ((rc = ptr_ok(from, 16)) != FL_OK || (rc = ptr_ok(to, 16)) != FL_OK) return rc;
   if (from == to) return FL_ERR_INVALID;
   const int64_t units = state_numel / kUnit;
-  return status_of(launch_state_convert(state_at(const_cast<void*>(from), units, from_bits),
-                                        state_at(to, units, 40 - from_bits), units,
+  const StateDev src = state_at(const_cast<void*>(from), units, from_bits);
+  const StateDev dst = state_at(to, units, 40 - from_bits);
+  for (int64_t u = 0; u < units; u += kMaxLaunchUnits) {
+    const int64_t n = units - u < kMaxLaunchUnits ? units - u : kMaxLaunchUnits;
+    rc = status_of(launch_state_convert(state_from(src, u), state_from(dst, u), n,
                                         static_cast<hipStream_t>(stream)));
+    if (rc != FL_OK) return rc;
+  }
+  return FL_OK;
 }
 
 }  // extern "C"

@@ -108,7 +108,21 @@ hipError_t launch_tensors(const TensorsArgs& a, int64_t units, hipStream_t) {
   return hipSuccess;
 }
 
-hipError_t launch_state_convert(const StateDev&, const StateDev&, int64_t, hipStream_t) {
+int64_t all;   // elements of a state that is converted
+
+hipError_t launch_state_convert(const StateDev& from, const StateDev& to, int64_t units,
+                                hipStream_t) {
+  check(units * 64 + 256 < kTooMany, "threads of the conversion");
+  const StateDev &narrow = from.bits == 8 ? from : to, &wide = from.bits == 8 ? to : from;
+  check(narrow.bits == 8 && wide.bits == 32, "bits");
+  const char *n = from.bits == 8 ? kIn : kOut, *w = from.bits == 8 ? kOut : kIn;
+  const int64_t at = static_cast<char*>(narrow.m) - n;
+  check(static_cast<char*>(narrow.v) == n + all + at, "codes of v");
+  check(reinterpret_cast<char*>(narrow.m_exp) == n + 2 * all + at / 64, "exponents of m");
+  check(reinterpret_cast<char*>(narrow.v_exp) == n + 2 * all + all / 64 + at / 64, "exponents of v");
+  check(static_cast<char*>(wide.m) == w + 4 * at, "m");
+  check(static_cast<char*>(wide.v) == w + 4 * all + 4 * at, "v");
+  spans.push_back({at, units * kUnit});
   return hipSuccess;
 }
 
@@ -164,5 +178,11 @@ int main() {
   tensors({700, 3 * most + 5, 512, 1});
   tensors({((int64_t)1 << 41) - 512, 1});
   for (int64_t n : {95, 96, 97, 300}) tensors(std::vector<int64_t>(n, 777));
+  for (int bits : {8, 32})
+    for (int64_t n : {(int64_t)512, most, most + 512, 3 * most - 1024, (int64_t)1 << 41}) {
+      flr::all = n;
+      check(fl_state_convert(n, bits, kIn, kOut, nullptr) == FL_OK, "status");
+      check_cover(n, "conversion");
+    }
   return 0;
 }

@@ -2,8 +2,10 @@
 which HIP refuses: such a call takes several.  (The largest array of a test is 64 GiB.)"""
 import math
 
+import numpy as np
 import pytest
 
+import state8 as S8
 from test_gpu_embed import env  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +50,39 @@ def test_embed_grad_of_a_table_of_64_gib(env, extra):  # noqa: F811
         dw[v] = 0.0
     for v in range(0, V, 1 << 15):
         assert not bool(dw[v:v + (1 << 15)].any()), v
+
+
+def test_convert_past_32_bits(env):  # noqa: F811
+    """A state of more elements than one launch takes, both ways: its first and last codes
+    and those where the launches meet."""
+    torch, P = env["torch"], env["P"]
+    n, k = (1 << 32) + 1024, 1024
+    narrow = torch.zeros(2 * n + n // 32, dtype=torch.uint8, device="cuda")
+    rng = np.random.RandomState(2)
+    starts = (0, (1 << 32) - k, n - k)
+    want = {}
+    for at in starts:
+        codes = [rng.randint(0, 8 * top + 7, k).astype(np.uint8) for top in (15, 31)]
+        exps = [rng.randint(100, 140, k // 64).astype(np.uint8) for _ in range(2)]
+        for c, e in zip(codes, exps):   # a block's exponent is that of its largest
+            c[::64] = 8 * (15 if c is codes[0] else 31)
+        for i, (c, e) in enumerate(zip(codes, exps)):
+            narrow[i * n + at:i * n + at + k] = torch.from_numpy(c).cuda()
+            first = 2 * n + i * (n // 64) + at // 64
+            narrow[first:first + k // 64] = torch.from_numpy(e).cuda()
+            want[i, at] = S8.decode(c, e, 15 if i == 0 else 31)
+    wide = torch.full((2 * n,), -7.0, device="cuda")
+    P.fl_state_convert(narrow, wide)
+    for (i, at), x in want.items():
+        part = wide[i * n + at:i * n + at + k]
+        assert np.array_equal(part.cpu().numpy(), x), (i, at)
+    back = torch.full_like(narrow, 99)
+    P.fl_state_convert(wide, back)
+    for (i, at), x in want.items():
+        c, e = S8.encode(x, 15 if i == 0 else 31)
+        first = 2 * n + i * (n // 64) + at // 64
+        assert np.array_equal(back[i * n + at:i * n + at + k].cpu().numpy(), c), (i, at)
+        assert np.array_equal(back[first:first + k // 64].cpu().numpy(), e), (i, at)
+        wide[i * n + at:i * n + at + k] = 0.0
+    for at in range(0, 2 * n, 1 << 30):
+        assert not bool(wide[at:at + (1 << 30)].any()), at
