@@ -123,6 +123,7 @@ __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a) {
   const int wave = all_waves % W, group = all_waves / W;
   const int64_t at = (wave * 64 + lane) * E;
   constexpr int64_t kStep = W * 64 * E;
+  const int left = (int)(a.D - at);   // elements of the row from this lane's first on
   const T* wt = static_cast<const T*>(a.weight);
   float dw[K][E] = {}, db[K][E] = {};
   u32x4 w[K] = {};
@@ -167,7 +168,8 @@ __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a) {
       Rows<T>::floats(w[k], h);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float xh = (f[e] - mean) * rstd;
+        // (behind the row's end 0, as mean * rstd may be no fp32 number)
+        const float xh = (kRms || (int)(k * kStep) + e < left ? f[e] - mean : 0.f) * rstd;
         const float c = wt ? g[e] * h[e] : g[e];
         s[0] = __builtin_fmaf(c, xh, s[0]);
         if constexpr (!kRms) s[1] = s[1] + c;
@@ -282,7 +284,7 @@ __global__ void __launch_bounds__(1024) k_norm_grad_few(const NormArgs a, int ro
   Rows<T>::floats(w, h);
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    f[e] = (f[e] - mean) * rstd;
+    f[e] = (kRms || at + e < n ? f[e] - mean : 0.f) * rstd;   // (0 behind the row's end)
     if (a.weight) g[e] = g[e] * h[e];
     s[0] = __builtin_fmaf(g[e], f[e], s[0]);
     if constexpr (!kRms) s[1] = s[1] + g[e];
