@@ -45,12 +45,13 @@ struct Rows<uint16_t> {
   static __device__ __forceinline__ float value(uint16_t x) {
     return __uint_as_float((uint32_t)x << 16);
   }
-  // the first n (1 to 7) elements at p, zeros behind them
+  // the first n (1 to 7) elements at p; behind them zeros, or with kFill the first one
+  template <bool kFill = false>
   static __device__ __forceinline__ u32x4 load_part(const uint16_t* p, int n) {
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < n) w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+    for (int e = 0; e < (kFill ? 8 : 7); ++e)
+      if (kFill || e < n) w[e / 2] |= (uint32_t)p[e < n ? e : 0] << (16 * (e & 1));
     return u32x4{w[0], w[1], w[2], w[3]};
   }
 };
@@ -80,11 +81,12 @@ struct Rows<float> {
   }
   static __device__ __forceinline__ float one(float x) { return x; }
   static __device__ __forceinline__ float value(float x) { return x; }
+  template <bool kFill = false>
   static __device__ __forceinline__ u32x4 load_part(const float* p, int n) {
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (e < n) w[e] = __float_as_uint(p[e]);
+    for (int e = 0; e < (kFill ? 4 : 3); ++e)
+      if (kFill || e < n) w[e] = __float_as_uint(p[e < n ? e : 0]);
     return u32x4{w[0], w[1], w[2], w[3]};
   }
 };

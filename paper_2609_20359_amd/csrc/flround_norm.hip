@@ -108,6 +108,16 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a)
   }
 }
 
+// As load_chunk, but with elements of the row behind its end, too (zeros for a row of no
+// elements): the gradient's lanes there have c = 0, and where mean * rstd is no fp32 number
+// (a row of one value, 2^100, and eps 2^-60) zeros in x's place would make c xh NaN.
+template <bool kPast = false, typename T>
+__device__ __forceinline__ u32x4 load_some(const T* row, int64_t at, int64_t n) {
+  if (at >= n) at = 0;
+  if (at + Rows<T>::kE <= n) return kPast ? Rows<T>::load_past(row + at) : Rows<T>::load(row + at);
+  return n > 0 ? Rows<T>::template load_part<true>(row + at, (int)(n - at)) : u32x4{0, 0, 0, 0};
+}
+
 // dx = rstd (c - mean(c) - xh mean(c xh)), c = dy w, xh = (x - mean) rstd (the second
 // term not for a root mean square), and the workgroup's sums of dy xh and of dy, which it
 // holds in registers over all of its rows, R at a time.  kNext: the next rows are asked
@@ -123,7 +133,6 @@ __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a) {
   const int wave = all_waves % W, group = all_waves / W;
   const int64_t at = (wave * 64 + lane) * E;
   constexpr int64_t kStep = W * 64 * E;
-  const int left = (int)(a.D - at);   // elements of the row from this lane's first on
   const T* wt = static_cast<const T*>(a.weight);
   float dw[K][E] = {}, db[K][E] = {};
   u32x4 w[K] = {};
@@ -142,7 +151,7 @@ __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a) {
     const bool some = row < a.T;
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      xn[k] = load_chunk<kPast>(xs + row * a.ldx, at + k * kStep, some ? a.D : 0);
+      xn[k] = load_some<kPast>(xs + row * a.ldx, at + k * kStep, some ? a.D : 0);
 #pragma unroll
     for (int k = 0; k < K; ++k)
       dn[k] = load_chunk<kPast>(ds + row * a.ldy, at + k * kStep, some ? a.D : 0);
@@ -168,8 +177,7 @@ __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a) {
       Rows<T>::floats(w[k], h);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        // (behind the row's end 0, as mean * rstd may be no fp32 number)
-        const float xh = (kRms || (int)(k * kStep) + e < left ? f[e] - mean : 0.f) * rstd;
+        const float xh = (f[e] - mean) * rstd;
         const float c = wt ? g[e] * h[e] : g[e];
         s[0] = __builtin_fmaf(c, xh, s[0]);
         if constexpr (!kRms) s[1] = s[1] + c;
@@ -274,7 +282,7 @@ __global__ void __launch_bounds__(1024) k_norm_grad_few(const NormArgs a, int ro
   const int64_t at = (wave * 64 + lane) * E, r = (int64_t)blockIdx.x * R + group;
   const bool some = r < a.T;
   const int64_t n = some ? a.D : 0;
-  const u32x4 x = load_chunk(xs + r * a.ldx, at, n), d = load_chunk(ds + r * a.ldy, at, n);
+  const u32x4 x = load_some(xs + r * a.ldx, at, n), d = load_chunk(ds + r * a.ldy, at, n);
   u32x4 w{0, 0, 0, 0};
   if (a.weight) w = load_chunk(static_cast<const T*>(a.weight), at, n);
   const float mean = !kRms && some ? a.mean_in[r] : 0.f, rstd = some ? a.rstd_in[r] : 0.f;
@@ -284,7 +292,7 @@ __global__ void __launch_bounds__(1024) k_norm_grad_few(const NormArgs a, int ro
   Rows<T>::floats(w, h);
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    f[e] = (kRms || at + e < n ? f[e] - mean : 0.f) * rstd;   // (0 behind the row's end)
+    f[e] = (f[e] - mean) * rstd;
     if (a.weight) g[e] = g[e] * h[e];
     s[0] = __builtin_fmaf(g[e], f[e], s[0]);
     if constexpr (!kRms) s[1] = s[1] + g[e];
