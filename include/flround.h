@@ -583,6 +583,8 @@ int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const 
  *   rms nonzero: the mean is taken as 0 (root mean square norm), and written as 0.
  *   weight, bias: D values of dtype, or NULL (1 and 0).  x: R rows (x_stride); y: R x D;
  *   mean, rstd: R floats (mean may be NULL), which the gradient needs.  eps finite, >= 0.
+ *   Squares and sums that are no fp32 numbers do no harm (the row is scaled by a power of
+ *   two); a row without variance has rstd = +inf where eps is 0, and y = NaN (0 / 0).
  *
  * fl_layer_norm_grad -- gradient of sum_rd dy[r][d] * y[r][d], at mean and rstd as
  *   fl_layer_norm wrote them; with xh = (x[r] - mean[r]) * rstd[r], c = dy[r] * weight:

@@ -1,7 +1,7 @@
 // flround_norm.hip -- gfx950 kernels of the layer norm and its gradient.
 //
 // Both read a row once, hold it in registers as it came (16-byte chunks, spread over
-// one, four or sixteen waves), and write a row: they are bound by memory.  Sums are in
+// one to sixteen waves), and write a row: they are bound by memory.  Sums are in
 // fp32 in a fixed order.
 #include "flr_launch.h"
 #include "flr_layers.h"
@@ -31,9 +31,80 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N], int wav
   }
 }
 
+// The largest of the threads' values (none of them NaN) over the waves of a row, in all.
+template <int W>
+__device__ __forceinline__ float row_max(float x, float (*red)[1], int wave) {
+  for (int d = 32; d > 0; d /= 2) x = __builtin_fmaxf(x, __shfl_xor(x, d));
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0) red[wave][0] = x;
+    __syncthreads();
+    x = red[0][0];
+    for (int w = 1; w < W; ++w) x = __builtin_fmaxf(x, red[w][0]);
+  }
+  return x;
+}
+
+// A row whose sum or whose squares are no fp32 numbers (values past 2^60), or whose squares
+// lose bits (values below 2^-60 beside an eps as small), from memory again: as the rows
+// below, but divided by 2^by, a power close to the row's largest magnitude or to sqrt(eps),
+// which is exact where it counts (2^0 for a row of zeros, or with an infinity or NaN).  All
+// waves of the row come here.
+template <typename T, int W, bool kRms>
+__device__ __forceinline__ void norm_scaled(const NormArgs& a, int64_t r, int64_t at,
+                                            float (*red)[W][1], int wave) {
+  constexpr int E = Rows<T>::kE;
+  constexpr int64_t kNext = W * 64 * E;
+  const T* row = static_cast<const T*>(a.x) + r * a.ldx;
+  const T* wt = static_cast<const T*>(a.weight);
+  const T* bs = static_cast<const T*>(a.bias);
+  int by = 0;
+  // f(element's place, its value / 2^by) for the lane's elements
+  auto every = [&](auto f) {
+#pragma unroll 1
+    for (int64_t k = at; k < a.D; k += kNext) {
+      float x[E];
+      Rows<T>::floats(load_chunk(row, k, a.D), x);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (k + e < a.D) f(k + e, __builtin_amdgcn_ldexpf(x[e], -by));
+    }
+  };
+  float most = 0.f, s[1] = {0.f}, q[1] = {0.f};
+  every([&](int64_t, float x) {
+    most = x == x ? __builtin_fmaxf(most, __builtin_fabsf(x)) : __builtin_inff();
+  });
+  most = row_max<W>(most, red[0], wave);
+  if (most > 0.f && most < __builtin_inff()) {
+    by = __builtin_amdgcn_frexp_expf(most);
+    const int least = a.eps > 0.f ? __builtin_amdgcn_frexp_expf(a.eps) / 2 : by;
+    by = by > least ? by : least;
+  }
+  if constexpr (!kRms) {
+    every([&](int64_t, float x) { s[0] = s[0] + x; });
+    row_sums<W>(s, red[1], wave);
+  }
+  const float n = (float)a.D, mean = kRms ? 0.f : s[0] / n;
+  every([&](int64_t, float x) { q[0] = __builtin_fmaf(x - mean, x - mean, q[0]); });
+  row_sums<W>(q, red[kRms ? 1 : 0], wave);
+  const float rstd = 1.0f / __builtin_sqrtf(q[0] / n + __builtin_amdgcn_ldexpf(a.eps, -2 * by));
+  if ((threadIdx.x & 63) == 0 && (W == 1 || wave == 0)) {
+    if (a.mean) a.mean[r] = __builtin_amdgcn_ldexpf(mean, by);
+    a.rstd[r] = __builtin_amdgcn_ldexpf(rstd, -by);
+  }
+  T* out = static_cast<T*>(a.y) + r * a.D;
+  every([&](int64_t k, float x) {
+    float y = (x - mean) * rstd;
+    if (wt) y = y * Rows<T>::value(wt[k]);
+    if (bs) y = y + Rows<T>::value(bs[k]);
+    out[k] = Rows<T>::one(y);
+  });
+}
+
 // y = (x - mean) rstd w + b.  W waves to a row, K chunks to a lane; outputs larger than the
 // L2s go past them, and so do inputs.  (16384 x 4096 bf16, four waves of two chunks: 44 us,
-// 6.1 TB/s; 46 through the caches, 45 only with outputs past them.)
+// 6.1 TB/s; 46 through the caches, 45 only with outputs past them.)  Rows at the ends of
+// fp32 are left to norm_scaled, which reads them again: kept in registers meanwhile, they
+// cost all rows of 16384 columns a quarter more time.
 template <typename T, int W, int K, bool kRms, bool kPast>
 __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a) {
   constexpr int E = Rows<T>::kE, kAt = W < 4 ? 4 / W : 1;
@@ -85,7 +156,13 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) k_norm(const NormArgs a)
     }
   }
   row_sums<W>(q, red[1], wave);
-  const float rstd = 1.0f / __builtin_sqrtf(q[0] / n + a.eps);
+  const float var = q[0] / n + a.eps;
+  const int ends = !(var >= 0x1p-120f && var <= 0x1.fffffep127f);   // (alike in all threads)
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(ends), 0)) {
+    norm_scaled<T, W, kRms>(a, r, at, red, wave);
+    return;
+  }
+  const float rstd = 1.0f / __builtin_sqrtf(var);
   if (lane == 0 && (W == 1 || wave == 0)) {
     if (a.mean) a.mean[r] = mean;
     a.rstd[r] = rstd;
