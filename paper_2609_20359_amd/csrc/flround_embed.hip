@@ -51,9 +51,9 @@ __global__ void __launch_bounds__(256) k_embed(const EmbedArgs a, int pieces) {
 
 constexpr int kIds = 16;   // ids that a lane holds at a time
 
-// Ids that are no words (< 0, or past 32 bits) as -1; those from V to 2^32 are no
+// Ids that are no words (< 0, or past 32 bits) as 2^32 - 1; those from V on are no
 // workgroup's.
-__device__ __forceinline__ int word_of(int2 id) { return id.y != 0 ? -1 : id.x; }
+__device__ __forceinline__ unsigned word_of(int2 id) { return id.y != 0 ? ~0u : (unsigned)id.x; }
 
 // One chunk to a thread, so that all that is written at a time lies together (128 k rows of
 // 8 KiB beside the sort: 165 to 172 us; 2 chunks 180, 4 chunks 184), and past the caches.
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
   }
   const int waves = blockDim.x / 64, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int v0 = blockIdx.x * a.words;
+  const unsigned v0 = blockIdx.x * a.words;
   const unsigned nv = (unsigned)(a.V - v0 < a.words ? a.V - v0 : a.words);
   const int share = (int)((a.T + waves * 64 - 1) / (waves * 64)) * 64;
   const int t0 = wave * share, t1 = t0 + share < (int)a.T ? t0 + share : (int)a.T;
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
   for (int i = lane; i < a.words; i += 64) mine[i] = 0;
   const uint64_t lower = (1ull << lane) - 1;
   const int2* ids = reinterpret_cast<const int2*>(a.ids);
-  // f(token, its word or -1) for 64 tokens of the share at a time
+  // f(token, its word or 2^32 - 1) for 64 tokens of the share at a time
   auto every = [&](auto f) {
     for (int t = t0; t < t1; t += 64 * kIds) {
       int2 id[kIds];
@@ -113,9 +113,9 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
         f(t0 + (int)(x & 0xFFFF), i + lane < found ? (int)(x >> 16) : -1);
       }
     } else {
-      every([&](int token, int word) {
-        const bool here = (unsigned)(word - v0) < nv;
-        if (__ballot(here)) f(token, here ? word - v0 : -1);
+      every([&](int token, unsigned word) {
+        const bool here = word - v0 < nv;
+        if (__ballot(here)) f(token, here ? (int)(word - v0) : -1);
       });
     }
   };
@@ -130,13 +130,13 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
       left &= ~same;
     }
   };
-  every([&](int token, int word) {
-    below += (unsigned)word < (unsigned)v0 ? 1 : 0;
-    const bool here = (unsigned)(word - v0) < nv;
+  every([&](int token, unsigned word) {
+    below += word < v0 ? 1 : 0;
+    const bool here = word - v0 < nv;
     const uint64_t at = __ballot(here);
     if (at) {
       const int place = found + __popcll(at & lower);
-      if (here && place < a.list) list[place] = (uint32_t)(word - v0) << 16 | (uint32_t)(token - t0);
+      if (here && place < a.list) list[place] = (word - v0) << 16 | (uint32_t)(token - t0);
       found += __popcll(at);
     }
   });
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(64 * kEmbedMaxWaves) k_embed_sort(const EmbedA
     const int first = w >= 0 ? mine[w] : 0;
     int rank, count;
     alike(w, rank, count);
-    if (w >= 0) a.order[first + rank] = make_int2(token, v0 + w);
+    if (w >= 0) a.order[first + rank] = make_int2(token, (int)v0 + w);
     if (w >= 0 && rank == 0) mine[w] = first + count;
   });
 }

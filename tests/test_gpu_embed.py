@@ -306,3 +306,24 @@ def test_refusals(env):
                      64, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(P.FlError):
             call()
+
+
+def test_ids_past_32_bits_among_many(env):
+    """As above, by way of the sort: ids whose low or high 32 bits are a word's, or a
+    negative number's, or 0."""
+    torch, P = env["torch"], env["P"]
+    V, top = 700, 1 << 31
+    odd = [1 << 32, (1 << 32) + 3, -(1 << 32) + 3, top - 1, top, top + 1, top + V, (1 << 32) - 1, (1 << 32) - V,
+           V, V + 1, -1, (1 << 63) - 1, -(1 << 63), 3 << 32, (699 << 32) + 699]
+    words = torch.arange(2000, device="cuda") % V
+    ids = torch.cat([words, torch.tensor(odd * 40, device="cuda")])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    ids = ids[torch.randperm(ids.numel(), generator=g, device="cuda")]
+    d = torch.ones(ids.numel(), 8, device="cuda")
+    d[(ids < 0) | (ids >= V)] = math.nan
+    dw = torch.empty(V, 8, device="cuda")
+    P.fl_embed_grad(ids, d, dw)
+    want = torch.full((V, 8), 2.0, device="cuda")
+    want[:600] = 3.0
+    assert torch.equal(dw, want)
