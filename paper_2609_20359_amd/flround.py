@@ -7,6 +7,7 @@ the current torch stream unless `stream` is given.  Every non-OK status
 raises FlError.  If the library is missing, importing the symbols raises:
 there is no fallback.
 """
+import array
 import ctypes
 import functools
 import operator
@@ -914,8 +915,8 @@ def _whole(t, dtype, what):
 class Tensors:
     """Parameters that fl_adamw_tensors steps together: float32 masters and their bf16
     working copies (None, or None for some: not written), all of one device, and which of
-    them decay (default: all).  It keeps the tensors and their addresses: make another one
-    when a parameter moves to other memory.
+    them decay (default: all).  It keeps the tensors, their memory and its addresses: when
+    one has moved to other memory, a step raises ValueError, and another Tensors is needed.
 
     n_state: elements of each moment; state(bits) gives a state before the first step."""
 
@@ -931,6 +932,7 @@ class Tensors:
         self.array = (FlTensor * max(count, 1))()
         self.device = None
         places = []
+        held, self._memory = [], []
         for i, (m, w) in enumerate(zip(self.masters, self.workings)):
             for t, dtype, what in ((m, torch.float32, "masters"), (w, torch.bfloat16, "workings")):
                 if t is None and what == "workings":
@@ -943,15 +945,24 @@ class Tensors:
                     raise ValueError("workings[%d] has %d elements; expected %d"
                                      % (i, t.numel(), m.numel()))
                 places.append((t.data_ptr(), t.numel() * t.element_size(), "%s[%d]" % (what, i)))
+                held.append(t)
+                self._memory.append(t.detach())   # (keeps it where t is given other memory)
             self.array[i] = FlTensor(m.numel(), m.data_ptr(), None if w is None else w.data_ptr(),
                                      1 if decays[i] else 0)
         places = sorted(p for p in places if p[1])
         for a, b in zip(places, places[1:]):
             if a[0] + a[1] > b[0]:
                 raise ValueError("%s and %s overlap" % (a[2], b[2]))
+        self._held, self._addresses = held, [t.data_ptr() for t in held]
         self.count = count
         self.sizes = [m.numel() for m in self.masters]
         self.n_state = int(lib().fl_tensors_state_numel(count, self.array))
+
+    def _check_places(self):
+        """That all masters and working copies are where they were."""
+        if list(map(_T.Tensor.data_ptr, self._held)) != self._addresses:
+            raise ValueError("a master or a working copy has moved to other memory: Tensors has "
+                             "to be made anew")
 
     def state(self, bits=8):
         """Moments of zero: a uint8 tensor for 8 bits, a float32 one (m, then v) for 32."""
@@ -963,6 +974,12 @@ class Tensors:
         return _T.zeros(nbytes if bits == 8 else nbytes // 4, dtype=dtype, device=device)
 
 
+@functools.lru_cache(maxsize=64)
+def _state_size(n, bits):
+    """Elements of the tensor that holds the moments of n elements."""
+    return lib().fl_tensors_state_bytes(n, bits) // (1 if bits == 8 else 4)
+
+
 def _state(t, n, dev, what):
     """(address, bits) of the moments of n elements."""
     torch = _T
@@ -972,12 +989,11 @@ def _state(t, n, dev, what):
         bits = 32
     else:
         raise ValueError("%s must be a uint8 or a float32 tensor" % what)
-    size = lib().fl_tensors_state_bytes(n, bits) // t.element_size()
-    return _array(t, (size,), t.dtype, dev, what), bits
+    return _array(t, (_state_size(n, bits),), t.dtype, dev, what), bits
 
 
 def _grad_ptrs(grads, sizes, dev):
-    """Addresses of the gradients (None for one that is left out), checked, and their
+    """Addresses of the gradients (0 for one that is left out), checked, and their
     dtype."""
     torch = _T
     T = torch.Tensor
@@ -995,7 +1011,7 @@ def _grad_ptrs(grads, sizes, dev):
     ptrs, dtype = [], None
     for i, g in enumerate(grads):
         if g is None:
-            ptrs.append(None)
+            ptrs.append(0)
             continue
         what = "grads[%d]" % i
         if dtype is None:
@@ -1024,6 +1040,7 @@ def fl_adamw_tensors(tensors, hp, step, grads, state, grad_scale=1.0, seed=0, st
     grads = list(grads)
     if len(grads) != count:
         raise ValueError("grads has %d entries; expected %d" % (len(grads), count))
+    tensors._check_places()
     ptrs, dtype = _grad_ptrs(grads, sizes, dev)
     if count == 0:
         return
@@ -1031,7 +1048,8 @@ def fl_adamw_tensors(tensors, hp, step, grads, state, grad_scale=1.0, seed=0, st
         raise ValueError("seed must be between 0 and 2^64 - 1")
     h = hparams(hp)
     p, bits = _state(state, tensors.n_state, dev, "state")
-    rc = lib().fl_adamw_tensors(count, tensors.array, (ctypes.c_void_p * count)(*ptrs),
+    at = array.array("Q", ptrs)
+    rc = lib().fl_adamw_tensors(count, tensors.array, at.buffer_info()[0],
                                 FL_F32 if dtype is torch.float32 else FL_BF16, float(grad_scale),
                                 ctypes.byref(h), int(step), bits, p, int(seed), _stream(stream))
     _check(rc, "fl_adamw_tensors")

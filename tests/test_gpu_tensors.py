@@ -446,3 +446,49 @@ def test_refusals(env):
             P.fl_state_convert(src, dst)
     empty = P.Tensors([])
     P.fl_adamw_tensors(empty, HP, 1, [], torch.zeros(0, device="cuda"))
+
+
+def test_a_parameter_that_moves(env):
+    """A master or a working copy that was given other memory, or whose memory was given
+    back: the step says so, and writes nowhere."""
+    torch, P = env["torch"], env["P"]
+
+    def resized(t):
+        t.untyped_storage().resize_(0)
+
+    def replaced(t):
+        t.data = t.data.clone()
+
+    for which in (0, 1):
+        for move in (replaced, resized):
+            masters = [torch.ones(n, device="cuda") for n in (100, 700, 0)]
+            workings = [torch.nn.Parameter(m.bfloat16()) for m in masters]
+            grads = [torch.ones_like(m) for m in masters]
+            ts = P.Tensors(masters, workings)
+            state = ts.state(8)
+            P.fl_adamw_tensors(ts, HP, 1, grads, state)
+            before = [t.detach().clone() for t in masters + workings]
+            move((masters, workings)[which][1])
+            kept = state.clone()
+            with pytest.raises(ValueError, match="moved"):
+                P.fl_adamw_tensors(ts, HP, 2, grads, state)
+            assert torch.equal(state, kept)
+            if move is replaced:
+                assert all(torch.equal(a, b) for a, b in zip(masters + workings, before))
+                P.fl_adamw_tensors(P.Tensors(masters, workings), HP, 2, grads, state)
+                assert not torch.equal(masters[1], before[1]) and not torch.equal(state, kept)
+                assert torch.equal(masters[0].bfloat16(), workings[0])
+
+
+def test_many_gradients_some_left_out(env):
+    """Addresses of gradients past the first launch's, with some left out on both sides."""
+    torch, P = env["torch"], env["P"]
+    sizes = [3] * 250
+    a, b = Group(torch, sizes, "bf16"), Group(torch, sizes, "bf16")
+    ta, tb = P.Tensors(a.masters), P.Tensors(b.masters)
+    left = {0, 1, 95, 96, 97, 200, 249}
+    before = [m.clone() for m in a.masters]
+    P.fl_adamw_tensors(ta, HP, 1, [None if k in left else g for k, g in enumerate(a.grads)], ta.state(32))
+    P.fl_adamw_tensors(tb, HP, 1, b.grads, tb.state(32))
+    for k in range(250):
+        assert torch.equal(a.masters[k], before[k] if k in left else b.masters[k]), k
