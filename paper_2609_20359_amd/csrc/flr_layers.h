@@ -45,7 +45,8 @@ inline int embed_pieces(const EmbedArgs& a) {
 
 // Tokens up to which the gradient is one launch, whose workgroups all read all ids (1000
 // tokens into 5000 x 1024: 12.5 us, 14.1 by the sort, but 22 and 18.6 where nine of ten are
-// one word).
+// one word; 512 tokens into 128256 x 4096 185 us, 513 by the sort 193).  It takes no
+// workspace.
 constexpr int kEmbedFew = 512;
 constexpr int kEmbedMaxWords = 512;
 constexpr int kEmbedMaxWaves = 16;
@@ -72,6 +73,11 @@ struct NormArgs {
   float* parts;            // n_parts rows of D for dweight, then as many for dbias
   int64_t n_parts;         // workgroups of the gradient
 };
+
+// Whether the gradient is one launch (up to 512 rows), which takes no workspace.
+inline bool norm_few(int64_t rows, int64_t width, bool bf16) {
+  return rows > 0 && rows <= 512 && width <= 1024 * (bf16 ? 8 : 4);
+}
 
 // Rows that a workgroup of the gradient takes at once.
 int norm_rows(int64_t width, bool bf16);

@@ -69,8 +69,10 @@ struct EmbedPlan {
 // wave for every 64 tokens up to the 16 that a workgroup has.
 EmbedPlan embed_plan(const fl_embed_shape& s) {
   EmbedPlan p{};
+  p.bytes = 256;   // for a workspace that does not start on 256 bytes
+  if (s.tokens <= kEmbedFew) return p;
   p.words = (int)std::min<int64_t>(ceil_div(s.vocab, kCus), kEmbedMaxWords);
-  p.waves = (int)std::clamp<int64_t>(ceil_div(s.tokens, 64), 1, kEmbedMaxWaves);
+  p.waves = (int)std::min<int64_t>(ceil_div(s.tokens, 64), kEmbedMaxWaves);
   // (the list's entries hold a token's place in the wave's share in 16 bits)
   p.list = (int)std::min<int64_t>(round_up(ceil_div(s.tokens, p.waves), 64), kEmbedMaxList);
   // Short tiles where tokens are few, as a wave takes its tokens one after the other; long
@@ -88,7 +90,7 @@ EmbedPlan embed_plan(const fl_embed_shape& s) {
   p.start = take(4 * (s.vocab + 1));
   p.order = take(8 * s.tokens);
   p.slab = take(8 * tiles * round_up(s.width, 8));
-  p.bytes = at + 256;   // for a workspace that does not start on 256 bytes
+  p.bytes += at;
   return p;
 }
 
@@ -109,7 +111,8 @@ int64_t norm_parts(const fl_norm_shape& s) {
 }
 
 size_t norm_bytes(const fl_norm_shape& s) {
-  return (size_t)(8 * norm_parts(s) * s.width) + 256;
+  const bool few = norm_few(s.rows, s.width, s.dtype == FL_BF16);
+  return (few ? 0 : (size_t)(8 * norm_parts(s) * s.width)) + 256;
 }
 
 NormArgs norm_args(const fl_norm_shape& s, const void* x, const void* weight) {

@@ -482,10 +482,8 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t st) {
   return a.rms ? forward<float, true>(a, st) : forward<float, false>(a, st);
 }
 
-constexpr int64_t kFewRows = 512;   // rows up to which the gradient is one launch
-
 hipError_t launch_norm_grad(const NormArgs& a, hipStream_t st) {
-  if (a.T > 0 && a.T <= kFewRows && a.D <= 1024 * (a.bf16 ? 8 : 4)) {
+  if (norm_few(a.T, a.D, a.bf16)) {
     if (a.bf16)
       return a.rms ? backward_few<uint16_t, true>(a, st) : backward_few<uint16_t, false>(a, st);
     return a.rms ? backward_few<float, true>(a, st) : backward_few<float, false>(a, st);

@@ -147,3 +147,16 @@ def test_binding_refuses_cpu_tensors():
     with pytest.raises(ValueError):
         P.fl_layer_norm_grad(w, None, None, torch.zeros(10), w.clone(), w.clone(), None, None,
                              rms=True)
+
+
+def test_calls_of_one_launch_need_no_workspace():
+    """Up to 512 tokens, or rows of up to 8192 bf16 or 4096 fp32 elements; more need theirs."""
+    L = P.lib()
+    for T, V, D in ((0, 100, 64), (1, 1 << 21, 1 << 15), (512, 5003, 1 << 15)):
+        for dtype in (F.FL_BF16, F.FL_F32):
+            assert L.fl_embed_workspace_bytes(ctypes.byref(eshape(T, V, D, 0, dtype))) == 256
+    assert L.fl_embed_workspace_bytes(ctypes.byref(eshape(513, 5003, 64))) > 4 * 5004 + 8 * 513
+    for R, D, dtype, few in ((0, 64, 0, True), (1, 64, 0, True), (512, 8192, 0, True), (512, 8193, 0, False),
+                             (513, 64, 0, False), (512, 4096, 1, True), (512, 4097, 1, False)):
+        n = L.fl_layer_norm_workspace_bytes(ctypes.byref(nshape(R, D, dtype=dtype)))
+        assert n == 256 if few else n > 8 * D, (R, D, dtype)
