@@ -50,8 +50,10 @@ inline int embed_pieces(const EmbedArgs& a) {
 constexpr int kEmbedFew = 512;
 constexpr int kEmbedMaxWords = 512;
 constexpr int kEmbedMaxWaves = 16;
-// Found tokens that a wave of the sort lists: half of its share of 32768 tokens (30 % of
-// them one word: 92 us for the gradient, 110 with a list of 512, which is read again).
+// Found tokens that a wave of the sort lists: half of its share of 32768 tokens.  (Added to
+// 32000 x 2048: 32768 tokens, 30 % of them one word, 74 us for the gradient, 91 with a list
+// of 512, as the ids of a share are read again where it is full; 131072 without a frequent
+// word 207 and 293.  With 90 % one word the list is full either way: 91 and 300.)
 constexpr int kEmbedMaxList = 1024;
 
 // The layer norm and its gradient.

@@ -76,10 +76,22 @@ EmbedPlan embed_plan(const fl_embed_shape& s) {
   // (the list's entries hold a token's place in the wave's share in 16 bits)
   p.list = (int)std::min<int64_t>(round_up(ceil_div(s.tokens, p.waves), 64), kEmbedMaxList);
   // Short tiles where tokens are few, as a wave takes its tokens one after the other; long
-  // ones where many words' parts would have to be joined (333 tokens: tiles of 4, 8 and 16
-  // 14.2, 14.9 and 17.7 us; 4096: 16, 32 and 64 191, 189 and 198; 32768, 30 % of them one
-  // word: 94, 86 and 82).
-  p.tile = s.tokens <= 1024 ? 4 : s.tokens <= 8192 ? 16 : 64;
+  // ones where many words' parts would have to be joined.  us for tiles of 4, 8, 16, 32 and
+  // 64, added to 32000 x 2048 bf16 (513 and 1024 tokens: x 4096), no word frequent / 90 % of
+  // the tokens one word:
+  //     513   14.2 16.1 18.7 25.7  -   / 16.2 17.4 18.8 25.4  -
+  //    1024   17.0 17.8 20.2 26.9  -   / 20.5 19.3 21.1 26.6  -
+  //    1025    -   15.9 19.3 26.2 39.1 /  -   19.0 21.0 26.5 38.8
+  //    2048    -   17.7 21.0 27.3 40.6 /  -   22.3 23.5 29.0 40.2
+  //    4096    -   22.3 23.6 29.0 41.6 /  -   31.3 28.0 32.7 44.5
+  //    8192    -   31.9 29.2 31.2 43.8 /  -   47.1 37.7 38.3 50.3
+  //   16384    -   52.0 46.2 44.1 50.1 /  -   85.8 65.1 53.4 57.2
+  //   32768    -   84.0 76.3 70.5 68.4 /  -  160.3 117.9 98.2 90.5
+  p.tile = s.tokens <= 1024    ? 4
+           : s.tokens <= 2048  ? 8
+           : s.tokens <= 8192  ? 16
+           : s.tokens <= 16384 ? 32
+                               : 64;
   const int64_t tiles = ceil_div(s.tokens, p.tile);
   size_t at = 0;
   auto take = [&at](int64_t bytes) {

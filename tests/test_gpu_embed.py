@@ -327,3 +327,11 @@ def test_ids_past_32_bits_among_many(env):
     want = torch.full((V, 8), 2.0, device="cuda")
     want[:600] = 3.0
     assert torch.equal(dw, want)
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("T", [1024, 1025, 2048, 2049, 8192, 8193, 16384, 16385])
+def test_both_sides_of_the_tiles_sizes(env, T, add):
+    """A third of the tokens one word, which goes on over many waves' tokens."""
+    ids, _, d = make(env["torch"], T, 900, 136, "bf16")
+    check_grad(env, ids, d, 900, 1.0, add)
