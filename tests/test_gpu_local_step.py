@@ -150,3 +150,63 @@ def test_step_in_a_graph(ex):
         torch.cuda.synchronize()
         assert torch.equal(m.grad, e.grad) and torch.equal(m.state, e.state)
         assert torch.equal(m.master, e.master) and torch.equal(m.working, e.working)
+
+
+def bounds(ex, m, ids, labels):
+    """What each element of the gradients may be off by: the errors at the top of this file
+    (x is exact here, as the scale is a power of two)."""
+    import torch
+
+    V, D, T = ex.V, ex.D, ex.T
+    w, W = m.w["norm"].double(), m.w["head"].double().view(V, D)
+    x = m.x.double()
+    rstd = 1 / (x.square().mean(1, keepdim=True) + ex.EPS).sqrt()
+    xh = x * rstd
+    y = xh * w
+    e_y = H * y.abs()
+    z = y @ W.t()
+    e_z = (e_y @ W.abs().t()).amax(1, keepdim=True)
+    p = torch.softmax(z, 1)
+    G = (p - torch.nn.functional.one_hot(labels, V)) / T
+    e_G = p * torch.expm1(2 * e_z) / T + H * G.abs()
+    dy = G @ W
+    e_dy = e_G @ W.abs() + H * dy.abs()
+    e_c = e_dy * w.abs()
+    c = dy * w
+    dx = rstd * (c - xh * (c * xh).mean(1, keepdim=True))
+    e_dx = rstd * (e_c + xh.abs() * (e_c * xh.abs()).mean(1, keepdim=True)) + H * dx.abs()
+    zero = torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    off = dict(head=e_G.t() @ y.abs() + (G.abs() + e_G).t() @ e_y, norm=(e_dy * xh.abs()).sum(0),
+               embed=zero.index_add(0, ids, e_dx) * ex.SCALE)
+    return {k: (off[k].flatten() + H * (m.g[k].double().abs() + off[k].flatten())) * 1.02 for k in off}
+
+
+def test_slopes_within_the_roundings(ex):
+    """Differences of the model's loss in 64 bits along each parameter's gradient and along
+    its signs: off from the step's gradient by no more than its elements may be, and by
+    1e-4 of it for the differences themselves (h moves a parameter by 1e-5 at most, so that
+    h^2 times a third derivative is far below).  Along the gradient that is about 1, 19 and
+    6 % for the head, the norm and the embedding."""
+    import torch
+
+    m, (ids, labels) = ex.Model(3, 0), ex.Data(6).batch()
+    m.gradients(ids, labels)
+    w, off = {k: m.w[k].double() for k in ex.SIZES}, bounds(ex, m, ids, labels)
+    most = dict(head=0.03, norm=0.25, embed=0.1)
+
+    def loss(w):
+        x = w["embed"].view(ex.V, ex.D)[ids] * ex.SCALE
+        y = x / (x.square().mean(1, keepdim=True) + ex.EPS).sqrt() * w["norm"]
+        z = y @ w["head"].view(ex.V, ex.D).t()
+        return (torch.logsumexp(z, 1) - z.gather(1, labels[:, None])[:, 0]).mean()
+
+    for k in ex.SIZES:
+        g = m.g[k].double()
+        for v in (g / g.norm(), torch.sign(g) / g.numel() ** 0.5):
+            h = 1e-5 / float(v.abs().max())
+            up, down = dict(w, **{k: w[k] + h * v}), dict(w, **{k: w[k] - h * v})
+            slope, want = float((loss(up) - loss(down)) / (2 * h)), float((g * v).sum())
+            may = float((off[k] * v.abs()).sum())
+            assert abs(slope - want) <= may + 1e-4 * want, k
+        v = g / g.norm()
+        assert float((off[k] * v.abs()).sum()) <= most[k] * float(g.norm()), k   # it says something
