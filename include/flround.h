@@ -574,8 +574,8 @@ int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const 
  *   the rows of the words that occur, rounded once, and the other rows are left alone
  *   (tied weights, several batches).  A negative id, or one >= V, takes no part: its
  *   row of dout is not looked at.  dout: T x D (stride: elements between its rows).
- *   workspace: fl_embed_workspace_bytes (0 is returned for an invalid shape); less:
- *   FL_ERR_SCRATCH.
+ *   workspace: fl_embed_workspace_bytes (0 is returned for an invalid shape; 256 up to 512
+ *   tokens, which use none); less: FL_ERR_SCRATCH.
  *
  * fl_layer_norm -- with E(.) the mean over a row's D elements:
  *     mean[r] = E(x[r]);  rstd[r] = 1 / sqrt(E((x[r] - mean[r])^2) + eps)
@@ -592,7 +592,8 @@ int fl_top_logits(int64_t rows, int64_t vocab, int64_t stride, int dtype, const 
  *     dweight = sum_r dy[r] * xh;  dbias = sum_r dy[r]
  *   dx: R x D; dweight, dbias: D values of dtype, or NULL; all are written, not added
  *   to.  dy: R rows (dy_stride).  mean is not read with rms.  workspace:
- *   fl_layer_norm_workspace_bytes.
+ *   fl_layer_norm_workspace_bytes (256 up to 512 rows of up to 8192 bf16 or 4096 fp32
+ *   elements, which use none).
  *
  * Limits (FL_ERR_INVALID beyond): tokens and rows <= 2^20, vocab <= 2^21, width <=
  * 2^15, strides <= 2^40.
@@ -633,15 +634,18 @@ int fl_layer_norm_grad(const fl_norm_shape* shape, const void* x, const void* we
  * where 8 bytes of moments for a parameter are too many.
  *
  * fl_adamw_tensors -- fl_adamw_step of each tensor, with g[i] = f32(grads[k][i]) *
- *   grad_scale, in one launch for up to 96 tensors; a parameter's arithmetic is that of
- *   fl_adamw_step, bit for bit.  tensors: host array, read during the call; grads: host
- *   array of `count` device pointers to values of grad_dtype (FL_BF16 or FL_F32).  A
- *   tensor whose gradient is NULL is left alone, its moments too; an empty tensor's
- *   pointers are not looked at.  master, working and gradients are aligned to their
- *   elements; masters and working copies overlap neither each other nor a gradient (a
- *   tensor is listed once).  step, h: as for fl_adamw_step; grad_scale finite.  There is
- *   no layout handle; the device is the current one; nothing is allocated, and calls may
- *   be captured into a HIP graph (which keeps the step's scalars as they are).
+ *   grad_scale, in one launch for up to 96 tensors and 2^32 elements; a parameter's
+ *   arithmetic is that of fl_adamw_step, bit for bit.  tensors: host array, read during the
+ *   call; grads: host array of `count` device pointers to values of grad_dtype (FL_BF16 or
+ *   FL_F32).  A tensor whose gradient is NULL is left alone, its moments too (those before
+ *   and behind it take a launch each); an empty tensor's pointers are not looked at.
+ *   master, working and gradients are aligned to their elements; masters, working copies
+ *   and the state overlap neither each other nor a gradient (a tensor is listed once).
+ *   step, h: as for fl_adamw_step; grad_scale finite.  There is no layout handle; the
+ *   device is the current one; nothing is allocated, and calls may be captured into a HIP
+ *   graph, which keeps the arguments as they are: the step's scalars, and with a seed the
+ *   random bits, so that every replay rounds an element alike (no mean of roundings over
+ *   replays of one step; capture the gradients and call the step outside).
  *
  *   state: device, 16-byte aligned, fl_tensors_state_bytes bytes, all zero before the
  *   first step.  With S = fl_tensors_state_numel (each tensor's elements rounded up to a
@@ -650,20 +654,25 @@ int fl_layer_norm_grad(const fl_norm_shape* shape, const void* x, const void* we
  *      8 bits: S codes of m, S of v, S / 64 exponent bytes of m, S / 64 of v.
  *   A block of 64 elements shares an exponent byte b: the exponent field of its largest
  *   finite magnitude as a float, one more where that one's mantissa is over 1.75, 12 at
- *   least (a lower byte, as before the first step, stands for 12).  A code of m is a sign, 4 bits of exponent E and 3 of mantissa M, of v 5 and 3;
- *   with T = 15 or 31 it stands for 2^(b - 127 + E - T) (1 + M / 8), or, where E = 0, for
+ *   least (a lower byte, as before the first step, stands for 12).  A code of m is a sign,
+ *   4 bits of exponent E and 3 of mantissa M, of v 5 and 3 (a v with a sign loses it); with
+ *   T = 15 or 31 it stands for 2^(b - 127 + E - T) (1 + M / 8), or, where E = 0, for
  *   2^(b - 126 - T) M / 8; E = T with M = 7 stands for NaN, and an infinite moment is held
- *   as NaN.  A moment in 32 bits (as AdamW defines it; the update itself takes it so)
- *   becomes a code
+ *   as NaN.  (2^128, which a magnitude from 1.9375 * 2^127 on is rounded to, is +-inf when
+ *   it is taken out.)  A moment in 32 bits (as AdamW defines it; the update itself takes it
+ *   so), its place between two codes held to 2^-20 of the block's smallest step, becomes a
+ *   code
  *     seed == 0: by rounding to nearest, ties to even;
  *     else: up with the probability of its place between the two codes (to 2^-20),
  *     with random bits that depend on seed, step and the element's place in state alone.
  *   A v above 0 is at least the smallest code.  seed must be 0 with 32 bits.
  *   Rounding to nearest is what holds a moment that moves by less than half a code's
- *   step (3 to 6 %) where it is; a seed lets it move on average.
+ *   step (3 to 6 %) where it is; a seed, with a step that counts up, lets it move on
+ *   average.
  *
  * fl_state_convert -- a state from 8 bits to 32 (exact), or from 32 to 8 (to nearest):
- *   from_bits 8 or 32; `to` has the other form.  state_numel: S.  Both 16-byte aligned.
+ *   from_bits 8 or 32; `to` has the other form.  state_numel: S.  Both 16-byte aligned,
+ *   and apart.
  *
  * fl_tensors_state_numel returns -1, fl_tensors_state_bytes 0 for invalid arguments.
  * Limit: S <= 2^41.

@@ -43,8 +43,9 @@ __global__ void __launch_bounds__(256) k_embed(const EmbedArgs a, int pieces) {
 // finds (few, as all workgroups read all tokens) and handles 64 of its list at a time;
 // one that finds more than the list holds reads the ids of its share again instead.
 //
-// 32768 tokens take 25 us, 6.5 of them reading the ids, which all waves do alike; the rest
-// is the workgroup of a word that 30 % of the tokens are.  4096 tokens take 9.
+// 32768 tokens take 23 us, 6.5 of them reading the ids, which all waves do alike; the rest
+// is the workgroup of a word that 30 % of the tokens are.  4096 tokens take 9.  The reading
+// grows as the tokens times the workgroups (256, or the words over 512).
 //
 // The workgroups behind those that sort fill the gradient with zeros meanwhile; the rows
 // of the words that occur are written by the next launch.

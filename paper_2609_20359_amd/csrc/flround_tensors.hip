@@ -9,10 +9,10 @@
 // States in 8 bits.  A block of 64 elements (16 lanes) shares an exponent byte b, that of
 // its largest magnitude.  A code is the top of the element's fp32 pattern after scaling
 // by 2^(15 - b) (first moment: a sign, 4 bits of exponent, 3 of mantissa) or 2^(31 - b)
-// (second moment, 5 and 3): what the scaling takes into fp32's subnormal range is the
-// code's too.  So coding is a scaling, an addition of the rounding and a shift, decoding
-// a shift and a scaling, both exact: an unchanged value is held unchanged even when its
-// block's exponent moves.
+// (second moment, 5 and 3): what the scaling takes into fp32's subnormal range, where it
+// rounds to 2^-20 of the smallest code, is the code's too.  So coding is a scaling, an
+// addition of the rounding and a shift, decoding a shift and a scaling, both exact: an
+// unchanged value is held unchanged even when its block's exponent moves.
 //   - Rounding to nearest stops a slow average: the second moment changes by 1 - beta2 of
 //     itself in a step, a code's step is 6 to 12 %.  With random bits below the code
 //     instead of half a step, the expected value of what is held is the moment.
@@ -34,8 +34,11 @@ typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
 constexpr uint32_t kInf = 0x7F800000u;
 
 // Random bits of elements i .. i + 3 (i a multiple of 4): two rounds of shifts and
-// products, with constants of a published search for little bias.  The four differ in two
-// bits until the first product, so one product gives the others' by additions.
+// products.  The two multipliers are from C. Wellons' "Prospecting for Hash Functions"
+// (2018), a search for little bias; the multiplier that gives the second moment's bits from
+// the first's is a prime next to 2^32 over the golden ratio (D. Knuth, TAOCP 3, 6.4).  The
+// four differ in two bits until the first product, so one product gives the others' by
+// additions.
 __device__ __forceinline__ void random_bits(const TensorsArgs& a, int64_t i, uint32_t x[4]) {
   constexpr uint32_t kFirst = 0x7FEB352Du;
   uint32_t y = (uint32_t)i ^ a.key_lo;
@@ -322,8 +325,8 @@ __device__ __forceinline__ void step_unit(const TensorsArgs& a, int k, int64_t f
 // and do not use), or of four with seven.  More waves than it takes to keep the memory
 // busy only spread what they read and write: 92 M elements with states in 32 bits take 422
 // us with 12 waves, 438 with 20, 445 with all 32; the states in 8 bits take more
-// arithmetic (about 580 instructions a unit beside 300), and with it 28 waves: 218 M
-// elements 568 us, with 16 797.
+// arithmetic (620 vector instructions a unit beside 300), and with it 28 waves: 218 M
+// elements 578 us, with 16 797.
 template <int kBits>
 constexpr int kThreads = kBits == 8 ? 256 : 64;
 template <int kBits>

@@ -105,6 +105,8 @@ int fl_adamw_tensors(int64_t count, const fl_tensor* tensors, const void* const*
   a.grad_scale = grad_scale;
   a.grad_f32 = grad_dtype == FL_F32;
   a.drawn = seed != 0;
+  // (odd multipliers: 2^64 over the golden ratio, and over the root of x^4 = x + 1, its
+  // counterpart in three dimensions)
   const uint64_t key = seed * 0x9E3779B97F4A7C15ull + (uint64_t)step * 0xD1B54A32D192ED03ull;
   a.key_lo = (uint32_t)key, a.key_hi = (uint32_t)(key >> 32);
   a.state = state_at(state, units, state_bits);

@@ -1030,7 +1030,8 @@ def fl_adamw_tensors(tensors, hp, step, grads, state, grad_scale=1.0, seed=0, st
     """One AdamW step of all `tensors` (a Tensors): grads holds a contiguous bf16 or
     float32 gradient (all of one dtype) for each, or None for one that is left alone;
     state as Tensors.state gives it, updated.  seed: nonzero rounds 8-bit moments by
-    random bits, whose expected value is the moment; 0 to nearest."""
+    random bits of the seed and the step, whose expected value is the moment (captured into
+    a graph, the same bits at each replay); 0 to nearest."""
     torch = _T or _torch()
     count, sizes = tensors.count, tensors.sizes
     dev = _dev() if tensors.device is not None else None
