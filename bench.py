@@ -30,7 +30,7 @@ PLACEMENTS = {
     "torch": (None, "torch's caching allocator"),
 }
 KERNEL_SOURCES = [os.path.join(ROOT, "paper_2609_20359_amd", "csrc", f)
-                  for f in ("flround_kernels.hip", "flr_internal.h")]
+                  for f in ("flround_kernels.hip", "flr_device.h", "flr_internal.h")]
 
 
 def log(*a):

@@ -155,3 +155,21 @@ def test_every_placement_choice_names_an_exported_function():
         assert label
         assert fn is None or callable(getattr(P, fn)), name
     assert bench.PLACEMENTS["staggered"][0] == "place_arrays"
+
+
+def test_kernel_source_hash_covers_the_kernels_headers():
+    """The code that the counters measured, wherever it stands: the round's kernels and
+    every header of the library that they include, directly or not."""
+    import os
+    import re
+
+    todo, seen = [p for p in bench.KERNEL_SOURCES if p.endswith(".hip")], set()
+    while todo:
+        p = todo.pop()
+        if p in seen:
+            continue
+        seen.add(p)
+        with open(p) as f:
+            names = re.findall(r'^#include "(flr_\w+\.h)"', f.read(), flags=re.M)
+        todo += [os.path.join(os.path.dirname(p), n) for n in names]
+    assert seen == set(bench.KERNEL_SOURCES)
