@@ -199,8 +199,8 @@ __device__ __forceinline__ u32x4 load_some(const T* row, int64_t at, int64_t n) 
 // term not for a root mean square), and the workgroup's sums of dy xh and of dy, which it
 // holds in registers over all of its rows, R at a time.  kNext: the next rows are asked
 // for while these are summed.  (16384 x 4096 bf16, two rows of eight waves, inputs past the
-// caches: 68 us, 6.0 TB/s, and 5 for the parts, 71 in all; through the caches 74, and so four
-// waves of two chunks 76.7, without the next rows 78.6.)
+// caches: 68 us, 6.0 TB/s, and 5 for the parts, 70 in all; through the caches 75, and so four
+// waves of two chunks 77, without the next rows 79.)
 template <typename T, int W, int K, int R, bool kRms, bool kNext, bool kPast>
 __global__ void __launch_bounds__(64 * W * R) k_norm_grad(const NormArgs a) {
   constexpr int E = Rows<T>::kE;
